@@ -376,6 +376,149 @@ gs_status gs_masked_linear_backward(const void* x_dev, const void* W_dev, const 
                                     int64_t T, const float* dsdl_dev, float* dlogits_dev, void* dx_dev,
                                     void* workspace_dev, size_t workspace_bytes, void* stream);
 
+/* ------------------------------------------------------------------------
+ * What stands between the projections when a pruned block is served: the norm
+ * before them, adapters beside them, and attention over a paged cache between
+ * the q, k, v and the output projection.  The paper has no counterpart (it
+ * evaluates inside an existing model); the mathematics is the LLaMA-2 / Qwen2.5
+ * blocks', whose projections the paper prunes.
+ *
+ * These calls need no handle: they read and write the caller's tensors, allocate
+ * nothing, synchronize nothing and may be captured into a CUDA graph.  Lengths,
+ * offsets and page tables are device tensors that the kernels read when they
+ * run, so a captured graph follows new values in them.  Values that would reach
+ * outside a tensor (a page number, a position, an adapter, an offset) are never
+ * followed: each call says what happens to such a token.
+ * ------------------------------------------------------------------------ */
+
+/*
+ * gs_add_rms_norm - h = x + residual, y = h * rsqrt(mean(h^2) + eps) * w per row.
+ * y is formed from the float32 h and rounded once.
+ *
+ * x_dev         bf16 [T][n].
+ * residual_dev  bf16 [T][n], or NULL (h = x).
+ * w_dev         bf16 [n].
+ * T, n          T >= 0 (0 is a no-op), 1 <= n <= 2^24.
+ * eps           >= 0 and finite.
+ * h_dev         bf16 [T][n] or NULL: the residual stream for the next call.  May
+ *               be residual_dev or x_dev itself.
+ * y_dev         bf16 [T][n] or NULL.  May be x_dev itself.
+ * y8_dev        e4m3 [T][n] or NULL: y / scale, rounded to nearest even, with
+ * scales_dev    float32 [T][ceil(n / group)] (group 0: [T]) and
+ *               scale = max(max|y| / 448, 2^-126) over the group's columns.
+ * group         0 (one scale a row) or 128; read with y8_dev only.
+ * One of y_dev and y8_dev at least; y8_dev and scales_dev overlap nothing else.
+ * A NaN or an infinity stays in its row (with an infinity the row's other values
+ * are zero; in 8 bits an infinite or NaN y is NaN).
+ * Errors: INVALID_ARG, UNSUPPORTED (group), CUDA.
+ */
+gs_status gs_add_rms_norm(const void* x_dev, const void* residual_dev, const void* w_dev, int64_t T, int64_t n, float eps,
+                          void* h_dev, void* y_dev, void* y8_dev, float* scales_dev, int32_t group, void* stream);
+
+/* One projection's low-rank adapters, and the activations of a call. */
+typedef struct gs_adapter_layer {
+  const void* x_dev;       /* bf16 [T][in]: what the projection read                     */
+  const void* base_dev;    /* bf16 [T][out]: what it wrote (gs_linear's y)               */
+  void* out_dev;           /* bf16 [T][out]; may be base_dev itself                      */
+  const void* A_dev;       /* bf16 [n_adapters][rank][in]                                */
+  const void* B_dev;       /* bf16 [n_adapters][out][rank]                               */
+  const float* scale_dev;  /* float32 [n_adapters] (alpha / rank)                        */
+  int64_t in, out;         /* in a multiple of 8; out >= 1; in, out < 2^31, out * rank and in * rank too */
+  int32_t n_adapters;      /* >= 1                                                       */
+  int32_t rank;            /* a multiple of 8, 8 ... 128 (lower ranks: pad with zeros)   */
+} gs_adapter_layer;
+
+/*
+ * gs_adapters_batched - out[t] = base[t] + scale_a B_a (A_a x[t]) for the n layers of
+ * one call, where token t belongs to sequence i with offsets[i] <= t < offsets[i + 1]
+ * and a = ids[i].  float32 sums, one rounding, at the output.  A sequence whose id is
+ * outside [0, n_adapters) has no adapter: out = base.
+ *
+ * offsets_dev  int32 [n_seqs + 1], non-decreasing, from 0 to T: the tokens of each
+ *              sequence (empty ones allowed).  Tokens that no sequence holds are not
+ *              written.
+ * ids_dev      int32 [n_seqs].
+ * n            0 ... 8 layers (0 is a no-op), one launch.  Outputs of different layers
+ *              do not overlap.
+ * Errors: INVALID_ARG, UNSUPPORTED (rank), CUDA.
+ */
+gs_status gs_adapters_batched(int32_t n, const gs_adapter_layer* layers, const int32_t* offsets_dev, const int32_t* ids_dev,
+                              int32_t n_seqs, int64_t T, void* stream);
+
+/* The keys and values of one layer: bf16 [pages][kv_heads][page_size][head_dim] each. */
+typedef struct gs_paged_cache {
+  void* k_dev;
+  void* v_dev;
+  int64_t pages;
+  int32_t page_size;       /* 16, 32, 64, 128 or 256                                     */
+  int32_t kv_heads;
+  int32_t head_dim;        /* 64 or 128                                                  */
+} gs_paged_cache;
+
+/*
+ * One step's sequences.  Sequence i brings the new tokens offsets[i] ... offsets[i + 1] - 1;
+ * with them it is kv_lens[i] tokens long, so its j-th new token has position
+ * kv_lens[i] - (offsets[i + 1] - offsets[i]) + j.  Position p lives in page
+ * table[i][p / page_size], slot p % page_size; entries past a sequence's length are not
+ * read.  Sequences without new tokens are allowed.
+ */
+typedef struct gs_seq_batch {
+  const int32_t* offsets_dev;   /* [n + 1], non-decreasing, from 0 to tokens             */
+  const int32_t* kv_lens_dev;   /* [n]                                                   */
+  const int32_t* table_dev;     /* [n][table_width]                                      */
+  int32_t n;
+  int32_t table_width;          /* table_width * page_size < 2^31                        */
+  int64_t tokens;               /* < 2^31                                                */
+  int32_t max_new;              /* at least the most new tokens of a sequence            */
+} gs_seq_batch;
+
+/*
+ * gs_cache_append - rotary embedding of a step's queries and keys, and its keys and
+ * values into the cache.  Channels i and i + head_dim / 2 are a pair, turned by row p
+ * (the token's position) of the angle tables: (a, b) -> (a cos - b sin, b cos + a sin).
+ *
+ * q_dev  bf16 [tokens][q_heads][head_dim], consecutive tokens q_stride elements apart
+ *        (a column slice of a joint projection's output); k_dev, v_dev
+ *        [tokens][kv_heads][head_dim] likewise.  Strides are multiples of 8.
+ * cos_dev, sin_dev  float32 [n_pos][head_dim / 2], 16-byte aligned.
+ * q_out_dev  bf16 [tokens][q_heads][head_dim], dense; may be q_dev itself where that is dense.
+ * A token without a place (no sequence, a negative position, one at or past n_pos or
+ * table_width * page_size, a page number outside [0, pages)) writes no key and no value;
+ * without a position in [0, n_pos) its query is copied as it is.
+ * Errors: INVALID_ARG, UNSUPPORTED (page_size, head_dim, more than 2^31 blocks), CUDA.
+ */
+gs_status gs_cache_append(const gs_paged_cache* cache, const gs_seq_batch* batch, const void* q_dev, int64_t q_stride,
+                          int32_t q_heads, const void* k_dev, int64_t k_stride, const void* v_dev, int64_t v_stride,
+                          const float* cos_dev, const float* sin_dev, int64_t n_pos, void* q_out_dev, void* stream);
+
+/*
+ * gs_paged_attention - causal attention of a step's queries over the cache: with
+ * p the token's position, out = sum_j softmax_j(scale q.k_j) v_j over j = 0 ... p of
+ * its sequence; query head h reads key head h / (q_heads / kv_heads).  One token per
+ * sequence, chunks of a prompt, whole prompts (kv_lens = the new tokens) and any mix.
+ * float32 scores, sums and softmax; the weights are rounded to bf16 for the second
+ * product.  A token without visible keys (a negative position, no sequence) gets zeros.
+ * Lengths beyond table_width * page_size are cut to it.
+ * Values of masked keys, whatever they are (infinities and NaN among them), and memory
+ * past a sequence's length in its last page do not reach the result; pages outside
+ * [0, pages) read as zeros.
+ *
+ * q_dev  bf16 [tokens][q_heads][head_dim], tokens q_stride elements apart (a multiple of 8).
+ * out_dev  bf16 [tokens][q_heads][head_dim], dense, fully overwritten.
+ * scale  finite.
+ * workspace_dev  gs_paged_attention_workspace bytes, 16-byte aligned, zero before its
+ *         first use; calls leave the part zero that has to be, so it serves one call
+ *         after another on one stream without being cleared.
+ * max_new chooses the kernels; a sequence with more new tokens than it says is served
+ * all the same, or (if max_new is below what needs the chunk kernel) gets zeros.
+ * Errors: INVALID_ARG, UNSUPPORTED (page_size, head_dim, more than 64 query heads a key
+ * head), CUDA.
+ */
+gs_status gs_paged_attention_workspace(const gs_paged_cache* cache, const gs_seq_batch* batch, int32_t q_heads, size_t* bytes);
+gs_status gs_paged_attention(const gs_paged_cache* cache, const gs_seq_batch* batch, const void* q_dev, int64_t q_stride,
+                             int32_t q_heads, float scale, void* out_dev, void* workspace_dev, size_t workspace_bytes,
+                             void* stream);
+
 /*
  * Test hooks for the failure paths (the paper has no counterpart; they exist
  * so that the error handling can be exercised without faulting a GPU).

@@ -25,6 +25,22 @@ _c_i32p = ctypes.POINTER(ctypes.c_int32)
 _c_u16p = ctypes.POINTER(ctypes.c_uint16)
 
 
+class _AdapterLayer(ctypes.Structure):   # gs_adapter_layer
+    _fields_ = [("x", ctypes.c_void_p), ("base", ctypes.c_void_p), ("out_ptr", ctypes.c_void_p), ("A", ctypes.c_void_p),
+                ("B", ctypes.c_void_p), ("scale", ctypes.c_void_p), ("inp", ctypes.c_int64), ("out", ctypes.c_int64),
+                ("n_adapters", ctypes.c_int32), ("rank", ctypes.c_int32)]
+
+
+class _CacheStruct(ctypes.Structure):    # gs_paged_cache
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("pages", ctypes.c_int64), ("page_size", ctypes.c_int32),
+                ("kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32)]
+
+
+class _BatchStruct(ctypes.Structure):    # gs_seq_batch
+    _fields_ = [("offsets", ctypes.c_void_p), ("kv_lens", ctypes.c_void_p), ("table", ctypes.c_void_p), ("n", ctypes.c_int32),
+                ("table_width", ctypes.c_int32), ("tokens", ctypes.c_int64), ("max_new", ctypes.c_int32)]
+
+
 def _load(path: Path = LIB_PATH) -> ctypes.CDLL:
     if not path.exists():
         raise ImportError(f"{path} is missing: build it with `python -c 'import __graft_entry__ as g; g.build()'`")
@@ -53,13 +69,19 @@ def _load(path: Path = LIB_PATH) -> ctypes.CDLL:
     lib.gs_gumbel_select.argtypes = [vp, vp, i64, ctypes.c_float, vp, vp, vp, vp]
     lib.gs_masked_linear_backward_workspace.argtypes = [vp, i32, ctypes.POINTER(ctypes.c_size_t)]
     lib.gs_masked_linear_backward.argtypes = [vp, vp, vp, vp, i64, vp, vp, vp, vp, ctypes.c_size_t, vp]
+    lib.gs_add_rms_norm.argtypes = [vp, vp, vp, i64, i64, ctypes.c_float, vp, vp, vp, vp, i32, vp]
+    lib.gs_adapters_batched.argtypes = [i32, vp, vp, vp, i32, i64, vp]
+    lib.gs_cache_append.argtypes = [vp, vp, vp, i64, i32, vp, i64, vp, i64, vp, vp, i64, vp, vp]
+    lib.gs_paged_attention_workspace.argtypes = [vp, vp, i32, ctypes.POINTER(ctypes.c_size_t)]
+    lib.gs_paged_attention.argtypes = [vp, vp, vp, i64, i32, ctypes.c_float, vp, vp, ctypes.c_size_t, vp]
     lib.gs_debug_fail_alloc.argtypes = [i64]
     lib.gs_debug_inject_wait.argtypes = [ctypes.c_int, ctypes.c_uint64]
     for fn in (lib.gs_pack, lib.gs_linear, lib.gs_linear_ex, lib.gs_linear_batched, lib.gs_unpack,
                lib.gs_packed_info, lib.gs_packed_export, lib.gs_device_status, lib.gs_select_groups,
                lib.gs_preserved_rates, lib.gs_debug_fail_alloc, lib.gs_debug_inject_wait, lib.gs_pack_groups,
                lib.gs_packed_group_shape, lib.gs_gumbel_select, lib.gs_masked_linear_backward_workspace,
-               lib.gs_masked_linear_backward):
+               lib.gs_masked_linear_backward, lib.gs_add_rms_norm, lib.gs_adapters_batched, lib.gs_cache_append,
+               lib.gs_paged_attention_workspace, lib.gs_paged_attention):
         fn.restype = ctypes.c_int
     return lib
 
@@ -356,6 +378,228 @@ def masked_linear_backward(x: torch.Tensor, W: torch.Tensor, p: Packed, dy: torc
                                          ws.data_ptr(), nbytes.value, _stream_ptr(stream)),
            "gs_masked_linear_backward")
     return dl, dx
+
+
+# --------------------------------------------------------------------------
+# the operators around a served block's projections
+# --------------------------------------------------------------------------
+
+def _empty(shape, dtype: torch.dtype, device, stream: Optional[torch.cuda.Stream]) -> torch.Tensor:
+    """A new tensor that belongs to the stream the call runs on."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=device)
+
+
+def _norm(x, weight, residual, eps, h, y, y8, scales, group, stream):
+    _require_cuda(x, torch.bfloat16, "x")
+    _require_cuda(weight, torch.bfloat16, "weight")
+    T, n = x.shape
+    if weight.shape != (n,):
+        raise ValueError("x must be [T, n] and weight [n]")
+    for t, name in ((residual, "residual"), (h, "h"), (y, "y")):
+        if t is not None:
+            _require_cuda(t, torch.bfloat16, name)
+            if t.shape != (T, n):
+                raise ValueError(f"{name} must have x's shape")
+    ptr = [None if t is None else t.data_ptr() for t in (residual, h, y, y8, scales)]
+    _check(lib.gs_add_rms_norm(x.data_ptr(), ptr[0], weight.data_ptr(), T, n, eps, ptr[1], ptr[2], ptr[3], ptr[4], group,
+                               _stream_ptr(stream)), "gs_add_rms_norm")
+
+
+def add_rms_norm(x: torch.Tensor, weight: torch.Tensor, residual: Optional[torch.Tensor] = None, eps: float = 1e-5,
+                 h: Optional[torch.Tensor] = None, y: Optional[torch.Tensor] = None,
+                 stream: Optional[torch.cuda.Stream] = None):
+    """h = x + residual, y = h / sqrt(mean(h^2) + eps) * weight over the rows of x [T, n]: (y, h), both bf16.
+    Without a residual, h is None unless it was given (a copy of x then).  h may be the residual's or x's own
+    tensor, y x's own."""
+    if y is None:
+        y = _empty(x.shape, torch.bfloat16, x.device, stream)
+    if h is None and residual is not None:
+        h = _empty(x.shape, torch.bfloat16, x.device, stream)
+    _norm(x, weight, residual, eps, h, y, None, None, 0, stream)
+    return y, h
+
+
+def add_rms_norm_fp8(x: torch.Tensor, weight: torch.Tensor, residual: Optional[torch.Tensor] = None, eps: float = 1e-5,
+                     group: int = 0, h: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None):
+    """add_rms_norm with y in 8 bits: (y8 e4m3 [T, n], scales float32 [T, groups], h), y = y8 * scales of the
+    element's group of columns (0: one group a row; 128)."""
+    y8 = _empty(x.shape, torch.float8_e4m3fn, x.device, stream)
+    scales = _empty((x.shape[0], -(-x.shape[1] // group) if group > 0 else 1), torch.float32, x.device, stream)
+    if h is None and residual is not None:
+        h = _empty(x.shape, torch.bfloat16, x.device, stream)
+    _norm(x, weight, residual, eps, h, None, y8, scales, group, stream)
+    return y8, scales, h
+
+
+class Adapters:
+    """The low-rank adapters of one projection: A [n, rank, in], B [n, out, rank] (bf16) and scale [n] (float32,
+    alpha / rank).  Ranks that are no multiple of 8 are padded with zeros, once, here."""
+
+    def __init__(self, A: torch.Tensor, B: torch.Tensor, scale: torch.Tensor):
+        for t, dt, name in ((A, torch.bfloat16, "A"), (B, torch.bfloat16, "B"), (scale, torch.float32, "scale")):
+            _require_cuda(t, dt, name)
+        if A.dim() != 3 or B.dim() != 3 or B.shape[0] != A.shape[0] or B.shape[2] != A.shape[1] or scale.shape != A.shape[:1]:
+            raise ValueError("A must be [n, rank, in], B [n, out, rank] and scale [n]")
+        pad = -A.shape[1] % 8
+        if pad:
+            A = torch.nn.functional.pad(A, (0, 0, 0, pad))
+            B = torch.nn.functional.pad(B, (0, pad))
+        self.A, self.B, self.scale = A, B, scale
+        self.n, self.rank, self.inp = A.shape
+        self.out = B.shape[1]
+
+
+def adapters_batched_into(xs: Sequence[torch.Tensor], bases: Sequence[torch.Tensor], ads: Sequence[Adapters],
+                          offsets: torch.Tensor, ids: torch.Tensor, outs: Sequence[torch.Tensor],
+                          stream: Optional[torch.cuda.Stream] = None) -> None:
+    """outs[i] = bases[i] + scale_a B_a (A_a xs[i]) for up to 8 layers of one step: sequence s has the tokens
+    offsets[s] ... offsets[s + 1] - 1 (int32 [n + 1]) and the adapter a = ids[s] (int32 [n]; outside [0, n): none).
+    outs[i] may be bases[i] itself, e.g. what linear_batched_into wrote."""
+    n = len(ads)
+    if not (len(xs) == len(bases) == len(outs) == n):
+        raise ValueError("xs, bases, ads, outs must have the same length")
+    if n == 0:
+        return
+    _require_cuda(offsets, torch.int32, "offsets")
+    _require_cuda(ids, torch.int32, "ids")
+    if offsets.dim() != 1 or ids.dim() != 1 or offsets.shape[0] != ids.shape[0] + 1:
+        raise ValueError("offsets must be [n + 1] and ids [n]")
+    T = xs[0].shape[0]
+    arr = (_AdapterLayer * n)()
+    for l, x, base, ad, out in zip(arr, xs, bases, ads, outs):
+        _require_cuda(x, torch.bfloat16, "x")
+        _require_cuda(base, torch.bfloat16, "base")
+        if out is not base:
+            _require_cuda(out, torch.bfloat16, "out")
+        if x.shape != (T, ad.inp) or base.shape != (T, ad.out) or out.shape != (T, ad.out):
+            raise ValueError("every x must be [T, in_i], base and out [T, out_i] with one T")
+        l.x, l.base, l.out_ptr = x.data_ptr(), base.data_ptr(), out.data_ptr()
+        l.A, l.B, l.scale = ad.A.data_ptr(), ad.B.data_ptr(), ad.scale.data_ptr()
+        l.inp, l.out, l.n_adapters, l.rank = ad.inp, ad.out, ad.n, ad.rank
+    _check(lib.gs_adapters_batched(n, arr, offsets.data_ptr(), ids.data_ptr(), ids.shape[0], T, _stream_ptr(stream)),
+           "gs_adapters_batched")
+
+
+def adapters_into(x: torch.Tensor, base: torch.Tensor, ad: Adapters, offsets: torch.Tensor, ids: torch.Tensor,
+                  out: torch.Tensor, stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+    """out = base + scale_a B_a (A_a x) for one layer (see adapters_batched_into)."""
+    adapters_batched_into((x,), (base,), (ad,), offsets, ids, (out,), stream)
+    return out
+
+
+def linear_adapted(x: torch.Tensor, p: Packed, ad: Adapters, offsets: torch.Tensor, ids: torch.Tensor,
+                   stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+    """The packed projection with its requests' adapters: y = x (W (.) M)^T + scale_a B_a (A_a x)."""
+    y = linear_into(x, p, _empty((x.shape[0], p.out), torch.bfloat16, x.device, stream), stream=stream)
+    return adapters_into(x, y, ad, offsets, ids, y, stream)
+
+
+class PagedCache:
+    """Keys and values of one layer, bf16 [pages, kv_heads, page_size, head_dim] each, and the attention's
+    workspace for each stream that uses it (views of one tensor per layer share nothing)."""
+
+    def __init__(self, k_pages: torch.Tensor, v_pages: torch.Tensor):
+        _require_cuda(k_pages, torch.bfloat16, "k_pages")
+        _require_cuda(v_pages, torch.bfloat16, "v_pages")
+        if k_pages.dim() != 4 or v_pages.shape != k_pages.shape:
+            raise ValueError("k_pages and v_pages must both be [pages, kv_heads, page_size, head_dim]")
+        self.k_pages, self.v_pages = k_pages, v_pages
+        self.pages, self.kv_heads, self.page_size, self.head_dim = k_pages.shape
+        self._c = _CacheStruct(k_pages.data_ptr(), v_pages.data_ptr(), self.pages, self.page_size, self.kv_heads, self.head_dim)
+        self._ref = ctypes.addressof(self._c)
+        self._need = {}
+        self._ws = {}
+
+    def _workspace(self, batch: "Batch", q_heads: int, stream: Optional[torch.cuda.Stream], sp: int) -> torch.Tensor:
+        need = self._need.get(q_heads)
+        if need is None:
+            c = ctypes.c_size_t()
+            _check(lib.gs_paged_attention_workspace(self._ref, batch._ref, q_heads, ctypes.byref(c)),
+                   "gs_paged_attention_workspace")
+            need = self._need[q_heads] = c.value
+        ws = self._ws.get(sp)
+        if ws is None or ws.numel() < need:
+            with torch.cuda.stream(stream if stream is not None else torch.cuda.current_stream()):
+                ws = self._ws[sp] = torch.zeros((max(need, 16),), dtype=torch.uint8, device=self.k_pages.device)
+        return ws
+
+
+class Batch:
+    """One step's sequences, made once for all layers.  Sequence i brings the tokens offsets[i] ... offsets[i + 1] - 1
+    (int32 [n + 1]), is kv_lens[i] tokens long with them (int32 [n]) and keeps position p in page
+    table[i, p // page_size] (int32 [n, width]).  max_new: at least the most new tokens of a sequence."""
+
+    def __init__(self, offsets: torch.Tensor, kv_lens: torch.Tensor, table: torch.Tensor, max_new: int):
+        for t, name in ((offsets, "offsets"), (kv_lens, "kv_lens"), (table, "table")):
+            _require_cuda(t, torch.int32, name)
+        n = kv_lens.numel()
+        if offsets.shape != (n + 1,) or kv_lens.dim() != 1 or table.dim() != 2 or table.shape[0] != n:
+            raise ValueError("offsets must be [n + 1], kv_lens [n] and table [n, width]")
+        self.offsets, self.kv_lens, self.table, self.max_new = offsets, kv_lens, table, int(max_new)
+        self._c = _BatchStruct(offsets.data_ptr(), kv_lens.data_ptr(), table.data_ptr(), n, table.shape[1], 0, self.max_new)
+        self._ref = ctypes.addressof(self._c)
+
+
+def _heads(t: torch.Tensor, D: int, name: str) -> int:
+    """The distance of two tokens of [T, heads, D], whose heads lie side by side (a slice of a joint projection may)."""
+    if not t.is_cuda:
+        raise ValueError(f"{name} must be a CUDA tensor")
+    if t.dtype != torch.bfloat16:
+        raise ValueError(f"{name} must be torch.bfloat16, got {t.dtype}")
+    if t.dim() != 3 or t.shape[2] != D or t.stride(2) != 1 or (t.stride(1) != D and t.shape[1] != 1):
+        raise ValueError(f"{name} must be [T, heads, {D}] with dense heads")
+    return t.stride(0) if t.shape[0] != 1 else t.shape[1] * D
+
+
+def cache_append(cache: PagedCache, batch: Batch, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cos: torch.Tensor,
+                 sin: torch.Tensor, q_out: Optional[torch.Tensor] = None,
+                 stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+    """Turns q [T, q_heads, D] and k [T, kv_heads, D] by their positions' angles (cos, sin: float32 [positions, D / 2];
+    channels i and i + D / 2 are a pair), writes k and v into the cache's pages and returns the turned q (q_out)."""
+    D = cache.head_dim
+    qs, ks, vs = _heads(q, D, "q"), _heads(k, D, "k"), _heads(v, D, "v")
+    T = q.shape[0]
+    if k.shape[0] != T or v.shape[0] != T or k.shape[1] != cache.kv_heads or v.shape[1] != cache.kv_heads:
+        raise ValueError("k and v must be [T, kv_heads, D] with q's T")
+    _require_cuda(cos, torch.float32, "cos")
+    _require_cuda(sin, torch.float32, "sin")
+    if cos.dim() != 2 or cos.shape[1] != D // 2 or sin.shape != cos.shape:
+        raise ValueError("cos and sin must be [positions, head_dim / 2]")
+    if q_out is None:
+        q_out = _empty(q.shape, torch.bfloat16, q.device, stream)
+    else:
+        _require_cuda(q_out, torch.bfloat16, "q_out")
+        if q_out.shape != q.shape:
+            raise ValueError("q_out must have q's shape")
+    batch._c.tokens = T
+    _check(lib.gs_cache_append(cache._ref, batch._ref, q.data_ptr(), qs, q.shape[1], k.data_ptr(), ks, v.data_ptr(), vs,
+                               cos.data_ptr(), sin.data_ptr(), cos.shape[0], q_out.data_ptr(), _stream_ptr(stream)),
+           "gs_cache_append")
+    return q_out
+
+
+def paged_attention(q: torch.Tensor, cache: PagedCache, batch: Batch, scale: Optional[float] = None,
+                    out: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+    """Causal attention of a step's queries q [T, q_heads, D] over the cache (the step's own keys are in it already:
+    cache_append), bf16 [T, q_heads, D].  scale: 1 / sqrt(D) if not given.  A token without visible keys gets zeros."""
+    D = cache.head_dim
+    qs = _heads(q, D, "q")
+    if out is None:
+        out = _empty(q.shape, torch.bfloat16, q.device, stream)
+    else:
+        _require_cuda(out, torch.bfloat16, "out")
+        if out.shape != q.shape:
+            raise ValueError("out must have q's shape")
+    batch._c.tokens = q.shape[0]
+    sp = _stream_ptr(stream)
+    ws = cache._workspace(batch, q.shape[1], stream, sp)
+    _check(lib.gs_paged_attention(cache._ref, batch._ref, q.data_ptr(), qs, q.shape[1],
+                                  D ** -0.5 if scale is None else scale, out.data_ptr(), ws.data_ptr(), ws.numel(), sp),
+           "gs_paged_attention")
+    return out
 
 
 def debug_fail_alloc(nth: int) -> None:
