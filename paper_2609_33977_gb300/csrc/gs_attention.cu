@@ -3,23 +3,12 @@
 // One warp per (token, query head): 32 keys at a time, one per lane for the scores
 // (a lane reads its key's whole row), then each lane owns head_dim / 32 channels of
 // the output.  Running maximum and sum in float32.
-#include "gs_block.cuh"
+#include "gs_attn.cuh"
+
+#include <cmath>
 
 namespace gs {
 namespace {
-
-struct AttnParams {
-  const uint16_t* q;
-  const uint16_t* k;
-  const uint16_t* v;
-  uint16_t* out;
-  const int32_t* offsets;
-  const int32_t* kv_lens;
-  const int32_t* table;
-  int64_t q_stride, tokens, pages;
-  int32_t n_seqs, width, page_shift, q_heads, kv_heads;
-  float scale;
-};
 
 template <int D>
 __global__ void __launch_bounds__(128) k_attention_simple(const AttnParams P) {
@@ -28,7 +17,7 @@ __global__ void __launch_bounds__(128) k_attention_simple(const AttnParams P) {
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int head = (int)blockIdx.y * 4 + warp;
   const int seq = block_count_le(P.offsets, P.n_seqs, (int)t);
-  if (head >= P.q_heads) return;
+  if (head >= P.q_heads || seq >= P.n_seqs || seq_info(P, seq).rows < P.min_rows) return;
   int64_t seen = 0;
   if (seq < P.n_seqs) {
     const int64_t first = P.offsets[seq], end = P.offsets[seq + 1];
@@ -56,14 +45,14 @@ __global__ void __launch_bounds__(128) k_attention_simple(const AttnParams P) {
       s = 0.f;
       if (at >= 0)
         for (int i = 0; i < D; ++i) s = fmaf(qs[warp][i], bf16_lo(P.k[at * D + i]), s);
-      s *= P.scale;
+      s *= P.negate ? -P.scale_log2 : P.scale_log2;
     }
     float top = s;
 #pragma unroll
     for (int d = 16; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
     const float mn = fmaxf(m, top), base = mn == -INFINITY ? 0.f : mn;
-    const float p = j < seen ? __expf(s - base) : 0.f;
-    const float f = m == -INFINITY ? 0.f : __expf(m - base);
+    const float p = j < seen ? ex2(s - base) : 0.f;
+    const float f = m == -INFINITY ? 0.f : ex2(m - base);
     float sum = p;
 #pragma unroll
     for (int d = 16; d > 0; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
@@ -87,10 +76,18 @@ __global__ void __launch_bounds__(128) k_attention_simple(const AttnParams P) {
 
 }  // namespace
 
-size_t attention_workspace_bytes(const gs_paged_cache&, const gs_seq_batch&, int32_t) { return 0; }
+// counters, then the parts of split items (16-byte aligned)
+constexpr int64_t kCounterBytes = 4096;
+static_assert(kCounterBytes >= 4 * 256, "one counter a CTA");
+
+int attention_ctas() { return sm_count() < 256 ? sm_count() : 256; }
+
+size_t attention_workspace_bytes(const gs_paged_cache& c, const gs_seq_batch&, int32_t) {
+  return (size_t)kCounterBytes + (size_t)attention_ctas() * 2 * 64 * (size_t)(c.head_dim + 2) * 4;
+}
 
 gs_status launch_paged_attention(const gs_paged_cache& c, const gs_seq_batch& b, const void* q, int64_t q_stride,
-                                 int32_t q_heads, float scale, void* out, void*, cudaStream_t s) {
+                                 int32_t q_heads, float scale, void* out, void* ws, cudaStream_t s) {
   AttnParams P;
   P.q = static_cast<const uint16_t*>(q);
   P.k = static_cast<const uint16_t*>(c.k_dev);
@@ -99,6 +96,10 @@ gs_status launch_paged_attention(const gs_paged_cache& c, const gs_seq_batch& b,
   P.offsets = b.offsets_dev;
   P.kv_lens = b.kv_lens_dev;
   P.table = b.table_dev;
+  P.cnt = static_cast<int32_t*>(ws);
+  P.parts = reinterpret_cast<float*>(static_cast<uint8_t*>(ws) + kCounterBytes);
+  P.err = device_error_flag();
+  if (!P.err) return GS_ERR_CUDA;
   P.q_stride = q_stride;
   P.tokens = b.tokens;
   P.pages = c.pages;
@@ -107,7 +108,21 @@ gs_status launch_paged_attention(const gs_paged_cache& c, const gs_seq_batch& b,
   P.page_shift = __builtin_ctz((unsigned)c.page_size);
   P.q_heads = q_heads;
   P.kv_heads = c.kv_heads;
-  P.scale = scale;
+  P.group = q_heads / c.kv_heads;
+  P.scale_log2 = std::fabs(scale) * 1.4426950408889634f;
+  P.negate = scale < 0.f;
+  const uint64_t rows = (uint64_t)c.pages * c.kv_heads * c.page_size;
+  const uint32_t box = (uint32_t)attn_rows_box(c.page_size);
+  if (!encode_tmap_slabs_bf16(&P.kmap, c.k_dev, (uint64_t)c.head_dim, rows, box, (uint32_t)c.head_dim / 64) ||
+      !encode_tmap_slabs_bf16(&P.vmap, c.v_dev, (uint64_t)c.head_dim, rows, box, (uint32_t)c.head_dim / 64))
+    return GS_ERR_CUDA;
+  const int64_t most = (int64_t)b.max_new * P.group;
+  P.min_rows = 1;
+  P.max_rows = attn_rows_most();
+  P.zero_rest = most <= attn_rows_most();
+  gs_status st = launch_attn_rows(P, c.head_dim, most < attn_rows_most() ? (int)most : attn_rows_most(), attention_ctas(), s);
+  if (st != GS_OK || P.zero_rest) return st;
+  P.min_rows = attn_rows_most() + 1;
   const dim3 grid((unsigned)b.tokens, (unsigned)((q_heads + 3) / 4));
   if (c.head_dim == 128) k_attention_simple<128><<<grid, 128, 0, s>>>(P);
   else k_attention_simple<64><<<grid, 128, 0, s>>>(P);
