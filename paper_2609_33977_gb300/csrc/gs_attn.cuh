@@ -39,6 +39,7 @@ struct AttnParams {
 // attn_rows.cu: sequences of at most attn_rows_most() rows; rows: a bound of theirs
 int attn_rows_most();
 int attn_rows_box(int page_size);   // rows of a TMA box
+int attn_rows_tile();               // keys of a unit
 gs_status launch_attn_rows(const AttnParams& P, int head_dim, int rows, int ctas, cudaStream_t s);
 
 struct SeqInfo {
@@ -71,47 +72,28 @@ __device__ __forceinline__ float ex2(float x) {
   return y;
 }
 
-// Tiles of an item, and where the items of a sequence lie.  Traits:
-//   kTile                                keys of a unit
-//   row_tiles(s, P)                      tiles of rows of a sequence (0: not this kernel's)
-//   tiles(s, P, rt)                      units of row tile rt, at least 1
-struct WorkSlot {   // a boundary between two CTAs
-  int64_t base;     // units before sequence r
-  int r;
-};
-
-// A CTA's share, the same for every thread.
-struct WorkRange {
-  int64_t total;   // units of the step
-  int64_t begin, end;
-  int64_t base;    // units before sequence r, which holds `begin`
-  int r;
-  int ctas;        // that share the units
-  int snap;
-};
-
-// Boundaries closer than this to an item's ends move there: a part shorter than the
-// cost of joining it is not worth its parallelism.  Where shares are long, a shift of
-// two units is small beside them; where they are short, joining costs more than four.
-__device__ __forceinline__ int snap_units(int64_t total, int ctas) { return total >= (int64_t)16 * ctas ? 2 : 4; }
-
+// Units are counted in 32 bits (the host refuses steps that could have more).  Traits:
+//   row_tiles(s, P)   tiles of rows of a sequence (0: not this kernel's)
+//   tiles(s, P, rt)   units of row tile rt, at least 1
+//   kLeast, kSnap     the least units worth a CTA; boundaries this close to an item's end move there
 template <class Traits>
-__device__ __forceinline__ int64_t seq_units(const AttnParams& P, const SeqInfo& s) {
+__device__ __forceinline__ int head_units(const AttnParams& P, const SeqInfo& s) {
   const int nr = Traits::row_tiles(s, P);
-  int64_t u = 0;
+  int u = 0;
   for (int i = 0; i < nr; ++i) u += Traits::tiles(s, P, i);
-  return u * P.kv_heads;
+  return u;
 }
 
-// The item of sequence s that holds unit `off` (counted from the sequence's first)
+// An item of a sequence: a key head and a row tile
 struct Item {
-  int h, rt, nt;       // key head, row tile, units
-  int64_t first;       // its first unit, from the sequence's first
+  int h, rt, nt;       // nt: its units
+  int first;           // its first unit, from the sequence's first
 };
+// the item that holds unit `off` of the sequence
 template <class Traits>
-__device__ __forceinline__ Item item_at(const AttnParams& P, const SeqInfo& s, int64_t off, int64_t per_head) {
+__device__ __forceinline__ Item item_at(const AttnParams& P, const SeqInfo& s, int off, int per_head) {
   Item it;
-  it.h = (int)(off / per_head);
+  it.h = off / per_head;
   it.first = it.h * per_head;
   const int nr = Traits::row_tiles(s, P);
   for (it.rt = 0; it.rt < nr; ++it.rt) {
@@ -122,69 +104,114 @@ __device__ __forceinline__ Item item_at(const AttnParams& P, const SeqInfo& s, i
   return it;
 }
 
-// Called by the whole block.  red: [34] int64 of shared memory; slots: [2].
+// total units over `ctas` CTAs: CTA c begins at c share + min(c, rest)
+struct Shares {
+  int total, ctas, share, rest;
+  // at least `least` units a CTA, unless there are CTAs for single items
+  __device__ __forceinline__ Shares(int n, int items, int most, int least) {
+    total = n;
+    ctas = max(1, min(most, max((n + least - 1) / least, items)));
+    share = n / ctas;
+    rest = n - share * ctas;
+  }
+  __device__ __forceinline__ int cut(int c) const { return c >= ctas ? total : c * share + min(c, rest); }
+  // the first boundary at or after unit v
+  __device__ __forceinline__ int first_cut(int v) const {
+    const int wide = rest * (share + 1);
+    return v <= wide ? (v + share) / (share + 1) : rest + (v - wide + share - 1) / share;
+  }
+};
+
+// Where a CTA begins and ends, in shared memory; written by divide_work.
+struct WorkSlot {
+  int at;         // the boundary, moved to an item's end where that is near
+  int base;       // units before sequence r
+  int r;          // the sequence that holds it (n_seqs: past the last)
+  int per_head;   // and its units a key head
+  SeqInfo s;
+};
+struct WorkShared {
+  int sums[2][32];
+  WorkSlot slot[2];
+};
+
+// Called by the whole block; afterwards every thread may read w.slot.  Boundaries within
+// Traits::kSnap units of an item's ends move there: a part that short is not worth the
+// cost of joining it.  Returns the division.
 template <class Traits, int THREADS>
-__device__ __forceinline__ WorkRange divide_work(const AttnParams& P, int cta, int ctas, int64_t* red, WorkSlot* slots) {
+__device__ __forceinline__ Shares divide_work(const AttnParams& P, int cta, WorkShared& w) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   constexpr int kW = THREADS / 32;
   static_assert(kW <= 32 && THREADS % 32 == 0, "block");
-  int64_t sum = 0;
-  for (int r = threadIdx.x; r < P.n_seqs; r += THREADS) sum += seq_units<Traits>(P, seq_info(P, r));
-#pragma unroll
-  for (int d = 16; d > 0; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
-  if (lane == 0) red[warp] = sum;
-  if (threadIdx.x < 2) slots[threadIdx.x] = WorkSlot{0, P.n_seqs};
-  __syncthreads();
-  WorkRange w;
-  w.total = 0;
-  for (int i = 0; i < kW; ++i) w.total += red[i];
-  // four units at least: a shorter share would end before its part is joined
-  const int64_t most = (w.total + 3) / 4;
-  w.ctas = (int)min((int64_t)ctas, max(most, (int64_t)1));
-  w.snap = snap_units(w.total, w.ctas);
-  const int64_t cut[2] = {min(cta, w.ctas) * w.total / w.ctas, min(cta + 1, w.ctas) * w.total / w.ctas};
-  __syncthreads();
-  int64_t carry = 0;
-  for (int r0 = 0; r0 < P.n_seqs && carry <= cut[1]; r0 += THREADS) {
+  const bool one_pass = P.n_seqs <= THREADS;   // a sequence a thread
+  SeqInfo mine;
+  int per_head = 0, total = 0, items = 0;
+  if (threadIdx.x < 2) w.slot[threadIdx.x].at = INT32_MAX;   // past the last: the total
+  if (!one_pass) {
+    int u = 0, n = 0;
+    for (int r = threadIdx.x; r < P.n_seqs; r += THREADS) {
+      mine = seq_info(P, r);
+      u += head_units<Traits>(P, mine);
+      n += Traits::row_tiles(mine, P);
+    }
+    u = __reduce_add_sync(0xffffffffu, u);
+    n = __reduce_add_sync(0xffffffffu, n);
+    if (lane == 0) {
+      w.sums[0][warp] = u;
+      w.sums[1][warp] = n;
+    }
+    __syncthreads();
+    for (int i = 0; i < kW; ++i) {
+      total += w.sums[0][i] * P.kv_heads;
+      items += w.sums[1][i] * P.kv_heads;
+    }
+    __syncthreads();
+  }
+  int carry = 0;
+  for (int r0 = 0; r0 < P.n_seqs; r0 += THREADS) {
     const int r = r0 + (int)threadIdx.x;
-    const int64_t u = r < P.n_seqs ? seq_units<Traits>(P, seq_info(P, r)) : 0;
-    int64_t incl = u;
+    per_head = 0;
+    int n = 0;
+    if (r < P.n_seqs) {
+      mine = seq_info(P, r);
+      per_head = head_units<Traits>(P, mine);
+      n = Traits::row_tiles(mine, P);
+    }
+    const int u = per_head * P.kv_heads;
+    int incl = u;
 #pragma unroll
     for (int d = 1; d < 32; d <<= 1) {
-      const int64_t o = __shfl_up_sync(0xffffffffu, incl, d);
+      const int o = __shfl_up_sync(0xffffffffu, incl, d);
       if (lane >= d) incl += o;
     }
-    if (lane == 31) red[warp] = incl;
+    n = __reduce_add_sync(0xffffffffu, n);
+    if (lane == 31) {
+      w.sums[0][warp] = incl;
+      w.sums[1][warp] = n;
+    }
     __syncthreads();
-    int64_t before = carry;
+    int base = carry + incl - u;
     for (int i = 0; i < kW; ++i) {
-      if (i < warp) before += red[i];
-      carry += red[i];
+      if (i < warp) base += w.sums[0][i];
+      carry += w.sums[0][i];
+      if (one_pass) items += w.sums[1][i] * P.kv_heads;
     }
-    const int64_t base = before + incl - u;
+    if (one_pass) total = carry;
+    const Shares sh(total, items, (int)gridDim.x, Traits::kLeast);
 #pragma unroll
-    for (int e = 0; e < 2; ++e)
-      if (cut[e] >= base && cut[e] < base + u) slots[e] = WorkSlot{base, r};
+    for (int e = 0; e < 2; ++e) {
+      const int off = sh.cut(min(cta + e, sh.ctas)) - base;
+      if (off < 0 || off >= u) continue;
+      const Item it = item_at<Traits>(P, mine, off, per_head);
+      const int at = off - it.first <= Traits::kSnap            ? it.first
+                     : it.first + it.nt - off <= Traits::kSnap ? it.first + it.nt
+                                                               : off;
+      w.slot[e] = WorkSlot{base + at, base, r, per_head, mine};
+    }
     __syncthreads();
+    if (carry > sh.cut(min(cta + 1, sh.ctas))) break;   // both boundaries are behind
   }
-  int64_t at[2];
-#pragma unroll
-  for (int e = 0; e < 2; ++e) {
-    at[e] = cut[e];
-    const WorkSlot sl = slots[e];
-    if (sl.r < P.n_seqs) {
-      const SeqInfo s = seq_info(P, sl.r);
-      const int64_t off = cut[e] - sl.base;
-      const Item it = item_at<Traits>(P, s, off, seq_units<Traits>(P, s) / P.kv_heads);
-      if (off - it.first <= w.snap) at[e] = sl.base + it.first;
-      else if (it.first + it.nt - off <= w.snap) at[e] = sl.base + it.first + it.nt;
-    }
-  }
-  w.begin = at[0];
-  w.end = at[1];
-  w.r = slots[0].r;
-  w.base = slots[0].base;
-  return w;
+  return Shares(total, items, (int)gridDim.x, Traits::kLeast);
 }
 
 // A stretch of one item's units in a CTA.
@@ -200,43 +227,41 @@ struct Segment {
 template <class Traits>
 struct Walker {
   const AttnParams& P;
-  WorkRange w;
-  int64_t pos, base, units;
-  int r;
+  const Shares sh;
+  int cta, pos, end, base, per_head, r;
   SeqInfo s;
-  __device__ __forceinline__ Walker(const AttnParams& p, const WorkRange& range)
-      : P(p), w(range), pos(range.begin), base(range.base), r(range.r) {
-    units = 0;
-    if (pos < w.end) {
-      s = seq_info(P, r);
-      units = seq_units<Traits>(P, s);
-    }
+  __device__ __forceinline__ Walker(const AttnParams& p, const Shares& shares, const WorkShared& w, int c)
+      : P(p), sh(shares), cta(c) {
+    pos = min(w.slot[0].at, sh.total);
+    end = min(w.slot[1].at, sh.total);
+    base = w.slot[0].base;
+    r = w.slot[0].r;
+    per_head = w.slot[0].per_head;
+    s = w.slot[0].s;
   }
-  __device__ __forceinline__ bool next(Segment& g, int cta) {
-    if (pos >= w.end) return false;
-    while (pos >= base + units) {   // `end` lies inside some sequence, so r stays in range
-      base += units;
+  __device__ __forceinline__ bool next(Segment& g) {
+    if (pos >= end) return false;
+    while (pos >= base + per_head * P.kv_heads) {   // `end` lies inside some sequence, so r stays in range
+      base += per_head * P.kv_heads;
       if (++r >= P.n_seqs) return false;
       s = seq_info(P, r);
-      units = seq_units<Traits>(P, s);
+      per_head = head_units<Traits>(P, s);
     }
     g.s = s;
     g.r = r;
-    g.it = item_at<Traits>(P, s, pos - base, units / P.kv_heads);
-    const int64_t first = base + g.it.first, last = first + g.it.nt;
-    g.ta = (int)(pos - first);
-    g.tb = (int)(min(last, w.end) - first);
+    g.it = item_at<Traits>(P, s, pos - base, per_head);
+    const int first = base + g.it.first, last = first + g.it.nt;
+    g.ta = pos - first;
+    g.tb = min(last, end) - first;
     pos = first + g.tb;
-    // the boundaries floor(c total / ctas) inside the item that were not moved to its ends
-    const int64_t lo = first + w.snap + 1, hi = last - w.snap;
-    const int64_t c_lo = (lo * w.ctas + w.total - 1) / w.total, c_hi = (hi * w.ctas + w.total - 1) / w.total - 1;
-    if (g.ta == 0 && g.tb == g.it.nt) {
-      g.parts = 1;
-      g.part = 0;
-      g.first_cta = cta;
-    } else {
-      g.first_cta = (int)c_lo - 1;
-      g.parts = (int)(c_hi - c_lo) + 2;
+    g.parts = 1;
+    g.part = 0;
+    g.first_cta = cta;
+    if (g.tb - g.ta != g.it.nt) {
+      // the boundaries inside the item that were not moved to its ends
+      const int c_lo = sh.first_cut(first + Traits::kSnap + 1), c_hi = sh.first_cut(last - Traits::kSnap) - 1;
+      g.first_cta = c_lo - 1;
+      g.parts = c_hi - c_lo + 2;
       g.part = cta - g.first_cta;
     }
     return true;

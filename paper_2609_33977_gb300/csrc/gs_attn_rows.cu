@@ -2,11 +2,11 @@
 // steps and short chunks.
 //
 // Bound by HBM: a sequence's keys and values are read once, for all its rows.  A unit
-// is 64 keys of a key head.  One warp fetches (TMA, one box per page and operand, a
-// ring of 5-6 units = 160-192 KB in flight per SM), the others compute with m16n8k16:
-// WR row tiles of 16 x WK shares of the unit's keys, each warp with its own running
-// maximum, sum and output, joined over the WK warps once per item.  An MMA row holds
-// a query; unused rows cost nothing that matters (the tensor pipe is 5-20 % busy).
+// is 128 keys of a key head.  One warp fetches (TMA, a box per page and operand, 192 KB
+// of units in flight per SM; a segment's queries come with its first unit), eight
+// compute with m16n8k16: WR row tiles of 16 x WK shares of the unit's keys, each warp
+// with its own running maximum, sum and output, joined over the WK warps once per
+// segment, in the segment's last stage.  Unused MMA rows cost nothing that matters.
 #include "gs_attn.cuh"
 
 #include <mutex>
@@ -15,10 +15,11 @@ namespace gs {
 namespace {
 using namespace sm100;
 
-constexpr int kTile = 64;
+constexpr int kTile = 128;
 constexpr uint64_t kArWaitLimitNs = 2000000000ull;
 
 struct FewTraits {
+  static constexpr int kLeast = 2, kSnap = 1;
   static __device__ __forceinline__ int row_tiles(const SeqInfo& s, const AttnParams& P) {
     return s.rows >= P.min_rows && s.rows <= P.max_rows ? 1 : 0;
   }
@@ -58,32 +59,68 @@ __device__ __forceinline__ uint32_t nonfinite2(uint32_t v) {
   return ((e & 0xFFFFu) == 0x7F80u ? 1u : 0u) | ((e >> 16) == 0x7F80u ? 0x10000u : 0u);
 }
 
-template <int D, int WR, int WK>
+// untiled copy of a row into shared memory (16-byte aligned, a multiple of 16 bytes)
+__device__ __forceinline__ void bulk_load(void* dst, const void* src, uint32_t bytes, uint64_t* bar) {
+  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(smem_u32(dst)),
+               "l"(src), "r"(bytes), "r"(smem_u32(bar))
+               : "memory");
+}
+
+template <int D, int WR>
 struct RowsCfg {
-  static constexpr int kWarps = WR * WK;             // consumers
+  static constexpr int kWarps = 8;                   // consumers
+  static constexpr int kWK = kWarps / WR;
   static constexpr int kThreads = (kWarps + 1) * 32; // + the fetching warp
   static constexpr int kRows = 16 * WR;
   static constexpr int kOpBytes = kTile * D * 2;
-  static constexpr int kStageBytes = 2 * kOpBytes;
-  static constexpr int kJoinBytes = WK * kRows * (D + 2) * 4;
-  static constexpr int kStages = (224 * 1024 - kJoinBytes) / kStageBytes;
-  static constexpr int kSmem = kStages * kStageBytes + kJoinBytes + 1024;
-  static_assert(kStages >= 4 && kSmem <= 227 * 1024 - 1024, "shared memory budget");
+  static constexpr int kStageBytes = 2 * kOpBytes;   // also what a join needs: kWarps x 16 x D floats
+  static constexpr int kQRow = D * 2 + 16;           // bytes of a row of queries: rows start in different banks
+  static constexpr int kQBytes = kRows * kQRow;
+  static constexpr int kQSlots = WR == 4 ? 1 : 2;    // segments whose queries are here ahead
+  static constexpr int kStages = 192 * 1024 / kStageBytes;
+  static constexpr int kSmem = kStages * kStageBytes + kQSlots * kQBytes + 1024;
+  static_assert(kWarps * 16 * D * 4 <= kStageBytes, "join");
+  static_assert(kSmem <= 227 * 1024 - 4096, "shared memory budget");
 };
 
-template <int D, int WR, int WK>
-__global__ void __launch_bounds__(RowsCfg<D, WR, WK>::kThreads, 1) k_attn_rows(const __grid_constant__ AttnParams P) {
-  using C = RowsCfg<D, WR, WK>;
-  constexpr int kSlabs = D / 64;
+// a row's D / 32 channels per lane
+template <int D>
+struct Lane;
+template <>
+struct Lane<128> {
+  using V = float4;
+  static __device__ __forceinline__ void unpack(const V& v, float (&a)[4]) { a[0] = v.x, a[1] = v.y, a[2] = v.z, a[3] = v.w; }
+  static __device__ __forceinline__ V pack(const float (&a)[4]) { return make_float4(a[0], a[1], a[2], a[3]); }
+  static __device__ __forceinline__ void store_bf16(uint16_t* dst, const float (&a)[4], float f) {
+    *reinterpret_cast<uint2*>(dst) = make_uint2(pack_bf16(a[0] * f, a[1] * f), pack_bf16(a[2] * f, a[3] * f));
+  }
+};
+template <>
+struct Lane<64> {
+  using V = float2;
+  static __device__ __forceinline__ void unpack(const V& v, float (&a)[2]) { a[0] = v.x, a[1] = v.y; }
+  static __device__ __forceinline__ V pack(const float (&a)[2]) { return make_float2(a[0], a[1]); }
+  static __device__ __forceinline__ void store_bf16(uint16_t* dst, const float (&a)[2], float f) {
+    *reinterpret_cast<uint32_t*>(dst) = pack_bf16(a[0] * f, a[1] * f);
+  }
+};
+
+template <int D, int WR>
+__global__ void __launch_bounds__(RowsCfg<D, WR>::kThreads, 1) k_attn_rows(const __grid_constant__ AttnParams P) {
+  using C = RowsCfg<D, WR>;
+  using L = Lane<D>;
+  constexpr int kSlabs = D / 64, kC = D / 32, WK = C::kWK;
   extern __shared__ uint8_t ar_smem_raw[];
   __shared__ __align__(8) uint64_t full_bar[C::kStages];
   __shared__ __align__(8) uint64_t empty_bar[C::kStages];
-  __shared__ int64_t red[34];
-  __shared__ WorkSlot slots[2];
+  __shared__ __align__(8) uint64_t qempty_bar[C::kQSlots];
+  __shared__ __align__(8) uint64_t join_bar;
+  __shared__ Segment segs[C::kStages];   // of the unit in a stage, where it is the segment's first; r < 0: the end
+  __shared__ WorkShared work;
+  __shared__ float2 join_ml[C::kWarps * 16];   // [WK][rows]: maximum and sum
   __shared__ int abort_s, last_s, bad_s[2];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(ar_smem_raw) + 1023) & ~uintptr_t(1023));
-  float* join = reinterpret_cast<float*>(smem + C::kStages * C::kStageBytes);   // [WK][rows][D], then [WK][rows][2]
-  float* join_ml = join + WK * C::kRows * D;
+  uint8_t* qsm = smem + C::kStages * C::kStageBytes;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int cta = (int)blockIdx.x;
   if (threadIdx.x == 0) {
@@ -91,30 +128,37 @@ __global__ void __launch_bounds__(RowsCfg<D, WR, WK>::kThreads, 1) k_attn_rows(c
       mbar_init(&full_bar[s], 1);
       mbar_init(&empty_bar[s], C::kWarps);
     }
+    for (int s = 0; s < C::kQSlots; ++s) mbar_init(&qempty_bar[s], C::kWarps);
+    mbar_init(&join_bar, C::kWarps);
     abort_s = 0;
     bad_s[0] = bad_s[1] = 0;
     fence_mbar_init();
   }
-  const WorkRange range = divide_work<FewTraits, C::kThreads>(P, cta, (int)gridDim.x, red, slots);
-  __syncthreads();
+  if (threadIdx.x == C::kWarps * 32) {
+    prefetch_tmap(&P.kmap);
+    prefetch_tmap(&P.vmap);
+  }
+  const Shares shares = divide_work<FewTraits, C::kThreads>(P, cta, work);
   volatile int* abort_flag = &abort_s;
-  const int chunk = min(1 << P.page_shift, kTile), chunk_shift = min(P.page_shift, 6);   // rows of a TMA box
+  const int chunk_shift = min(P.page_shift, 7), chunk = 1 << chunk_shift;   // rows of a TMA box
+  const auto wait_warp = [&](uint64_t* bar, uint32_t parity) {
+    return __all_sync(0xffffffffu, mbar_wait_bounded(bar, parity, abort_flag, P.err, kArWaitLimitNs, kDevErrTimeout)) != 0;
+  };
 
   if (warp == C::kWarps) {
     // ------------------------------------------------------------ fetch
-    Walker<FewTraits> walk(P, range);
+    Walker<FewTraits> walk(P, shares, work, cta);
     Segment g;
     const int32_t no_row = (int32_t)((P.pages * P.kv_heads) << P.page_shift);   // past the last: reads as zeros
-    uint32_t st = 0, ph = 1u;
+    uint32_t st = 0, ph = 1u, qs = 0, qph = 1u;
     bool ok = true;
-    const int per_tile = kTile >> chunk_shift;   // boxes of a whole unit and operand (1, 2 or 4)
-    while (ok && walk.next(g, cta)) {
+    while (ok && walk.next(g)) {
       const int len = g.s.len();
       const int64_t trow = (int64_t)g.r * P.width;
       int held = -1, page = -1;   // lane i holds table entry 32 held + i
       for (int t = g.ta; t < g.tb; ++t) {
         const int valid = min(kTile, max(0, len - t * kTile));
-        const int boxes = (valid + chunk - 1) >> chunk_shift;
+        const int boxes = (valid + chunk - 1) >> chunk_shift;   // at most 8
         // all boxes of a unit have their table entries within one block of 32
         const int e0 = (t * kTile) >> P.page_shift;
         if (e0 >> 5 != held) {
@@ -122,22 +166,36 @@ __global__ void __launch_bounds__(RowsCfg<D, WR, WK>::kThreads, 1) k_attn_rows(c
           const int e = 32 * held + lane;
           page = e < P.width && ((int64_t)e << P.page_shift) < len ? __ldg(P.table + trow + e) : -1;
         }
-        if (!__all_sync(0xffffffffu, mbar_wait_bounded(&empty_bar[st], ph, abort_flag, P.err, kArWaitLimitNs, kDevErrTimeout))) {
+        const bool first = t == g.ta;
+        if (!wait_warp(&empty_bar[st], ph) || (first && !wait_warp(&qempty_bar[qs], qph))) {
           ok = false;
           break;
         }
         uint8_t* stage = smem + st * C::kStageBytes;
-        if (lane == 0) mbar_arrive_expect_tx(&full_bar[st], 2u * (uint32_t)(boxes * chunk * D * 2));
+        if (lane == 0) {
+          if (first) segs[st] = g;
+          mbar_arrive_expect_tx(&full_bar[st], 2u * (uint32_t)(boxes * chunk * D * 2) + (first ? (uint32_t)(g.s.rows * D * 2) : 0u));
+        }
         __syncwarp();
+        // lane b fetches box b of the keys, lane 16 + b of the values
         const int b = lane & 15, key = t * kTile + (b << chunk_shift);
         const int pg = __shfl_sync(0xffffffffu, page, (key >> P.page_shift) & 31);
         if (b < boxes) {
           const int32_t row = pg >= 0 && pg < P.pages
                                   ? (int32_t)((((int64_t)pg * P.kv_heads + g.it.h) << P.page_shift) + (key & ((1 << P.page_shift) - 1)))
                                   : no_row;
-          uint8_t* dst = stage + b * (chunk * D * 2);
-          if (lane < 16) tma_load_3d(dst, &P.kmap, &full_bar[st], 0, row, 0);
-          else tma_load_3d(dst + C::kOpBytes, &P.vmap, &full_bar[st], 0, row, 0);
+          tma_load_3d(stage + b * (chunk * D * 2) + (lane >> 4) * C::kOpBytes, lane < 16 ? &P.kmap : &P.vmap, &full_bar[st], 0, row, 0);
+        }
+        if (first) {
+          for (int row = lane; row < g.s.rows; row += 32) {
+            const int tok = row / P.group, hd = row - tok * P.group;
+            bulk_load(qsm + qs * C::kQBytes + row * C::kQRow,
+                      P.q + (int64_t)(g.s.tok0 + tok) * P.q_stride + (int64_t)(g.it.h * P.group + hd) * D, D * 2, &full_bar[st]);
+          }
+          if (++qs == C::kQSlots) {
+            qs = 0;
+            qph ^= 1u;
+          }
         }
         __syncwarp();
         if (++st == C::kStages) {
@@ -146,46 +204,81 @@ __global__ void __launch_bounds__(RowsCfg<D, WR, WK>::kThreads, 1) k_attn_rows(c
         }
       }
     }
-    (void)per_tile;
+    if (ok && wait_warp(&empty_bar[st], ph) && lane == 0) {   // the end
+      segs[st].r = -1;
+      mbar_arrive(&full_bar[st]);
+    }
+    // ---- rows that nothing computes: tokens of no sequence, and sequences of more rows than were announced
+    const int64_t row16 = (int64_t)P.q_heads * D / 8;   // 16-byte pieces of a token's output
+    const auto zero = [&](int64_t t0, int64_t t1) {
+      for (int64_t i = t0 * row16 + lane; i < t1 * row16; i += 32) reinterpret_cast<uint4*>(P.out)[i] = make_uint4(0u, 0u, 0u, 0u);
+    };
+    const int64_t before = min((int64_t)max(0, __ldg(P.offsets)), P.tokens), after = max(0, __ldg(P.offsets + P.n_seqs));
+    for (int64_t t = cta; t < before; t += gridDim.x) zero(t, t + 1);
+    for (int64_t t = after + cta; t < P.tokens; t += gridDim.x) zero(t, t + 1);
+    if (P.zero_rest)
+      for (int r = cta; r < P.n_seqs; r += (int)gridDim.x) {
+        const SeqInfo s = seq_info(P, r);
+        if (s.rows > P.max_rows) zero(s.tok0, (int64_t)s.tok0 + s.n);
+      }
   } else {
     // ------------------------------------------------------------ compute
     const int wr = warp / WK, wk = warp % WK, gq = lane >> 2, qd = lane & 3;
-    constexpr int kKeys = kTile / WK;         // this warp's keys of a unit
-    constexpr int kNt = kKeys / 8;
-    const auto bar_compute = [&]() { asm volatile("bar.sync 1, %0;" ::"n"(C::kWarps * 32) : "memory"); };
-    Walker<FewTraits> walk(P, range);
-    Segment g;
-    uint32_t st = 0, ph = 0u, turn = 0;
-    bool ok = true;
-    // a lane's ldmatrix row: keys (K) or keys of the transposed blocks (V), and its 16-byte column
-    const int kb = wk * kKeys;
-    const auto tile_addr = [&](uint32_t op, int key, int col16) -> uint32_t {   // col16: 16-byte column of the row
-      const int box = key >> chunk_shift, r = key & (chunk - 1), slab = col16 >> 3;
-      return op + (uint32_t)(((box * kSlabs + slab) << chunk_shift) + r) * 128u + (uint32_t)(((col16 & 7) ^ (r & 7)) << 4);
+    constexpr int kKeys = kTile / WK;              // this warp's keys of a unit: 16, 32 or 64
+    constexpr int kSub = kKeys < 32 ? kKeys : 32;  // keys between two steps of the running maximum
+    constexpr int kNt = kSub / 8;
+    uint32_t jph = 0;
+    // the compute warps' barrier, bounded like every wait: false when some role gave up
+    const auto meet = [&]() {
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&join_bar);
+      const bool met = wait_warp(&join_bar, jph);
+      jph ^= 1u;
+      return met;
     };
-    while (ok && walk.next(g, cta)) {
+    uint32_t st = 0, ph = 0u, turn = 0, qs = 0;
+    bool ok = true;
+    const int kb = wk * kKeys;
+    // Byte offset of a key's row in an operand, and its swizzle: 16-byte column c of slab s is at
+    // ((offset + s slab) ^ (c << 4)) for a row whose swizzle is folded into the offset.
+    const uint32_t slab = (uint32_t)chunk * 128u;
+    const auto row_off = [&](int key) -> uint32_t {
+      const int r = key & (chunk - 1);
+      return (uint32_t)((key >> chunk_shift) * kSlabs) * slab + (uint32_t)r * 128u + (uint32_t)((r & 7) << 4);
+    };
+    // keys: matrices (keys 0-7, 8-15) x (columns, columns + 8); values: (keys 0-15) x (columns, columns + 8), transposed
+    uint32_t koff[kKeys / 16], voff[kKeys / 16];
+#pragma unroll
+    for (int i = 0; i < kKeys / 16; ++i) {
+      koff[i] = row_off(kb + 16 * i + (lane & 7) + ((lane >> 4) << 3)) ^ (((lane >> 3) & 1) << 4);
+      voff[i] = row_off(kb + 16 * i + (lane & 15)) ^ ((lane >> 4) << 4);
+    }
+    while (true) {
+      if (!wait_warp(&full_bar[st], ph)) break;
+      const Segment g = segs[st];
+      if (g.r < 0) break;
       const int len = g.s.len();
-      // rows of this lane: 16 wr + gq and + 8
+      // rows of this lane: 16 wr + gq and + 8.  Rows past the last hold whatever the buffer held: nobody reads theirs.
       const int row0 = 16 * wr + gq;
       uint32_t qf[D / 16][4];
       int seen[2];
+      const uint32_t flip = P.negate ? 0x80008000u : 0u;
 #pragma unroll
       for (int hf = 0; hf < 2; ++hf) {
         const int row = row0 + 8 * hf;
-        const bool on = row < g.s.rows;
-        const int tok = on ? row / P.group : 0, hd = on ? row - tok * P.group : 0;
-        seen[hf] = on ? g.s.seen(tok) : 0;
-        const uint32_t* src = reinterpret_cast<const uint32_t*>(P.q + (int64_t)(g.s.tok0 + tok) * P.q_stride +
-                                                                (int64_t)(g.it.h * P.group + hd) * D) + qd;
-        const uint32_t flip = P.negate ? 0x80008000u : 0u;
+        seen[hf] = row < g.s.rows ? g.s.seen(row / P.group) : 0;
+        const uint32_t* src = reinterpret_cast<const uint32_t*>(qsm + qs * C::kQBytes + row * C::kQRow) + qd;
 #pragma unroll
         for (int ks = 0; ks < D / 16; ++ks) {
-          qf[ks][hf] = on ? __ldg(src + 8 * ks) ^ flip : 0u;
-          qf[ks][hf + 2] = on ? __ldg(src + 8 * ks + 4) ^ flip : 0u;
+          qf[ks][hf] = src[8 * ks] ^ flip;
+          qf[ks][hf + 2] = src[8 * ks + 4] ^ flip;
         }
       }
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&qempty_bar[qs]);
+      if (++qs == C::kQSlots) qs = 0;
       const int all_see = g.s.seen(0);                 // keys below this are visible to every row
-      const bool work = 16 * wr < g.s.rows;            // a warp without rows only keeps step
+      const bool on = 16 * wr < g.s.rows;              // a warp without rows only keeps step
       float o[D / 8][4];
       float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
 #pragma unroll
@@ -194,26 +287,36 @@ __global__ void __launch_bounds__(RowsCfg<D, WR, WK>::kThreads, 1) k_attn_rows(c
         for (int e = 0; e < 4; ++e) o[j][e] = 0.f;
       uint32_t bad = 0;
       for (int t = g.ta; t < g.tb; ++t) {
-        if (!__all_sync(0xffffffffu, mbar_wait_bounded(&full_bar[st], ph, abort_flag, P.err, kArWaitLimitNs, kDevErrTimeout))) {
-          ok = false;
-          break;
+        if (t > g.ta) {
+          // the stage before goes back; the segment's last one is kept for the join
+          __syncwarp();
+          if (lane == 0) mbar_arrive(&empty_bar[st]);
+          if (++st == C::kStages) {
+            st = 0;
+            ph ^= 1u;
+          }
+          if (!wait_warp(&full_bar[st], ph)) {
+            ok = false;
+            break;
+          }
         }
-        if (work) {
-          const uint32_t kop = smem_u32(smem + st * C::kStageBytes), vop = kop + C::kOpBytes;
-          const int key0 = t * kTile + kb;             // the warp's first key
-          const bool masked = key0 + kKeys > all_see;
+        const uint32_t kop = smem_u32(smem + st * C::kStageBytes), vop = kop + C::kOpBytes;
+#pragma unroll
+        for (int sub = 0; sub < kKeys / kSub; ++sub) {
+          const int key0 = t * kTile + kb + sub * kSub;   // its first key
+          if (!on || key0 >= len) break;                  // uniform over the warp
+          const bool masked = key0 + kSub > all_see;
           float s[kNt][4];
 #pragma unroll
           for (int j = 0; j < kNt; ++j)
 #pragma unroll
             for (int e = 0; e < 4; ++e) s[j][e] = 0.f;
-          // two key tiles (16 keys) and one 16-deep step per ldmatrix: matrices (keys 0-7, 8-15) x (columns, columns + 8)
 #pragma unroll
           for (int ks = 0; ks < D / 16; ++ks)
 #pragma unroll
             for (int j = 0; j < kNt; j += 2) {
               uint32_t kf[4];
-              ldsm4(kf, tile_addr(kop, kb + 8 * j + (lane & 7) + ((lane >> 4) << 3), 2 * ks + ((lane >> 3) & 1)));
+              ldsm4(kf, (kop + koff[sub * (kSub / 16) + j / 2] + (ks >> 2) * slab) ^ (uint32_t)((ks & 3) << 5));
               mma16816(s[j], qf[ks], kf[0], kf[1]);
               mma16816(s[j + 1], qf[ks], kf[2], kf[3]);
             }
@@ -227,14 +330,14 @@ __global__ void __launch_bounds__(RowsCfg<D, WR, WK>::kThreads, 1) k_attn_rows(c
               s[j][e] = v;
               top[e >> 1] = fmaxf(top[e >> 1], v);
             }
-          float f[2];
+          float f[2], base[2];
 #pragma unroll
           for (int hf = 0; hf < 2; ++hf) {
             const float mn = fmaxf(m[hf], quad_max(top[hf]));
             f[hf] = mn == m[hf] ? 1.f : ex2(m[hf] - mn);   // m = -inf: 0
             m[hf] = mn;
+            base[hf] = mn == -INFINITY ? 0.f : mn;
           }
-          const float base[2] = {m[0] == -INFINITY ? 0.f : m[0], m[1] == -INFINITY ? 0.f : m[1]};
           float sum[2] = {0.f, 0.f};
 #pragma unroll
           for (int j = 0; j < kNt; ++j)
@@ -252,160 +355,161 @@ __global__ void __launch_bounds__(RowsCfg<D, WR, WK>::kThreads, 1) k_attn_rows(c
               for (int e = 0; e < 4; ++e) o[j][e] *= f[e >> 1];
           }
 #pragma unroll
-          for (int kk = 0; kk < kKeys / 16; ++kk) {
+          for (int kk = 0; kk < kSub / 16; ++kk) {
             const uint32_t pf[4] = {pack_bf16(s[2 * kk][0], s[2 * kk][1]), pack_bf16(s[2 * kk][2], s[2 * kk][3]),
                                     pack_bf16(s[2 * kk + 1][0], s[2 * kk + 1][1]), pack_bf16(s[2 * kk + 1][2], s[2 * kk + 1][3])};
-            // which keys of this lane's fragments exist: 2 qd, 2 qd + 1, and the same + 8
-            uint32_t keep[2] = {0xFFFFFFFFu, 0xFFFFFFFFu};
-            if (masked) {
+            const uint32_t va = vop + voff[sub * (kSub / 16) + kk];
+            if (!masked) {
+#pragma unroll
+              for (int j = 0; j < D / 8; j += 2) {
+                uint32_t vf[4];   // (keys 0-7, keys 8-15) of columns 8 j, then of 8 j + 8
+                ldsm4t(vf, (va + (j >> 3) * slab) ^ (uint32_t)((j & 7) << 4));
+                mma16816(o[j], pf, vf[0], vf[1]);
+                mma16816(o[j + 1], pf, vf[2], vf[3]);
+              }
+            } else {
+              // Keys past the end become zeros.  A weight of zero does not silence an infinity or a NaN: those of
+              // keys that only some rows see are left out, and added at the join where they are seen.
+              uint32_t keep[2];
+              int part[2];   // bit 0 / 1: key 2 qd / 2 qd + 1 (+ 8) is one that not every row sees
 #pragma unroll
               for (int b = 0; b < 2; ++b) {
                 const int key = key0 + 16 * kk + 8 * b + 2 * qd;
                 keep[b] = (key < len ? 0xFFFFu : 0u) | (key + 1 < len ? 0xFFFF0000u : 0u);
+                part[b] = (key >= all_see ? 1 : 0) | (key + 1 >= all_see ? 2 : 0);
               }
-            }
 #pragma unroll
-            for (int j = 0; j < D / 8; j += 2) {
-              uint32_t vf[4];   // (keys 0-7, keys 8-15) of columns 8 j, then of 8 j + 8
-              ldsm4t(vf, tile_addr(vop, kb + 16 * kk + (lane & 15), j + (lane >> 4)));
-              if (masked) {
+              for (int j = 0; j < D / 8; j += 2) {
+                uint32_t vf[4];
+                ldsm4t(vf, (va + (j >> 3) * slab) ^ (uint32_t)((j & 7) << 4));
 #pragma unroll
                 for (int b = 0; b < 4; ++b) {
                   vf[b] &= keep[b & 1];
-                  const uint32_t nf = nonfinite2(vf[b]);   // a weight of zero does not silence it: the join adds it where seen
-                  const int key = key0 + 16 * kk + 8 * (b & 1) + 2 * qd;
+                  const uint32_t nf = nonfinite2(vf[b]);
                   uint32_t drop = 0;
-                  if ((nf & 1u) && key >= all_see) drop |= 0xFFFFu;
-                  if ((nf >> 16) && key + 1 >= all_see) drop |= 0xFFFF0000u;
+                  if ((nf & 1u) && (part[b & 1] & 1)) drop |= 0xFFFFu;
+                  if ((nf >> 16) && (part[b & 1] & 2)) drop |= 0xFFFF0000u;
                   bad |= drop;
                   vf[b] &= ~drop;
                 }
+                mma16816(o[j], pf, vf[0], vf[1]);
+                mma16816(o[j + 1], pf, vf[2], vf[3]);
               }
-              mma16816(o[j], pf, vf[0], vf[1]);
-              mma16816(o[j + 1], pf, vf[2], vf[3]);
             }
           }
         }
-        __syncwarp();
-        if (lane == 0) mbar_arrive(&empty_bar[st]);
-        if (++st == C::kStages) {
-          st = 0;
-          ph ^= 1u;
-        }
       }
       if (!ok) break;
-      // ---- join the WK warps of every row tile
+      // ---- join the WK warps of every row tile, in the stage that every warp has read
       ++turn;
-      if (work) {
+      if (!meet()) break;
+      float* join = reinterpret_cast<float*>(smem + st * C::kStageBytes);   // [WK][rows][D]
+      if (on) {
 #pragma unroll
         for (int hf = 0; hf < 2; ++hf) {
           const int row = row0 + 8 * hf;
-          float* dst = join + ((size_t)wk * C::kRows + row) * D + 2 * qd;
-#pragma unroll
-          for (int j = 0; j < D / 8; ++j) *reinterpret_cast<float2*>(dst + 8 * j) = make_float2(o[j][2 * hf], o[j][2 * hf + 1]);
           const float sum = quad_sum(l[hf]);
-          if (qd == 0) *reinterpret_cast<float2*>(join_ml + ((size_t)wk * C::kRows + row) * 2) = make_float2(m[hf], sum);
+          if (row < g.s.rows) {
+            float* dst = join + (wk * C::kRows + row) * D + 2 * qd;
+#pragma unroll
+            for (int j = 0; j < D / 8; ++j) *reinterpret_cast<float2*>(dst + 8 * j) = make_float2(o[j][2 * hf], o[j][2 * hf + 1]);
+            if (qd == 0) join_ml[wk * C::kRows + row] = make_float2(m[hf], sum);
+          }
         }
         if (bad) bad_s[turn & 1] = 1;
       }
-      bar_compute();
+      if (!meet()) break;
       const bool fix = bad_s[turn & 1] != 0;
       if (threadIdx.x == 0) bad_s[(turn + 1) & 1] = 0;
       float* slot = g.parts > 1 ? part_slot(P, g.first_cta, g.part, C::kRows, D) : nullptr;
-      const int key_end = min(len, g.tb * kTile), key_begin = max(all_see, g.ta * kTile);
-      for (int i = threadIdx.x; i < g.s.rows * (D / 4); i += C::kWarps * 32) {
-        const int row = i / (D / 4), d = 4 * (i % (D / 4));
-        float mm = -INFINITY, ll = 0.f;
+      for (int row = warp; row < g.s.rows; row += C::kWarps) {   // a warp a row
+        const float2 ml = lane < WK ? join_ml[lane * C::kRows + row] : make_float2(-INFINITY, 0.f);
+        float mm = ml.x;
 #pragma unroll
-        for (int w = 0; w < WK; ++w) mm = fmaxf(mm, join_ml[(w * C::kRows + row) * 2]);
-        const float b = mm == -INFINITY ? 0.f : mm;
-        float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
+        for (int d = WK / 2; d > 0; d >>= 1) mm = fmaxf(mm, __shfl_xor_sync(0xffffffffu, mm, d));
+        mm = __shfl_sync(0xffffffffu, mm, 0);
+        const float fw = ex2(ml.x - (mm == -INFINITY ? 0.f : mm));
+        float ll = ml.y * fw;
+#pragma unroll
+        for (int d = WK / 2; d > 0; d >>= 1) ll += __shfl_xor_sync(0xffffffffu, ll, d);
+        ll = __shfl_sync(0xffffffffu, ll, 0);
+        float a[kC];
+#pragma unroll
+        for (int c = 0; c < kC; ++c) a[c] = 0.f;
 #pragma unroll
         for (int w = 0; w < WK; ++w) {
-          const float2 ml = *reinterpret_cast<const float2*>(join_ml + (w * C::kRows + row) * 2);
-          const float fw = ex2(ml.x - b);
-          const float4 v = *reinterpret_cast<const float4*>(join + ((size_t)w * C::kRows + row) * D + d);
-          ll = fmaf(ml.y, fw, ll);
-          a.x = fmaf(v.x, fw, a.x);
-          a.y = fmaf(v.y, fw, a.y);
-          a.z = fmaf(v.z, fw, a.z);
-          a.w = fmaf(v.w, fw, a.w);
+          const float f = __shfl_sync(0xffffffffu, fw, w);
+          float v[kC];
+          L::unpack(reinterpret_cast<const typename L::V*>(join + (w * C::kRows + row) * D)[lane], v);
+#pragma unroll
+          for (int c = 0; c < kC; ++c) a[c] = fmaf(v[c], f, a[c]);
         }
         const int tok = row / P.group, hd = row - tok * P.group, vis = g.s.seen(tok);
         if (fix) {   // infinities and NaN of keys that only some rows see
-          for (int key = key_begin; key < min(key_end, vis); ++key) {
+          const int end = min(min(len, g.tb * kTile), vis);
+          for (int key = max(all_see, g.ta * kTile); key < end; ++key) {
             const int pg = __ldg(P.table + (int64_t)g.r * P.width + (key >> P.page_shift));
             if (pg < 0 || pg >= P.pages) continue;
-            const uint16_t* vr = P.v + ((((int64_t)pg * P.kv_heads + g.it.h) << P.page_shift) + (key & ((1 << P.page_shift) - 1))) * D + d;
-            const float v0 = bf16_lo(vr[0]), v1 = bf16_lo(vr[1]), v2 = bf16_lo(vr[2]), v3 = bf16_lo(vr[3]);
-            if (!isfinite(v0)) a.x += v0;
-            if (!isfinite(v1)) a.y += v1;
-            if (!isfinite(v2)) a.z += v2;
-            if (!isfinite(v3)) a.w += v3;
+            const uint16_t* vr =
+                P.v + ((((int64_t)pg * P.kv_heads + g.it.h) << P.page_shift) + (key & ((1 << P.page_shift) - 1))) * D + kC * lane;
+#pragma unroll
+            for (int c = 0; c < kC; ++c) {
+              const float v = bf16_lo(vr[c]);
+              if (!isfinite(v)) a[c] += v;
+            }
           }
         }
         if (slot) {
-          *reinterpret_cast<float4*>(slot + (size_t)row * D + d) = a;
-          if (d == 0) *reinterpret_cast<float2*>(slot + (size_t)C::kRows * D + 2 * row) = make_float2(mm, ll);
+          reinterpret_cast<typename L::V*>(slot + (size_t)row * D)[lane] = L::pack(a);
+          if (lane == 0) *reinterpret_cast<float2*>(slot + (size_t)C::kRows * D + 2 * row) = make_float2(mm, ll);
         } else {
-          const float inv = vis > 0 ? 1.f / ll : 0.f;
-          *reinterpret_cast<uint2*>(P.out + ((int64_t)(g.s.tok0 + tok) * P.q_heads + g.it.h * P.group + hd) * D + d) =
-              make_uint2(pack_bf16(a.x * inv, a.y * inv), pack_bf16(a.z * inv, a.w * inv));
+          L::store_bf16(P.out + ((int64_t)(g.s.tok0 + tok) * P.q_heads + g.it.h * P.group + hd) * D + kC * lane, a,
+                        vis > 0 ? 1.f / ll : 0.f);
         }
+      }
+      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");   // the stage was written here; copies overwrite it
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&empty_bar[st]);
+      if (++st == C::kStages) {
+        st = 0;
+        ph ^= 1u;
       }
       if (slot) {
         // ---- the last of the item's CTAs joins its parts, in order
         __threadfence();
-        bar_compute();
+        if (!meet()) break;
         if (threadIdx.x == 0) {
           const int got = atomicAdd(P.cnt + g.first_cta, 1);
           last_s = got == g.parts - 1;
           if (last_s) P.cnt[g.first_cta] = 0;
           __threadfence();
         }
-        bar_compute();
+        if (!meet()) break;
         if (last_s) {
-          for (int i = threadIdx.x; i < g.s.rows * (D / 4); i += C::kWarps * 32) {
-            const int row = i / (D / 4), d = 4 * (i % (D / 4));
-            float mm = -INFINITY, ll = 0.f;
-            float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
+          for (int row = warp; row < g.s.rows; row += C::kWarps) {
+            float mm = -INFINITY, ll = 0.f, a[kC];
+#pragma unroll
+            for (int c = 0; c < kC; ++c) a[c] = 0.f;
 #pragma unroll 4
             for (int p = 0; p < g.parts; ++p) {
               const float* sp = part_slot(P, g.first_cta, p, C::kRows, D);
               const float2 ml = __ldcg(reinterpret_cast<const float2*>(sp + (size_t)C::kRows * D + 2 * row));
-              const float4 v = __ldcg(reinterpret_cast<const float4*>(sp + (size_t)row * D + d));
+              float v[kC];
+              L::unpack(__ldcg(reinterpret_cast<const typename L::V*>(sp + (size_t)row * D) + lane), v);
               const float mn = fmaxf(mm, ml.x), b = mn == -INFINITY ? 0.f : mn;
               const float f0 = ex2(mm - b), f1 = ex2(ml.x - b);
               ll = ll * f0 + ml.y * f1;
-              a.x = a.x * f0 + v.x * f1;
-              a.y = a.y * f0 + v.y * f1;
-              a.z = a.z * f0 + v.z * f1;
-              a.w = a.w * f0 + v.w * f1;
+#pragma unroll
+              for (int c = 0; c < kC; ++c) a[c] = a[c] * f0 + v[c] * f1;
               mm = mn;
             }
             const int tok = row / P.group, hd = row - tok * P.group;
-            const float inv = g.s.seen(tok) > 0 ? 1.f / ll : 0.f;
-            *reinterpret_cast<uint2*>(P.out + ((int64_t)(g.s.tok0 + tok) * P.q_heads + g.it.h * P.group + hd) * D + d) =
-                make_uint2(pack_bf16(a.x * inv, a.y * inv), pack_bf16(a.z * inv, a.w * inv));
+            L::store_bf16(P.out + ((int64_t)(g.s.tok0 + tok) * P.q_heads + g.it.h * P.group + hd) * D + kC * lane, a,
+                          g.s.seen(tok) > 0 ? 1.f / ll : 0.f);
           }
         }
       }
-      bar_compute();   // the join buffers may be written again
     }
-    // ---- rows that nothing computes: tokens of no sequence, and sequences of more rows than were announced
-    const int64_t row16 = (int64_t)P.q_heads * D / 8;   // 16-byte pieces of a token's output
-    const auto zero = [&](int64_t t0, int64_t t1) {
-      for (int64_t i = t0 * row16 + threadIdx.x; i < t1 * row16; i += C::kWarps * 32)
-        reinterpret_cast<uint4*>(P.out)[i] = make_uint4(0u, 0u, 0u, 0u);
-    };
-    const int64_t before = min((int64_t)max(0, __ldg(P.offsets)), P.tokens), after = max(0, __ldg(P.offsets + P.n_seqs));
-    for (int64_t t = cta; t < before; t += gridDim.x) zero(t, t + 1);
-    for (int64_t t = after + cta; t < P.tokens; t += gridDim.x) zero(t, t + 1);
-    if (P.zero_rest)
-      for (int r = cta; r < P.n_seqs; r += (int)gridDim.x) {
-        const SeqInfo s = seq_info(P, r);
-        if (s.rows > P.max_rows) zero(s.tok0, (int64_t)s.tok0 + s.n);
-      }
   }
   __syncthreads();
   if (abort_s) {
@@ -416,13 +520,12 @@ __global__ void __launch_bounds__(RowsCfg<D, WR, WK>::kThreads, 1) k_attn_rows(c
   }
 }
 
-template <int D, int WR, int WK>
+template <int D, int WR>
 gs_status rows_launch(const AttnParams& P, int ctas, cudaStream_t s) {
-  using C = RowsCfg<D, WR, WK>;
-  static const cudaError_t attr =
-      cudaFuncSetAttribute(k_attn_rows<D, WR, WK>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::kSmem);
+  using C = RowsCfg<D, WR>;
+  static const cudaError_t attr = cudaFuncSetAttribute(k_attn_rows<D, WR>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::kSmem);
   if (attr != cudaSuccess) return GS_ERR_CUDA;
-  k_attn_rows<D, WR, WK><<<(unsigned)ctas, C::kThreads, C::kSmem, s>>>(P);
+  k_attn_rows<D, WR><<<(unsigned)ctas, C::kThreads, C::kSmem, s>>>(P);
   note_launch();
   return cudaGetLastError() == cudaSuccess ? GS_OK : GS_ERR_CUDA;
 }
@@ -433,13 +536,12 @@ int attn_rows_most() { return 64; }
 
 int attn_rows_box(int page_size) { return page_size < kTile ? page_size : kTile; }
 
-// rows: an upper bound of the rows of the sequences that are this kernel's
+int attn_rows_tile() { return kTile; }
+
 gs_status launch_attn_rows(const AttnParams& P, int head_dim, int rows, int ctas, cudaStream_t s) {
   if (head_dim == 128)
-    return rows <= 16 ? rows_launch<128, 1, 4>(P, ctas, s) : rows <= 32 ? rows_launch<128, 2, 4>(P, ctas, s)
-                                                                        : rows_launch<128, 4, 2>(P, ctas, s);
-  return rows <= 16 ? rows_launch<64, 1, 4>(P, ctas, s) : rows <= 32 ? rows_launch<64, 2, 4>(P, ctas, s)
-                                                                     : rows_launch<64, 4, 2>(P, ctas, s);
+    return rows <= 16 ? rows_launch<128, 1>(P, ctas, s) : rows <= 32 ? rows_launch<128, 2>(P, ctas, s) : rows_launch<128, 4>(P, ctas, s);
+  return rows <= 16 ? rows_launch<64, 1>(P, ctas, s) : rows <= 32 ? rows_launch<64, 2>(P, ctas, s) : rows_launch<64, 4>(P, ctas, s);
 }
 
 }  // namespace gs
