@@ -511,8 +511,10 @@ gs_status gs_cache_append(const gs_paged_cache* cache, const gs_seq_batch* batch
  *         after another on one stream without being cleared.
  * max_new chooses the kernels; a sequence with more new tokens than it says is served
  * all the same, or (if max_new is below what needs the chunk kernel) gets zeros.
+ * After GS_ERR_DEVICE_TIMEOUT the workspace has to be zeroed again.
  * Errors: INVALID_ARG, UNSUPPORTED (page_size, head_dim, more than 64 query heads a key
- * head), CUDA.
+ * head, tokens * q_heads / kv_heads of 10^9 and more, or more than 2 * 10^9 tiles of
+ * 128 keys x 256 rows in the page tables), CUDA.
  */
 gs_status gs_paged_attention_workspace(const gs_paged_cache* cache, const gs_seq_batch* batch, int32_t q_heads, size_t* bytes);
 gs_status gs_paged_attention(const gs_paged_cache* cache, const gs_seq_batch* batch, const void* q_dev, int64_t q_stride,

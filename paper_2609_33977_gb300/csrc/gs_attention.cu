@@ -1,96 +1,48 @@
-// Causal attention of a step's new tokens over a paged cache.
-//
-// One warp per (token, query head): 32 keys at a time, one per lane for the scores
-// (a lane reads its key's whole row), then each lane owns head_dim / 32 channels of
-// the output.  Running maximum and sum in float32.
+// Attention over a paged cache: which kernel serves which sequence, workspace, launch.
 #include "gs_attn.cuh"
 
+#include <algorithm>
 #include <cmath>
 
 namespace gs {
 namespace {
 
-template <int D>
-__global__ void __launch_bounds__(128) k_attention_simple(const AttnParams P) {
-  __shared__ float qs[4][D];
-  const int64_t t = blockIdx.x;
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int head = (int)blockIdx.y * 4 + warp;
-  const int seq = block_count_le(P.offsets, P.n_seqs, (int)t);
-  if (head >= P.q_heads || seq >= P.n_seqs || seq_info(P, seq).rows < P.min_rows) return;
-  int64_t seen = 0;
-  if (seq < P.n_seqs) {
-    const int64_t first = P.offsets[seq], end = P.offsets[seq + 1];
-    if (t >= first) seen = (int64_t)P.kv_lens[seq] - (end - first) + (t - first) + 1;
-    seen = min(seen, (int64_t)P.width << P.page_shift);
-  }
-  constexpr int C = D / 32;
-  for (int i = lane; i < D; i += 32) qs[warp][i] = bf16_lo(P.q[t * P.q_stride + head * D + i]);
-  __syncwarp();
-  const int kvh = head / (P.q_heads / P.kv_heads);
-  float m = -INFINITY, l = 0.f, o[C];
-#pragma unroll
-  for (int c = 0; c < C; ++c) o[c] = 0.f;
-  const auto row = [&](int64_t j) -> int64_t {   // -1: no such page
-    const int64_t page = P.table[(int64_t)seq * P.width + (j >> P.page_shift)];
-    if (page < 0 || page >= P.pages) return -1;
-    return ((page * P.kv_heads + kvh) << P.page_shift) + (j & ((1 << P.page_shift) - 1));
-  };
-  for (int64_t j0 = 0; j0 < seen; j0 += 32) {
-    const int64_t j = j0 + lane;
-    float s = -INFINITY;
-    int64_t at = -1;
-    if (j < seen) {
-      at = row(j);
-      s = 0.f;
-      if (at >= 0)
-        for (int i = 0; i < D; ++i) s = fmaf(qs[warp][i], bf16_lo(P.k[at * D + i]), s);
-      s *= P.negate ? -P.scale_log2 : P.scale_log2;
-    }
-    float top = s;
-#pragma unroll
-    for (int d = 16; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
-    const float mn = fmaxf(m, top), base = mn == -INFINITY ? 0.f : mn;
-    const float p = j < seen ? ex2(s - base) : 0.f;
-    const float f = m == -INFINITY ? 0.f : ex2(m - base);
-    float sum = p;
-#pragma unroll
-    for (int d = 16; d > 0; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
-    l = l * f + sum;
-    m = mn;
-#pragma unroll
-    for (int c = 0; c < C; ++c) o[c] *= f;
-    const int n = (int)min((int64_t)32, seen - j0);
-    for (int i = 0; i < n; ++i) {
-      const float w = __shfl_sync(0xffffffffu, p, i);
-      const int64_t a = __shfl_sync(0xffffffffu, at, i);
-      if (a >= 0)
-#pragma unroll
-        for (int c = 0; c < C; ++c) o[c] = fmaf(w, bf16_lo(P.v[a * D + lane + 32 * c]), o[c]);
-    }
-  }
-  const float inv = seen > 0 ? 1.f / l : 0.f;
-#pragma unroll
-  for (int c = 0; c < C; ++c) P.out[(t * P.q_heads + head) * D + lane + 32 * c] = (uint16_t)pack_bf16(o[c] * inv, 0.f);
+// Arrival counters (two a CTA), then the parts of split items.
+constexpr int64_t kCounterBytes = 4096;
+constexpr int kMaxCtas = 256;
+static_assert(kCounterBytes >= 2 * 4 * kMaxCtas, "two counters a CTA");
+
+int attention_ctas() { return std::min(sm_count(), kMaxCtas); }
+
+// The few-row kernel serves sequences of at most attn_rows_most() rows, the chunk kernel
+// the others.  Where all sequences are as long as the longest (known from the sizes
+// alone), one launch does; otherwise the host cannot tell, and both kernels look for theirs.
+struct Kernels {
+  bool few, chunk;
+};
+Kernels kernels_of(const gs_seq_batch& b, int32_t group) {
+  const int64_t most = (int64_t)b.max_new * group;
+  if (most <= attn_rows_most()) return {true, false};
+  return {b.tokens != (int64_t)b.n * b.max_new, true};
 }
 
 }  // namespace
 
-// counters, then the parts of split items (16-byte aligned)
-constexpr int64_t kCounterBytes = 4096;
-static_assert(kCounterBytes >= 4 * 256, "one counter a CTA");
+bool attention_units_fit(const gs_paged_cache& c, const gs_seq_batch& b, int32_t q_heads) {
+  const double rows = (double)b.tokens * (q_heads / c.kv_heads), cap = (double)b.table_width * c.page_size;
+  const double units = (rows / attn_chunk_rows() + b.n + 1.0) * c.kv_heads * (cap / std::min(attn_rows_tile(), attn_chunk_tile()) + 1.0);
+  return rows < 1e9 && units < 2e9;
+}
 
-int attention_ctas() { return sm_count() < 256 ? sm_count() : 256; }
-
-size_t attention_workspace_bytes(const gs_paged_cache& c, const gs_seq_batch&, int32_t) {
-  return (size_t)kCounterBytes + (size_t)attention_ctas() * 2 * 64 * (size_t)(c.head_dim + 2) * 4;
+size_t attention_workspace_bytes(const gs_paged_cache& c, const gs_seq_batch& b, int32_t q_heads) {
+  const int rows = kernels_of(b, q_heads / c.kv_heads).chunk ? attn_chunk_rows() : attn_rows_most();
+  return (size_t)kCounterBytes + (size_t)attention_ctas() * 2 * (size_t)rows * (size_t)(c.head_dim + 2) * 4;
 }
 
 gs_status launch_paged_attention(const gs_paged_cache& c, const gs_seq_batch& b, const void* q, int64_t q_stride,
                                  int32_t q_heads, float scale, void* out, void* ws, cudaStream_t s) {
   AttnParams P;
   P.q = static_cast<const uint16_t*>(q);
-  P.k = static_cast<const uint16_t*>(c.k_dev);
   P.v = static_cast<const uint16_t*>(c.v_dev);
   P.out = static_cast<uint16_t*>(out);
   P.offsets = b.offsets_dev;
@@ -109,25 +61,32 @@ gs_status launch_paged_attention(const gs_paged_cache& c, const gs_seq_batch& b,
   P.q_heads = q_heads;
   P.kv_heads = c.kv_heads;
   P.group = q_heads / c.kv_heads;
-  P.scale_log2 = std::fabs(scale) * 1.4426950408889634f;
+  // a scale of zero weighs all keys alike: so does one this small, and masked scores (-inf) stay what they are
+  P.scale_log2 = std::max(std::fabs(scale) * 1.4426950408889634f, 1e-36f);
   P.negate = scale < 0.f;
-  const uint64_t rows = (uint64_t)c.pages * c.kv_heads * c.page_size;
-  const uint32_t box = (uint32_t)attn_rows_box(c.page_size);
-  if (!encode_tmap_slabs_bf16(&P.kmap, c.k_dev, (uint64_t)c.head_dim, rows, box, (uint32_t)c.head_dim / 64) ||
-      !encode_tmap_slabs_bf16(&P.vmap, c.v_dev, (uint64_t)c.head_dim, rows, box, (uint32_t)c.head_dim / 64))
+  const uint64_t rows = (uint64_t)c.pages * c.kv_heads * c.page_size, D = (uint64_t)c.head_dim;
+  const uint32_t slabs = (uint32_t)D / 64;
+  const Kernels k = kernels_of(b, P.group);
+  if (k.few) {
+    const uint32_t box = (uint32_t)attn_rows_box(c.page_size);
+    if (!encode_tmap_slabs_bf16(&P.kmap, c.k_dev, D, rows, box, slabs) || !encode_tmap_slabs_bf16(&P.vmap, c.v_dev, D, rows, box, slabs))
+      return GS_ERR_CUDA;
+    P.min_rows = 1;
+    P.max_rows = attn_rows_most();
+    P.zero_rest = !k.chunk;
+    const int most = (int)std::min((int64_t)b.max_new * P.group, (int64_t)attn_rows_most());
+    const gs_status st = launch_attn_rows(P, c.head_dim, most, attention_ctas(), s);
+    if (st != GS_OK || !k.chunk) return st;
+  }
+  const uint32_t box = (uint32_t)attn_chunk_box(c.page_size);
+  // keys of a page smaller than a unit arrive slab by slab
+  if (!encode_tmap_slabs_bf16(&P.kmap, c.k_dev, D, rows, box, (int)box == attn_chunk_tile() ? slabs : 1u) ||
+      !encode_tmap_slabs_bf16(&P.vmap, c.v_dev, D, rows, box, slabs))
     return GS_ERR_CUDA;
-  const int64_t most = (int64_t)b.max_new * P.group;
-  P.min_rows = 1;
-  P.max_rows = attn_rows_most();
-  P.zero_rest = most <= attn_rows_most();
-  gs_status st = launch_attn_rows(P, c.head_dim, most < attn_rows_most() ? (int)most : attn_rows_most(), attention_ctas(), s);
-  if (st != GS_OK || P.zero_rest) return st;
-  P.min_rows = attn_rows_most() + 1;
-  const dim3 grid((unsigned)b.tokens, (unsigned)((q_heads + 3) / 4));
-  if (c.head_dim == 128) k_attention_simple<128><<<grid, 128, 0, s>>>(P);
-  else k_attention_simple<64><<<grid, 128, 0, s>>>(P);
-  note_launch();
-  return cudaGetLastError() == cudaSuccess ? GS_OK : GS_ERR_CUDA;
+  P.min_rows = k.few ? attn_rows_most() + 1 : 1;
+  P.max_rows = INT32_MAX;
+  P.zero_rest = !k.few;
+  return launch_attn_chunk(P, c.head_dim, attention_ctas(), s);
 }
 
 }  // namespace gs

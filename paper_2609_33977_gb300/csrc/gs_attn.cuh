@@ -19,7 +19,6 @@ namespace gs {
 struct AttnParams {
   CUtensorMap kmap, vmap;   // (64, rows, head_dim / 64) slabs over [pages * kv_heads * page_size][head_dim]
   const uint16_t* q;
-  const uint16_t* k;
   const uint16_t* v;        // the value pages (re-read where a masked tile holds an infinity or NaN)
   uint16_t* out;
   const int32_t* offsets;
@@ -31,7 +30,7 @@ struct AttnParams {
   int64_t q_stride, tokens, pages;
   int32_t n_seqs, width, page_shift, q_heads, kv_heads, group;
   int32_t min_rows, max_rows;   // sequences with that many rows (new tokens x query heads a key head) are this kernel's
-  int32_t zero_rest;            // write zeros for the sequences above max_rows (no other kernel runs)
+  int32_t zero_rest;            // no other kernel runs: zeros for the tokens of sequences above max_rows, and of none
   float scale_log2;             // |scale| log2(e)
   int32_t negate;               // scale < 0: the queries' signs are flipped
 };
@@ -41,6 +40,12 @@ int attn_rows_most();
 int attn_rows_box(int page_size);   // rows of a TMA box
 int attn_rows_tile();               // keys of a unit
 gs_status launch_attn_rows(const AttnParams& P, int head_dim, int rows, int ctas, cudaStream_t s);
+
+// attn_chunk.cu: any number of rows
+int attn_chunk_box(int page_size);
+int attn_chunk_tile();
+int attn_chunk_rows();              // rows of an item
+gs_status launch_attn_chunk(const AttnParams& P, int head_dim, int ctas, cudaStream_t s);
 
 struct SeqInfo {
   int tok0, n, rows;   // first new token, new tokens, rows
@@ -267,6 +272,21 @@ struct Walker {
     return true;
   }
 };
+
+// Zeros for the tokens of no sequence, and (large) of sequences above max_rows, by one warp of every CTA.
+__device__ __forceinline__ void zero_rows(const AttnParams& P, int head_dim, int cta, int lane, bool large) {
+  const int64_t row16 = (int64_t)P.q_heads * head_dim / 8;   // 16-byte pieces of a token's output
+  const auto zero = [&](int64_t t0, int64_t t1) {
+    for (int64_t i = t0 * row16 + lane; i < t1 * row16; i += 32) reinterpret_cast<uint4*>(P.out)[i] = make_uint4(0u, 0u, 0u, 0u);
+  };
+  const int64_t before = min((int64_t)max(0, __ldg(P.offsets)), P.tokens), after = max(0, __ldg(P.offsets + P.n_seqs));
+  for (int64_t t = cta; t < before; t += gridDim.x) zero(t, t + 1);
+  for (int64_t t = after + cta; t < P.tokens; t += gridDim.x) zero(t, t + 1);
+  for (int r = cta; large && r < P.n_seqs; r += (int)gridDim.x) {
+    const SeqInfo s = seq_info(P, r);
+    if (s.rows > P.max_rows) zero(s.tok0, (int64_t)s.tok0 + s.n);
+  }
+}
 
 // Where part `part` of a split item lies: a CTA holds at most one part of an item that
 // began before it, and at most one of an item that goes on after it.

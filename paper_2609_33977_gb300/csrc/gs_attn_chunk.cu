@@ -1,0 +1,675 @@
+// Attention of many rows (new tokens x query heads a key head): chunks of a prompt,
+// whole prompts.
+//
+// Bound by the tensor cores (4 head_dim FLOP a visible pair) and by the exponentials
+// beside them.  An item is 256 rows of a key head against its visible keys, a unit
+// 128 keys.  The rows are two halves of 128, one per softmax warpgroup, whose thread
+// i owns row i, so that maxima and sums need no exchange.  Per half and unit:
+//     S = Q K^T (tcgen05, both operands in shared memory, S in TMEM), the thread
+//     reads its row of S, writes P = exp2(c S - m) over it as bf16, and
+//     O += P V (A = P in TMEM, B = V as stored, i.e. MN-major), O stays in TMEM.
+// The halves take the tensor cores in turn: one's products run under the other's
+// exponentials.  O is rescaled only when a row's maximum grew by more than 2^8
+// (each row for itself), else the old maximum stays in use: exact, since both the
+// sum and O carry it.
+//
+// Keys and values arrive page by page (TMA) in one ring of five 32 KB slots.  Values
+// of a unit that some row does not see are looked over first: rows past the sequence's
+// end become zeros, and infinities and NaN are taken out (a weight of zero would not
+// silence them) and added at the end to the rows that see them.
+//
+// TMEM: S of the halves at columns 0 and 128, O at 256 and 384.
+#include "gs_attn.cuh"
+
+namespace gs {
+namespace {
+using namespace sm100;
+
+constexpr int kCT = 128;                       // keys of a unit
+constexpr int kHalf = 128, kRowsItem = 256;
+constexpr int kAcThreads = 384;                // warps: keys, MMA, values, value check, then two softmax warpgroups
+constexpr int kRing = 5;
+constexpr int kSegs = 4;
+constexpr uint64_t kAcWaitLimitNs = 2000000000ull;
+constexpr int kRegsOther = 72, kRegsSoftmax = 216;
+static_assert(4 * 32 * kRegsOther + 8 * 32 * kRegsSoftmax <= kAcThreads * 168, "register split");
+
+struct ChunkTraits {
+  static constexpr int kLeast = 4, kSnap = 2;
+  static __device__ __forceinline__ int row_tiles(const SeqInfo& s, const AttnParams& P) {
+    return s.rows >= P.min_rows && s.rows <= P.max_rows ? (s.rows + kRowsItem - 1) / kRowsItem : 0;
+  }
+  // units that the rows up to `row_end` of a sequence see
+  static __device__ __forceinline__ int units_of(const SeqInfo& s, const AttnParams& P, int row_end) {
+    return max(1, (s.seen((min(row_end, s.rows) - 1) / P.group) + kCT - 1) / kCT);
+  }
+  static __device__ __forceinline__ int tiles(const SeqInfo& s, const AttnParams& P, int rt) {
+    return units_of(s, P, (rt + 1) * kRowsItem);
+  }
+};
+
+template <int D>
+struct ChunkCfg {
+  static constexpr int kOpBytes = kCT * D * 2;         // a unit's keys or values
+  static constexpr int kQBytes = kHalf * D * 2;        // a half's queries
+  static constexpr int kSmem = 2 * kQBytes + kRing * kOpBytes + 1024;
+  static constexpr int kSlabs = D / 64;
+};
+
+// D[tmem] (+)= A[tmem] * B[smem], one CTA
+__device__ __forceinline__ void mma_bf16_ts(uint32_t d_tmem, uint32_t a_tmem, uint64_t bdesc, uint32_t idesc, uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "setp.ne.b32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
+      ::"r"(d_tmem), "r"(a_tmem), "l"(bdesc), "r"(idesc), "r"(accumulate)
+      : "memory");
+}
+__device__ __forceinline__ void tmem_st_x32(uint32_t taddr, const uint32_t (&v)[32]) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,"
+      "%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31,%32};" ::"r"(taddr),
+      "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]), "r"(v[8]), "r"(v[9]), "r"(v[10]),
+      "r"(v[11]), "r"(v[12]), "r"(v[13]), "r"(v[14]), "r"(v[15]), "r"(v[16]), "r"(v[17]), "r"(v[18]), "r"(v[19]), "r"(v[20]),
+      "r"(v[21]), "r"(v[22]), "r"(v[23]), "r"(v[24]), "r"(v[25]), "r"(v[26]), "r"(v[27]), "r"(v[28]), "r"(v[29]), "r"(v[30]),
+      "r"(v[31])
+      : "memory");
+}
+// Shared-memory descriptor of the values as an MN-major operand, 128-byte swizzle: 64-channel
+// blocks of `block` bytes, 8-key groups 1024 bytes apart
+__device__ __forceinline__ uint64_t sdesc_v(uint32_t saddr, uint32_t block) {
+  uint64_t d = 0;
+  d |= (uint64_t)((saddr >> 4) & 0x3FFFu);
+  d |= (uint64_t)(block >> 4) << 16;
+  d |= (uint64_t)(1024 >> 4) << 32;
+  d |= (uint64_t)1 << 46;
+  d |= (uint64_t)2 << 61;
+  return d;
+}
+__device__ __forceinline__ float max3(float a, float b, float c) { return fmaxf(fmaxf(a, b), c); }
+__device__ __forceinline__ uint32_t nonfinite2(uint32_t v) {   // bits of the halves that are an infinity or NaN
+  const uint32_t e = v & 0x7F807F80u;
+  return ((e & 0xFFFFu) == 0x7F80u ? 0xFFFFu : 0u) | ((e >> 16) == 0x7F80u ? 0xFFFF0000u : 0u);
+}
+
+template <int D>
+__global__ void __launch_bounds__(kAcThreads, 1) k_attn_chunk(const __grid_constant__ AttnParams P) {
+  using C = ChunkCfg<D>;
+  extern __shared__ uint8_t ac_smem_raw[];
+  // A slot holds keys and values in turn (the ring is odd).  Whoever waits for one kind may be ahead of the other, so
+  // each kind has its own barriers; they move once per use by that kind, every second turn of the ring.
+  __shared__ __align__(8) uint64_t kfull_bar[kRing], vfull_bar[kRing];   // bytes have landed
+  __shared__ __align__(8) uint64_t clean_bar[kRing];                     // values looked over
+  __shared__ __align__(8) uint64_t empty_bar[kRing];                     // moves with every use
+  __shared__ __align__(8) uint64_t seg_full[kSegs];
+  __shared__ __align__(8) uint64_t seg_empty[kSegs];
+  __shared__ __align__(8) uint64_t q_bar[2];           // a half's queries are in shared memory
+  __shared__ __align__(8) uint64_t s_bar[2];           // S is in TMEM
+  __shared__ __align__(8) uint64_t p_bar[2];           // P is in TMEM, O is rescaled
+  __shared__ __align__(8) uint64_t o_bar[2];           // P V is done
+  __shared__ __align__(8) uint64_t join_bar[2];
+  __shared__ __align__(8) uint64_t drain_bar;
+  __shared__ Segment segs[kSegs];
+  __shared__ WorkShared work;
+  __shared__ uint32_t tmem_base_s;
+  __shared__ int abort_s, bad_s[kSegs], last_s[2];
+  uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(ac_smem_raw) + 1023) & ~uintptr_t(1023));
+  uint8_t* ring = smem + 2 * C::kQBytes;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int cta = (int)blockIdx.x;
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < kRing; ++s) {
+      mbar_init(&kfull_bar[s], 1);
+      mbar_init(&vfull_bar[s], 1);
+      mbar_init(&empty_bar[s], 1);
+      mbar_init(&clean_bar[s], 1);
+    }
+    for (int s = 0; s < kSegs; ++s) {
+      mbar_init(&seg_full[s], 1);
+      mbar_init(&seg_empty[s], 11);   // every warp but the one that fills it
+    }
+    for (int h = 0; h < 2; ++h) {
+      mbar_init(&q_bar[h], 4);
+      mbar_init(&s_bar[h], 1);
+      mbar_init(&p_bar[h], 4);
+      mbar_init(&o_bar[h], 1);
+      mbar_init(&join_bar[h], 4);
+    }
+    mbar_init(&drain_bar, 1);
+    abort_s = 0;
+    fence_mbar_init();
+    prefetch_tmap(&P.kmap);
+    prefetch_tmap(&P.vmap);
+  }
+  if (warp == 1) {
+    tmem_alloc(&tmem_base_s, 512);
+    tmem_relinquish();
+  }
+  const Shares shares = divide_work<ChunkTraits, kAcThreads>(P, cta, work);
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = tmem_base_s;
+  volatile int* abort_flag = &abort_s;
+  const int box_shift = min(P.page_shift, 7), box = 1 << box_shift;   // rows of a TMA box
+  const auto wait_warp = [&](uint64_t* bar, uint32_t parity) {
+    return __all_sync(0xffffffffu, mbar_wait_bounded(bar, parity, abort_flag, P.err, kAcWaitLimitNs, kDevErrTimeout)) != 0;
+  };
+  // A half's units end where its last row's keys end.
+  const auto half_units = [&](const Segment& g, int h) {
+    return ChunkTraits::units_of(g.s, P, g.it.rt * kRowsItem + (h + 1) * kHalf);
+  };
+  const auto halves = [&](const Segment& g) { return g.s.rows - g.it.rt * kRowsItem > kHalf ? 2 : 1; };
+
+  if (warp < 4) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsOther));
+    uint32_t sg = 0, sph = 0;          // segment slot and its phase
+    const auto next_seg = [&]() {
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&seg_empty[sg]);
+      if (++sg == kSegs) {
+        sg = 0;
+        sph ^= 1u;
+      }
+    };
+    if (warp == 0 || warp == 2) {
+      // ---------------------------------------------------------- copies: warp 0 keys (it also divides the work), warp 2 values
+      const bool keys = warp == 0;
+      Walker<ChunkTraits> walk(P, shares, work, cta);
+      Segment g;
+      const int32_t no_row = (int32_t)((P.pages * P.kv_heads) << P.page_shift);   // past the last: reads as zeros
+      uint32_t slot = keys ? 0 : 1, ph = 1u;
+      bool ok = true;
+      while (ok) {
+        if (keys) {
+          const bool more = walk.next(g);
+          if (!wait_warp(&seg_empty[sg], sph ^ 1u)) break;
+          if (lane == 0) {
+            if (!more) g.r = -1;
+            segs[sg] = g;
+            mbar_arrive(&seg_full[sg]);
+          }
+          __syncwarp();
+          if (++sg == kSegs) {
+            sg = 0;
+            sph ^= 1u;
+          }
+          if (!more) break;
+        } else {
+          if (!wait_warp(&seg_full[sg], sph)) break;
+          g = segs[sg];
+          next_seg();
+          if (g.r < 0) break;
+        }
+        const int len = g.s.len();
+        const int64_t trow = (int64_t)g.r * P.width;
+        int held = -1, page = -1;   // lane i holds table entry 32 held + i
+        for (int t = g.ta; t < g.tb; ++t) {
+          const int valid = min(kCT, max(0, len - t * kCT));
+          const int boxes = (valid + box - 1) >> box_shift;   // at most 8
+          const int e0 = (t * kCT) >> P.page_shift;
+          if (e0 >> 5 != held) {
+            held = e0 >> 5;
+            const int e = 32 * held + lane;
+            page = e < P.width && ((int64_t)e << P.page_shift) < len ? __ldg(P.table + trow + e) : -1;
+          }
+          const int key = t * kCT + ((lane & 7) << box_shift);
+          const int pg = __shfl_sync(0xffffffffu, page, (key >> P.page_shift) & 31);
+          const int32_t row = pg >= 0 && pg < P.pages
+                                  ? (int32_t)((((int64_t)pg * P.kv_heads + g.it.h) << P.page_shift) + (key & ((1 << P.page_shift) - 1)))
+                                  : no_row;
+          if (!wait_warp(&empty_bar[slot], ph)) {
+            ok = false;
+            break;
+          }
+          uint8_t* dst = ring + slot * C::kOpBytes;
+          uint64_t* full = keys ? &kfull_bar[slot] : &vfull_bar[slot];
+          if (elect_one()) mbar_arrive_expect_tx(full, (uint32_t)(boxes * box * D * 2));
+          __syncwarp();
+          // Keys: slabs of 64 channels x 128 keys.  Values: box after box, each with its slabs.
+          for (int b = 0; b < boxes; ++b) {
+            const int32_t r = __shfl_sync(0xffffffffu, row, b);
+            if (elect_one()) {
+              if (!keys) {
+                tma_load_3d(dst + b * (box * D * 2), &P.vmap, full, 0, r, 0);
+              } else if (box == kCT) {
+                tma_load_3d(dst, &P.kmap, full, 0, r, 0);
+              } else {
+#pragma unroll
+                for (int sl = 0; sl < C::kSlabs; ++sl)
+                  tma_load_3d(dst + sl * (kCT * 128) + b * (box * 128), &P.kmap, full, 0, r, sl);
+              }
+            }
+            __syncwarp();
+          }
+          slot += 2;
+          if (slot >= kRing) {
+            slot -= kRing;
+            ph ^= 1u;
+          }
+        }
+      }
+    } else if (warp == 1) {
+      // ---------------------------------------------------------- MMA issuer
+      const uint32_t idesc_s = idesc_bf16_f32(kHalf, kCT);
+      const uint32_t idesc_o = idesc_bf16_f32(kHalf, D) | (1u << 16);   // bit 16: B is MN-major
+      uint32_t ks = 0, kturn = 0u, vs = 1, vturn = 0u;   // slots, and turns of the ring
+      uint32_t qph[2] = {0u, 0u}, pph[2] = {0u, 0u}, oph[2] = {0u, 0u};
+      const uint32_t vblock = (uint32_t)box * 128u;
+      bool ok = true;
+      // S of half h against the keys in slot k
+      const auto issue_s = [&](int h, uint32_t k, bool last) {
+        if (elect_one()) {
+          const uint64_t a = sdesc_sw128(smem_u32(smem + h * C::kQBytes)), b = sdesc_sw128(smem_u32(ring + k * C::kOpBytes));
+#pragma unroll
+          for (int kk = 0; kk < D / 16; ++kk) {
+            const uint64_t off = (uint64_t)(((kk >> 2) * (kHalf * 128) + (kk & 3) * 32) >> 4);
+            mma_bf16_ss(tmem + h * 128, a + off, b + off, idesc_s, kk == 0 ? 0u : 1u);
+          }
+          mma_commit(&s_bar[h]);
+          if (last) mma_commit(&empty_bar[k]);
+        }
+        __syncwarp();
+      };
+      static_assert(kHalf == kCT, "one slab size for queries and keys");
+      while (ok) {
+        if (!wait_warp(&seg_full[sg], sph)) break;
+        const Segment g = segs[sg];
+        next_seg();
+        if (g.r < 0) break;
+        const int nh = halves(g);
+        int end[2];   // units [ta, end) of a half; the last half has them all
+        for (int h = 0; h < 2; ++h) end[h] = h < nh ? min(g.tb, half_units(g, h)) : 0;
+        if (!wait_warp(&kfull_bar[ks], (kturn >> 1) & 1u)) break;
+        for (int h = 0; h < nh && ok; ++h) {
+          if (g.ta >= end[h]) continue;
+          ok = wait_warp(&q_bar[h], qph[h]);
+          qph[h] ^= 1u;
+          tc_fence_after();
+          if (ok) issue_s(h, ks, h == nh - 1);
+        }
+        for (int t = g.ta; t < g.tb && ok; ++t) {
+          uint32_t kn = ks + 2, kn_turn = kturn;   // the next unit's keys
+          if (kn >= kRing) {
+            kn -= kRing;
+            ++kn_turn;
+          }
+          if (!wait_warp(&clean_bar[vs], (vturn >> 1) & 1u)) {
+            ok = false;
+            break;
+          }
+          if (t + 1 < g.tb && !wait_warp(&kfull_bar[kn], (kn_turn >> 1) & 1u)) {
+            ok = false;
+            break;
+          }
+          for (int h = 0; h < nh; ++h) {
+            if (t >= end[h]) continue;
+            if (!wait_warp(&p_bar[h], pph[h])) {
+              ok = false;
+              break;
+            }
+            pph[h] ^= 1u;
+            tc_fence_after();
+            if (elect_one()) {
+              const uint32_t v = smem_u32(ring + vs * C::kOpBytes);
+#pragma unroll
+              for (int kk = 0; kk < kCT / 16; ++kk) {
+                const int key = 16 * kk;
+                const uint32_t off = (uint32_t)(key >> box_shift) * (vblock * C::kSlabs) + (uint32_t)(key & (box - 1)) * 128u;
+                mma_bf16_ts(tmem + 256 + h * 128, tmem + h * 128 + 8 * kk, sdesc_v(v + off, vblock), idesc_o,
+                            t == g.ta && kk == 0 ? 0u : 1u);
+              }
+              mma_commit(&o_bar[h]);
+              if (h == nh - 1) mma_commit(&empty_bar[vs]);
+            }
+            __syncwarp();
+            if (t + 1 < end[h]) {
+              // S goes where P is being read: not before that product is over
+              if (!wait_warp(&o_bar[h], oph[h])) {
+                ok = false;
+                break;
+              }
+              tc_fence_after();
+              issue_s(h, kn, h == nh - 1);
+            }
+            oph[h] ^= 1u;
+          }
+          ks = kn;
+          kturn = kn_turn;
+          vs += 2;
+          if (vs >= kRing) {
+            vs -= kRing;
+            ++vturn;
+          }
+        }
+      }
+      // whatever was issued is over before TMEM goes back
+      if (elect_one()) {
+        mma_commit(&drain_bar);
+        mbar_wait_bounded(&drain_bar, 0u, nullptr, P.err, kAcWaitLimitNs, kDevErrTimeout);
+      }
+      __syncwarp();
+    } else {
+      // ---------------------------------------------------------- values that some row does not see
+      uint32_t vs = 1, vturn = 0u;
+      bool ok = true;
+      while (ok) {
+        if (!wait_warp(&seg_full[sg], sph)) break;
+        const Segment g = segs[sg];
+        const uint32_t at = sg;
+        if (g.r >= 0 && lane == 0) bad_s[at] = 0;
+        __syncwarp();
+        next_seg();
+        if (g.r < 0) break;
+        const int len = g.s.len(), all_see = g.s.seen(g.it.rt * kRowsItem / P.group);
+        for (int t = g.ta; t < g.tb; ++t) {
+          if (!wait_warp(&vfull_bar[vs], (vturn >> 1) & 1u)) {
+            ok = false;
+            break;
+          }
+          const int key0 = t * kCT;
+          if (key0 + kCT > all_see) {
+            uint8_t* v = ring + vs * C::kOpBytes;
+            // a key's row is kSlabs pieces of 128 bytes; their swizzle does not matter here
+            const auto piece = [&](int k, int i) {   // 16-byte piece i of key k of the unit
+              return reinterpret_cast<uint4*>(v + (((k >> box_shift) * C::kSlabs + (i >> 3)) << box_shift) * 128 +
+                                              (k & (box - 1)) * 128 + (i & 7) * 16);
+            };
+            constexpr int kPieces = D / 8, kStep = 32 / kPieces;   // keys of a step of the warp
+            const int end = min(kCT, max(0, len - key0));
+            bool bad = false;
+            for (int k = max(0, all_see - key0) + lane / kPieces; k < kCT; k += kStep) {
+              uint4* p = piece(k, lane % kPieces);
+              if (k >= end) {
+                *p = make_uint4(0u, 0u, 0u, 0u);
+              } else {
+                uint4 x = *p;
+                const uint4 n = make_uint4(nonfinite2(x.x), nonfinite2(x.y), nonfinite2(x.z), nonfinite2(x.w));
+                if (n.x | n.y | n.z | n.w) {
+                  *p = make_uint4(x.x & ~n.x, x.y & ~n.y, x.z & ~n.z, x.w & ~n.w);
+                  bad = true;
+                }
+              }
+            }
+            if (bad) bad_s[at] = 1;
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+          }
+          __syncwarp();
+          if (lane == 0) mbar_arrive(&clean_bar[vs]);
+          vs += 2;
+          if (vs >= kRing) {
+            vs -= kRing;
+            ++vturn;
+          }
+        }
+      }
+      if (P.zero_rest) zero_rows(P, D, cta, lane, false);
+    }
+  } else {
+    // ------------------------------------------------------------ softmax: a row a thread
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegsSoftmax));
+    const int h = (warp - 4) >> 2, quarter = warp & 3;
+    const uint32_t ts = tmem + h * 128 + ((uint32_t)(32 * quarter) << 16);
+    const uint32_t to = tmem + 256 + h * 128 + ((uint32_t)(32 * quarter) << 16);
+    uint32_t sg = 0, sph = 0, s_ph = 0u, o_ph = 0u, j_ph = 0u;
+    const auto meet = [&]() {   // the warpgroup's barrier, bounded like every wait
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&join_bar[h]);
+      const bool met = wait_warp(&join_bar[h], j_ph);
+      j_ph ^= 1u;
+      return met;
+    };
+    const float c = P.scale_log2;
+    bool ok = true;
+    while (ok) {
+      if (!wait_warp(&seg_full[sg], sph)) break;
+      const Segment g = segs[sg];
+      const uint32_t at = sg;
+      if (++sg == kSegs) {
+        sg = 0;
+        sph ^= 1u;
+      }
+      const auto seg_done = [&]() {
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&seg_empty[at]);
+      };
+      if (g.r < 0) break;
+      if (h >= halves(g)) {
+        seg_done();
+        continue;
+      }
+      const int row_h = g.it.rt * kRowsItem + h * kHalf;        // the half's first row
+      const int end = min(g.tb, half_units(g, h));
+      const int row = row_h + 32 * quarter + lane;              // this thread's
+      const bool row_on = row < g.s.rows;
+      const int tok = row_on ? row / P.group : 0, hd = row_on ? row - tok * P.group : 0;
+      const int vis = row_on ? g.s.seen(tok) : 0;
+      const int all_see = g.s.seen(row_h / P.group);
+      float m = -INFINITY, l = 0.f;
+      if (g.ta < end) {
+        // ---- the warp's 32 rows of queries, swizzled as the MMA reads them
+        constexpr int kPieces = D / 8, kStep = 32 / kPieces;
+        const uint32_t flip = P.negate ? 0x80008000u : 0u;
+        uint4 x[32 / kStep];
+#pragma unroll
+        for (int i = 0; i < 32 / kStep; ++i) {
+          const int r = row_h + 32 * quarter + i * kStep + lane / kPieces;
+          x[i] = make_uint4(0u, 0u, 0u, 0u);
+          if (r < g.s.rows) {
+            const int tk = r / P.group, hq = r - tk * P.group;
+            x[i] = __ldg(reinterpret_cast<const uint4*>(P.q + (int64_t)(g.s.tok0 + tk) * P.q_stride +
+                                                        (int64_t)(g.it.h * P.group + hq) * D) + lane % kPieces);
+          }
+        }
+#pragma unroll
+        for (int i = 0; i < 32 / kStep; ++i) {
+          const int r = 32 * quarter + i * kStep + lane / kPieces, p = lane % kPieces;
+          *reinterpret_cast<uint4*>(smem + h * C::kQBytes + (p >> 3) * (kHalf * 128) + r * 128 + (((p & 7) ^ (r & 7)) << 4)) =
+              make_uint4(x[i].x ^ flip, x[i].y ^ flip, x[i].z ^ flip, x[i].w ^ flip);
+        }
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&q_bar[h]);
+      }
+      for (int t = g.ta; t < end; ++t) {
+        if (!wait_warp(&s_bar[h], s_ph)) {
+          ok = false;
+          break;
+        }
+        s_ph ^= 1u;
+        tc_fence_after();
+        uint32_t s[4][32];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) tmem_ld_x32(ts + 32 * i, s[i]);
+        tmem_wait_ld();
+#pragma unroll
+        for (int i = 0; i < 4; ++i) reg_fence(s[i]);
+        const int key0 = t * kCT;
+        if (key0 + kCT > all_see) {
+          const int n = vis - key0;
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int e = 0; e < 32; ++e)
+              if (32 * i + e >= n) s[i][e] = 0xFF800000u;   // -inf
+        }
+        float top[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          top[i] = __uint_as_float(s[i][0]);
+#pragma unroll
+          for (int e = 1; e < 31; e += 2) top[i] = max3(top[i], __uint_as_float(s[i][e]), __uint_as_float(s[i][e + 1]));
+          top[i] = fmaxf(top[i], __uint_as_float(s[i][31]));
+        }
+        const float mt = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
+        float f = 1.f;
+        if ((mt - m) * c > 8.f) {   // m = -inf: always, once a key is seen
+          f = ex2((m - mt) * c);
+          m = mt;
+        }
+        if (t > g.ta && __any_sync(0xffffffffu, f != 1.f)) {
+#pragma unroll
+          for (int i = 0; i < D / 32; ++i) {
+            uint32_t o[32];
+            tmem_ld_x32(to + 32 * i, o);
+            tmem_wait_ld();
+            reg_fence(o);
+#pragma unroll
+            for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * f);
+            tmem_st_x32(to + 32 * i, o);
+          }
+        }
+        const float mc = m == -INFINITY ? 0.f : m * c;
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+          for (int e = 0; e < 32; ++e) s[i][e] = __float_as_uint(ex2(fmaf(__uint_as_float(s[i][e]), c, -mc)));
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          uint32_t p[32];
+#pragma unroll
+          for (int e = 0; e < 16; ++e) {
+            p[e] = pack_bf16(__uint_as_float(s[2 * i][2 * e]), __uint_as_float(s[2 * i][2 * e + 1]));
+            p[16 + e] = pack_bf16(__uint_as_float(s[2 * i + 1][2 * e]), __uint_as_float(s[2 * i + 1][2 * e + 1]));
+          }
+          tmem_st_x32(ts + 32 * i, p);
+        }
+        tmem_wait_st();
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&p_bar[h]);
+        float sum[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+          for (int e = 0; e < 32; ++e) sum[i] += __uint_as_float(s[i][e]);
+        l = l * f + ((sum[0] + sum[1]) + (sum[2] + sum[3]));
+        if (t + 1 < end) o_ph ^= 1u;   // P V of this unit is over when the next S is there
+      }
+      if (!ok) break;
+      // ---- the segment's result
+      float o[D];
+      if (g.ta < end) {
+        if (!wait_warp(&o_bar[h], o_ph)) break;
+        o_ph ^= 1u;
+        tc_fence_after();
+#pragma unroll
+        for (int i = 0; i < D / 32; ++i) {
+          uint32_t v[32];
+          tmem_ld_x32(to + 32 * i, v);
+          tmem_wait_ld();
+          reg_fence(v);
+#pragma unroll
+          for (int e = 0; e < 32; ++e) o[32 * i + e] = __uint_as_float(v[e]);
+        }
+      } else {
+#pragma unroll
+        for (int e = 0; e < D; ++e) o[e] = 0.f;
+      }
+      if (bad_s[at]) {   // infinities and NaN of keys that only some rows see
+        const int stop = min(g.tb * kCT, vis);
+        for (int key = max(g.s.seen(g.it.rt * kRowsItem / P.group), g.ta * kCT); key < stop; ++key) {
+          const int pg = __ldg(P.table + (int64_t)g.r * P.width + (key >> P.page_shift));
+          if (pg < 0 || pg >= P.pages) continue;
+          const uint16_t* vr = P.v + ((((int64_t)pg * P.kv_heads + g.it.h) << P.page_shift) + (key & ((1 << P.page_shift) - 1))) * D;
+#pragma unroll
+          for (int e = 0; e < D; ++e) {
+            const float x = bf16_lo(__ldg(vr + e));
+            if (!isfinite(x)) o[e] += x;
+          }
+        }
+      }
+      seg_done();
+      uint16_t* dst = P.out + ((int64_t)(g.s.tok0 + tok) * P.q_heads + g.it.h * P.group + hd) * D;
+      const auto store = [&](float inv) {
+        if (!row_on) return;
+#pragma unroll
+        for (int e = 0; e < D; e += 8)
+          *reinterpret_cast<uint4*>(dst + e) =
+              make_uint4(pack_bf16(o[e] * inv, o[e + 1] * inv), pack_bf16(o[e + 2] * inv, o[e + 3] * inv),
+                         pack_bf16(o[e + 4] * inv, o[e + 5] * inv), pack_bf16(o[e + 6] * inv, o[e + 7] * inv));
+      };
+      if (g.parts == 1) {
+        store(vis > 0 ? 1.f / l : 0.f);
+      } else {
+        // parts: [D / 4][256 rows][4], then [256][2]; the warpgroup that arrives last joins its half
+        const int ri = h * kHalf + 32 * quarter + lane;
+        float* slot = part_slot(P, g.first_cta, g.part, kRowsItem, D);
+#pragma unroll
+        for (int e = 0; e < D; e += 4)
+          *reinterpret_cast<float4*>(slot + (size_t)(e * kRowsItem + 4 * ri)) = make_float4(o[e], o[e + 1], o[e + 2], o[e + 3]);
+        *reinterpret_cast<float2*>(slot + (size_t)(D * kRowsItem + 2 * ri)) = make_float2(m, l);
+        __threadfence();
+        if (!meet()) break;
+        if (quarter == 0 && lane == 0) {
+          const int got = atomicAdd(P.cnt + 2 * g.first_cta + h, 1);
+          last_s[h] = got == g.parts - 1;
+          if (last_s[h]) P.cnt[2 * g.first_cta + h] = 0;
+          __threadfence();
+        }
+        if (!meet()) break;
+        if (last_s[h]) {
+          float mm = -INFINITY, ll = 0.f;
+          for (int p = 0; p < g.parts; ++p)
+            mm = fmaxf(mm, __ldcg(part_slot(P, g.first_cta, p, kRowsItem, D) + D * kRowsItem + 2 * ri));
+          const float base = mm == -INFINITY ? 0.f : mm;
+#pragma unroll
+          for (int e = 0; e < D; ++e) o[e] = 0.f;
+          for (int p = 0; p < g.parts; ++p) {
+            const float* sp = part_slot(P, g.first_cta, p, kRowsItem, D);
+            const float2 ml = __ldcg(reinterpret_cast<const float2*>(sp + D * kRowsItem + 2 * ri));
+            const float fp = ml.x == mm ? 1.f : ex2((ml.x - base) * c);
+            ll = fmaf(ml.y, fp, ll);
+#pragma unroll
+            for (int e = 0; e < D; e += 4) {
+              const float4 v = __ldcg(reinterpret_cast<const float4*>(sp + (size_t)(e * kRowsItem + 4 * ri)));
+              o[e] = fmaf(v.x, fp, o[e]);
+              o[e + 1] = fmaf(v.y, fp, o[e + 1]);
+              o[e + 2] = fmaf(v.z, fp, o[e + 2]);
+              o[e + 3] = fmaf(v.w, fp, o[e + 3]);
+            }
+          }
+          store(vis > 0 ? 1.f / ll : 0.f);
+        }
+      }
+      // the next segment's S may overwrite this one's: every read of TMEM is behind
+      tc_fence_before();
+    }
+  }
+  tc_fence_before();
+  __syncthreads();
+  if (abort_s) {
+    // a role gave up: give copies in flight time to land
+    const uint64_t t0 = globaltimer_ns();
+    while (globaltimer_ns() - t0 < 2000000ull) {
+    }
+  }
+  if (warp == 1) {
+    tc_fence_after();
+    tmem_dealloc(tmem, 512);
+  }
+}
+
+template <int D>
+gs_status chunk_launch(const AttnParams& P, int ctas, cudaStream_t s) {
+  static const cudaError_t attr =
+      cudaFuncSetAttribute(k_attn_chunk<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, ChunkCfg<D>::kSmem);
+  if (attr != cudaSuccess) return GS_ERR_CUDA;
+  k_attn_chunk<D><<<(unsigned)ctas, kAcThreads, ChunkCfg<D>::kSmem, s>>>(P);
+  note_launch();
+  return cudaGetLastError() == cudaSuccess ? GS_OK : GS_ERR_CUDA;
+}
+
+}  // namespace
+
+int attn_chunk_box(int page_size) { return page_size < kCT ? page_size : kCT; }
+
+int attn_chunk_tile() { return kCT; }
+
+int attn_chunk_rows() { return kRowsItem; }
+
+gs_status launch_attn_chunk(const AttnParams& P, int head_dim, int ctas, cudaStream_t s) {
+  return head_dim == 128 ? chunk_launch<128>(P, ctas, s) : chunk_launch<64>(P, ctas, s);
+}
+
+}  // namespace gs

@@ -208,19 +208,7 @@ __global__ void __launch_bounds__(RowsCfg<D, WR>::kThreads, 1) k_attn_rows(const
       segs[st].r = -1;
       mbar_arrive(&full_bar[st]);
     }
-    // ---- rows that nothing computes: tokens of no sequence, and sequences of more rows than were announced
-    const int64_t row16 = (int64_t)P.q_heads * D / 8;   // 16-byte pieces of a token's output
-    const auto zero = [&](int64_t t0, int64_t t1) {
-      for (int64_t i = t0 * row16 + lane; i < t1 * row16; i += 32) reinterpret_cast<uint4*>(P.out)[i] = make_uint4(0u, 0u, 0u, 0u);
-    };
-    const int64_t before = min((int64_t)max(0, __ldg(P.offsets)), P.tokens), after = max(0, __ldg(P.offsets + P.n_seqs));
-    for (int64_t t = cta; t < before; t += gridDim.x) zero(t, t + 1);
-    for (int64_t t = after + cta; t < P.tokens; t += gridDim.x) zero(t, t + 1);
-    if (P.zero_rest)
-      for (int r = cta; r < P.n_seqs; r += (int)gridDim.x) {
-        const SeqInfo s = seq_info(P, r);
-        if (s.rows > P.max_rows) zero(s.tok0, (int64_t)s.tok0 + s.n);
-      }
+    zero_rows(P, D, cta, lane, P.zero_rest != 0);
   } else {
     // ------------------------------------------------------------ compute
     const int wr = warp / WK, wk = warp % WK, gq = lane >> 2, qd = lane & 3;

@@ -19,6 +19,7 @@ gs_status launch_cache_append(const gs_paged_cache& c, const gs_seq_batch& b, co
                               const void* k, int64_t k_stride, const void* v, int64_t v_stride, const float* cos_t,
                               const float* sin_t, int64_t n_pos, void* q_out, cudaStream_t s);
 // attention.cu
+bool attention_units_fit(const gs_paged_cache& c, const gs_seq_batch& b, int32_t q_heads);   // work is counted in 32 bits
 size_t attention_workspace_bytes(const gs_paged_cache& c, const gs_seq_batch& b, int32_t q_heads);
 gs_status launch_paged_attention(const gs_paged_cache& c, const gs_seq_batch& b, const void* q, int64_t q_stride,
                                  int32_t q_heads, float scale, void* out, void* ws, cudaStream_t s);

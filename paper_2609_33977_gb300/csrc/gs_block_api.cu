@@ -130,7 +130,7 @@ static gs_status check_attention(const gs_paged_cache* cache, const gs_seq_batch
   gs_status st = check_cache(cache);
   if (st != GS_OK || (st = check_batch(batch, cache)) != GS_OK) return st;
   if (q_heads <= 0 || q_heads % cache->kv_heads != 0) return GS_ERR_INVALID_ARG;
-  if (q_heads / cache->kv_heads > 64) return GS_ERR_UNSUPPORTED;
+  if (q_heads / cache->kv_heads > 64 || !attention_units_fit(*cache, *batch, q_heads)) return GS_ERR_UNSUPPORTED;
   return GS_OK;
 }
 

@@ -183,7 +183,9 @@ class Packed:
 
 
 def trim() -> None:
-    """Give the device buffers kept from released handles back to the device (waits for it)."""
+    """Give the device buffers kept from released handles back to the device (waits for it), and the
+    attention's workspaces to torch's allocator."""
+    _attention_ws.clear()
     lib.gs_trim()
 
 
@@ -498,8 +500,7 @@ def linear_adapted(x: torch.Tensor, p: Packed, ad: Adapters, offsets: torch.Tens
 
 
 class PagedCache:
-    """Keys and values of one layer, bf16 [pages, kv_heads, page_size, head_dim] each, and the attention's
-    workspace for each stream that uses it (views of one tensor per layer share nothing)."""
+    """Keys and values of one layer, bf16 [pages, kv_heads, page_size, head_dim] each."""
 
     def __init__(self, k_pages: torch.Tensor, v_pages: torch.Tensor):
         _require_cuda(k_pages, torch.bfloat16, "k_pages")
@@ -510,21 +511,28 @@ class PagedCache:
         self.pages, self.kv_heads, self.page_size, self.head_dim = k_pages.shape
         self._c = _CacheStruct(k_pages.data_ptr(), v_pages.data_ptr(), self.pages, self.page_size, self.kv_heads, self.head_dim)
         self._ref = ctypes.addressof(self._c)
-        self._need = {}
-        self._ws = {}
 
-    def _workspace(self, batch: "Batch", q_heads: int, stream: Optional[torch.cuda.Stream], sp: int) -> torch.Tensor:
-        need = self._need.get(q_heads)
-        if need is None:
-            c = ctypes.c_size_t()
-            _check(lib.gs_paged_attention_workspace(self._ref, batch._ref, q_heads, ctypes.byref(c)),
-                   "gs_paged_attention_workspace")
-            need = self._need[q_heads] = c.value
-        ws = self._ws.get(sp)
-        if ws is None or ws.numel() < need:
-            with torch.cuda.stream(stream if stream is not None else torch.cuda.current_stream()):
-                ws = self._ws[sp] = torch.zeros((max(need, 16),), dtype=torch.uint8, device=self.k_pages.device)
-        return ws
+
+# The attention's workspace, one per (device, stream) for all layers; calls leave it ready for the next.  A graph
+# goes on using the one it was captured with: those stay (_attention_ws_in_graphs).
+_attention_ws: dict = {}
+_attention_ws_in_graphs: dict = {}
+
+
+def _attention_workspace(need: int, device, stream: Optional[torch.cuda.Stream], sp: int) -> torch.Tensor:
+    if stream is not None and stream != torch.cuda.current_stream():
+        with torch.cuda.stream(stream):
+            return _attention_workspace(need, device, None, sp)
+    key = (device.index, sp)
+    ws = _attention_ws.get(key)
+    fits = ws is not None and ws.numel() >= need
+    if torch.cuda.is_current_stream_capturing():
+        if not fits:               # the graph's own memory, zeroed in every replay
+            return torch.zeros((need,), dtype=torch.uint8, device=device)
+        _attention_ws_in_graphs[ws.data_ptr()] = ws
+    elif not fits:
+        ws = _attention_ws[key] = torch.zeros((need,), dtype=torch.uint8, device=device)
+    return ws
 
 
 class Batch:
@@ -541,6 +549,17 @@ class Batch:
         self.offsets, self.kv_lens, self.table, self.max_new = offsets, kv_lens, table, int(max_new)
         self._c = _BatchStruct(offsets.data_ptr(), kv_lens.data_ptr(), table.data_ptr(), n, table.shape[1], 0, self.max_new)
         self._ref = ctypes.addressof(self._c)
+        self._need = {}
+
+    def _workspace_bytes(self, cache: PagedCache, q_heads: int) -> int:
+        key = (q_heads, cache.kv_heads, cache.head_dim, cache.page_size, self._c.tokens)
+        need = self._need.get(key)
+        if need is None:
+            c = ctypes.c_size_t()
+            _check(lib.gs_paged_attention_workspace(cache._ref, self._ref, q_heads, ctypes.byref(c)),
+                   "gs_paged_attention_workspace")
+            need = self._need[key] = c.value
+        return need
 
 
 def _heads(t: torch.Tensor, D: int, name: str) -> int:
@@ -595,7 +614,7 @@ def paged_attention(q: torch.Tensor, cache: PagedCache, batch: Batch, scale: Opt
             raise ValueError("out must have q's shape")
     batch._c.tokens = q.shape[0]
     sp = _stream_ptr(stream)
-    ws = cache._workspace(batch, q.shape[1], stream, sp)
+    ws = _attention_workspace(batch._workspace_bytes(cache, q.shape[1]), q.device, stream, sp)
     _check(lib.gs_paged_attention(cache._ref, batch._ref, q.data_ptr(), qs, q.shape[1],
                                   D ** -0.5 if scale is None else scale, out.data_ptr(), ws.data_ptr(), ws.numel(), sp),
            "gs_paged_attention")
@@ -613,7 +632,10 @@ def debug_inject_wait(algo: int, limit_ns: int) -> None:
 
 
 def device_status(stream: Optional[torch.cuda.Stream] = None) -> int:
-    return int(lib.gs_device_status(_stream_ptr(stream)))
+    status = int(lib.gs_device_status(_stream_ptr(stream)))
+    if status == GS_ERR_DEVICE_TIMEOUT:
+        _attention_ws.clear()      # counters of a kernel that gave up are not zero
+    return status
 
 
 def launch_count() -> int:
