@@ -77,21 +77,43 @@ __device__ __forceinline__ float ex2(float x) {
   return y;
 }
 
+// A bounded wait for barriers that complete within a microsecond or two: the clock and the
+// abort flag are only looked at after many tries (a try itself waits for a while).
+__device__ __forceinline__ bool mbar_wait_short(uint64_t* bar, uint32_t parity, volatile int* abort_flag, int* err,
+                                                uint64_t limit_ns) {
+#pragma unroll 1
+  for (int i = 0; i < 64; ++i)
+    if (sm100::mbar_try_wait(bar, parity)) return true;
+  const uint64_t t0 = sm100::globaltimer_ns();
+  while (true) {
+#pragma unroll 1
+    for (int i = 0; i < 64; ++i)
+      if (sm100::mbar_try_wait(bar, parity)) return true;
+    if (*abort_flag) return false;
+    if (sm100::globaltimer_ns() - t0 > limit_ns) {
+      *abort_flag = 1;
+      atomicExch(err, kDevErrTimeout);
+      return false;
+    }
+  }
+}
+
 // Units are counted in 32 bits (the host refuses steps that could have more).  Traits:
 //   row_tiles(s, P)   tiles of rows of a sequence (0: not this kernel's)
 //   tiles(s, P, rt)   units of row tile rt, at least 1
 //   kLeast, kSnap     the least units worth a CTA; boundaries this close to an item's end move there
+//   kOver             what an item costs beside its units, in units: they lie before its first one and hold no work
 template <class Traits>
 __device__ __forceinline__ int head_units(const AttnParams& P, const SeqInfo& s) {
   const int nr = Traits::row_tiles(s, P);
   int u = 0;
-  for (int i = 0; i < nr; ++i) u += Traits::tiles(s, P, i);
+  for (int i = 0; i < nr; ++i) u += Traits::tiles(s, P, i) + Traits::kOver;
   return u;
 }
 
 // An item of a sequence: a key head and a row tile
 struct Item {
-  int h, rt, nt;       // nt: its units
+  int h, rt, nt;       // nt: its units, kOver among them
   int first;           // its first unit, from the sequence's first
 };
 // the item that holds unit `off` of the sequence
@@ -102,7 +124,7 @@ __device__ __forceinline__ Item item_at(const AttnParams& P, const SeqInfo& s, i
   it.first = it.h * per_head;
   const int nr = Traits::row_tiles(s, P);
   for (it.rt = 0; it.rt < nr; ++it.rt) {
-    it.nt = Traits::tiles(s, P, it.rt);
+    it.nt = Traits::tiles(s, P, it.rt) + Traits::kOver;
     if (off < it.first + it.nt) break;
     it.first += it.nt;
   }
@@ -208,9 +230,9 @@ __device__ __forceinline__ Shares divide_work(const AttnParams& P, int cta, Work
       const int off = sh.cut(min(cta + e, sh.ctas)) - base;
       if (off < 0 || off >= u) continue;
       const Item it = item_at<Traits>(P, mine, off, per_head);
-      const int at = off - it.first <= Traits::kSnap            ? it.first
-                     : it.first + it.nt - off <= Traits::kSnap ? it.first + it.nt
-                                                               : off;
+      const int at = off - it.first <= Traits::kSnap + Traits::kOver ? it.first
+                     : it.first + it.nt - off <= Traits::kSnap      ? it.first + it.nt
+                                                                    : off;
       w.slot[e] = WorkSlot{base + at, base, r, per_head, mine};
     }
     __syncthreads();
@@ -222,9 +244,9 @@ __device__ __forceinline__ Shares divide_work(const AttnParams& P, int cta, Work
 // A stretch of one item's units in a CTA.
 struct Segment {
   SeqInfo s;
-  Item it;
+  int h, rt;           // key head, row tile
   int r;
-  int ta, tb;          // its units [ta, tb) of the item's nt
+  int ta, tb;          // the item's units [ta, tb)
   int parts, part;     // parts of the item, and which one this is
   int first_cta;       // the CTA of part 0
 };
@@ -254,21 +276,23 @@ struct Walker {
     }
     g.s = s;
     g.r = r;
-    g.it = item_at<Traits>(P, s, pos - base, per_head);
-    const int first = base + g.it.first, last = first + g.it.nt;
-    g.ta = pos - first;
-    g.tb = min(last, end) - first;
-    pos = first + g.tb;
+    const Item it = item_at<Traits>(P, s, pos - base, per_head);
+    g.h = it.h;
+    g.rt = it.rt;
+    const int first = base + it.first, last = first + it.nt, stop = min(last, end);
+    g.ta = max(0, pos - first - Traits::kOver);
+    g.tb = stop - first - Traits::kOver;
     g.parts = 1;
     g.part = 0;
     g.first_cta = cta;
-    if (g.tb - g.ta != g.it.nt) {
+    if (pos != first || stop != last) {
       // the boundaries inside the item that were not moved to its ends
-      const int c_lo = sh.first_cut(first + Traits::kSnap + 1), c_hi = sh.first_cut(last - Traits::kSnap) - 1;
+      const int c_lo = sh.first_cut(first + Traits::kSnap + Traits::kOver + 1), c_hi = sh.first_cut(last - Traits::kSnap) - 1;
       g.first_cta = c_lo - 1;
       g.parts = c_hi - c_lo + 2;
       g.part = cta - g.first_cta;
     }
+    pos = stop;
     return true;
   }
 };

@@ -3,39 +3,40 @@
 //
 // Bound by the tensor cores (4 head_dim FLOP a visible pair) and by the exponentials
 // beside them.  An item is 256 rows of a key head against its visible keys, a unit
-// 128 keys.  The rows are two halves of 128, one per softmax warpgroup, whose thread
+// 64 keys.  The rows are two halves of 128, one per softmax warpgroup, whose thread
 // i owns row i, so that maxima and sums need no exchange.  Per half and unit:
 //     S = Q K^T (tcgen05, both operands in shared memory, S in TMEM), the thread
 //     reads its row of S, writes P = exp2(c S - m) over it as bf16, and
 //     O += P V (A = P in TMEM, B = V as stored, i.e. MN-major), O stays in TMEM.
-// The halves take the tensor cores in turn: one's products run under the other's
-// exponentials.  O is rescaled only when a row's maximum grew by more than 2^8
-// (each row for itself), else the old maximum stays in use: exact, since both the
-// sum and O carry it.
+// Each half has two S, so that the next unit's S is there when the softmax comes to
+// it; the MMA warp issues whatever is ready, of either half.  (Units of 128 keys
+// leave room for one S a half, which then waits for P V: twice the time.)  O is
+// rescaled only when a row's maximum grew by more than 2^8 (each row for itself),
+// else the old maximum stays in use: exact, since both the sum and O carry it.
 //
-// Keys and values arrive page by page (TMA) in one ring of five 32 KB slots.  Values
+// Keys and values arrive page by page (TMA) in rings of five 16 KB slots each.  Values
 // of a unit that some row does not see are looked over first: rows past the sequence's
 // end become zeros, and infinities and NaN are taken out (a weight of zero would not
 // silence them) and added at the end to the rows that see them.
 //
-// TMEM: S of the halves at columns 0 and 128, O at 256 and 384.
+// TMEM: S of the halves at columns 0, 64 and 128, 192, O at 256 and 384.
 #include "gs_attn.cuh"
 
 namespace gs {
 namespace {
 using namespace sm100;
 
-constexpr int kCT = 128;                       // keys of a unit
+constexpr int kCT = 64;                        // keys of a unit
 constexpr int kHalf = 128, kRowsItem = 256;
 constexpr int kAcThreads = 384;                // warps: keys, MMA, values, value check, then two softmax warpgroups
-constexpr int kRing = 5;
+constexpr int kRing = 5;                       // slots of keys, and as many of values
 constexpr int kSegs = 4;
 constexpr uint64_t kAcWaitLimitNs = 2000000000ull;
 constexpr int kRegsOther = 72, kRegsSoftmax = 216;
 static_assert(4 * 32 * kRegsOther + 8 * 32 * kRegsSoftmax <= kAcThreads * 168, "register split");
 
 struct ChunkTraits {
-  static constexpr int kLeast = 4, kSnap = 2;
+  static constexpr int kLeast = 8, kSnap = 3, kOver = 2;
   static __device__ __forceinline__ int row_tiles(const SeqInfo& s, const AttnParams& P) {
     return s.rows >= P.min_rows && s.rows <= P.max_rows ? (s.rows + kRowsItem - 1) / kRowsItem : 0;
   }
@@ -52,7 +53,7 @@ template <int D>
 struct ChunkCfg {
   static constexpr int kOpBytes = kCT * D * 2;         // a unit's keys or values
   static constexpr int kQBytes = kHalf * D * 2;        // a half's queries
-  static constexpr int kSmem = 2 * kQBytes + kRing * kOpBytes + 1024;
+  static constexpr int kSmem = 2 * kQBytes + 2 * kRing * kOpBytes + 1024;
   static constexpr int kSlabs = D / 64;
 };
 
@@ -86,26 +87,52 @@ __device__ __forceinline__ uint64_t sdesc_v(uint32_t saddr, uint32_t block) {
   d |= (uint64_t)2 << 61;
   return d;
 }
+__device__ __forceinline__ bool mbar_test_wait(uint64_t* bar, uint32_t parity) {   // does not suspend
+  uint32_t ok;
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+      "selp.u32 %0, 1, 0, p;\n\t}"
+      : "=r"(ok)
+      : "r"(smem_u32(bar)), "r"(parity)
+      : "memory");
+  return ok != 0;
+}
 __device__ __forceinline__ float max3(float a, float b, float c) { return fmaxf(fmaxf(a, b), c); }
 __device__ __forceinline__ uint32_t nonfinite2(uint32_t v) {   // bits of the halves that are an infinity or NaN
   const uint32_t e = v & 0x7F807F80u;
   return ((e & 0xFFFFu) == 0x7F80u ? 0xFFFFu : 0u) | ((e >> 16) == 0x7F80u ? 0xFFFF0000u : 0u);
 }
 
+// two float32 at once
+__device__ __forceinline__ uint64_t pair(uint32_t lo, uint32_t hi) {
+  uint64_t r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "r"(lo), "r"(hi));
+  return r;
+}
+__device__ __forceinline__ void unpair(uint64_t v, uint32_t& lo, uint32_t& hi) { asm("mov.b64 {%0, %1}, %2;" : "=r"(lo), "=r"(hi) : "l"(v)); }
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+  uint64_t d;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
+  return d;
+}
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
+  uint64_t d;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+  return d;
+}
+
 template <int D>
 __global__ void __launch_bounds__(kAcThreads, 1) k_attn_chunk(const __grid_constant__ AttnParams P) {
   using C = ChunkCfg<D>;
   extern __shared__ uint8_t ac_smem_raw[];
-  // A slot holds keys and values in turn (the ring is odd).  Whoever waits for one kind may be ahead of the other, so
-  // each kind has its own barriers; they move once per use by that kind, every second turn of the ring.
-  __shared__ __align__(8) uint64_t kfull_bar[kRing], vfull_bar[kRing];   // bytes have landed
-  __shared__ __align__(8) uint64_t clean_bar[kRing];                     // values looked over
-  __shared__ __align__(8) uint64_t empty_bar[kRing];                     // moves with every use
-  __shared__ __align__(8) uint64_t seg_full[kSegs];
-  __shared__ __align__(8) uint64_t seg_empty[kSegs];
+  __shared__ __align__(8) uint64_t kfull_bar[kRing], kempty_bar[kRing];   // keys: bytes have landed, slot is free
+  __shared__ __align__(8) uint64_t vfull_bar[kRing], vempty_bar[kRing];   // values
+  __shared__ __align__(8) uint64_t clean_bar[kRing];                      // values looked over
+  __shared__ __align__(8) uint64_t seg_full[kSegs], seg_empty[kSegs];
   __shared__ __align__(8) uint64_t q_bar[2];           // a half's queries are in shared memory
-  __shared__ __align__(8) uint64_t s_bar[2];           // S is in TMEM
-  __shared__ __align__(8) uint64_t p_bar[2];           // P is in TMEM, O is rescaled
+  __shared__ __align__(8) uint64_t s_bar[2][2];        // [half][buffer]: S is in TMEM
+  __shared__ __align__(8) uint64_t p_bar[2][2];        // P is in TMEM, O is rescaled
   __shared__ __align__(8) uint64_t o_bar[2];           // P V is done
   __shared__ __align__(8) uint64_t join_bar[2];
   __shared__ __align__(8) uint64_t drain_bar;
@@ -114,14 +141,16 @@ __global__ void __launch_bounds__(kAcThreads, 1) k_attn_chunk(const __grid_const
   __shared__ uint32_t tmem_base_s;
   __shared__ int abort_s, bad_s[kSegs], last_s[2];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(ac_smem_raw) + 1023) & ~uintptr_t(1023));
-  uint8_t* ring = smem + 2 * C::kQBytes;
+  uint8_t* ring_k = smem + 2 * C::kQBytes;
+  uint8_t* ring_v = ring_k + kRing * C::kOpBytes;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int cta = (int)blockIdx.x;
   if (threadIdx.x == 0) {
     for (int s = 0; s < kRing; ++s) {
       mbar_init(&kfull_bar[s], 1);
+      mbar_init(&kempty_bar[s], 1);
       mbar_init(&vfull_bar[s], 1);
-      mbar_init(&empty_bar[s], 1);
+      mbar_init(&vempty_bar[s], 1);
       mbar_init(&clean_bar[s], 1);
     }
     for (int s = 0; s < kSegs; ++s) {
@@ -130,8 +159,10 @@ __global__ void __launch_bounds__(kAcThreads, 1) k_attn_chunk(const __grid_const
     }
     for (int h = 0; h < 2; ++h) {
       mbar_init(&q_bar[h], 4);
-      mbar_init(&s_bar[h], 1);
-      mbar_init(&p_bar[h], 4);
+      for (int b = 0; b < 2; ++b) {
+        mbar_init(&s_bar[h][b], 1);
+        mbar_init(&p_bar[h][b], 4);
+      }
       mbar_init(&o_bar[h], 1);
       mbar_init(&join_bar[h], 4);
     }
@@ -151,15 +182,13 @@ __global__ void __launch_bounds__(kAcThreads, 1) k_attn_chunk(const __grid_const
   tc_fence_after();
   const uint32_t tmem = tmem_base_s;
   volatile int* abort_flag = &abort_s;
-  const int box_shift = min(P.page_shift, 7), box = 1 << box_shift;   // rows of a TMA box
+  const int box_shift = min(P.page_shift, 6), box = 1 << box_shift;   // rows of a TMA box
   const auto wait_warp = [&](uint64_t* bar, uint32_t parity) {
-    return __all_sync(0xffffffffu, mbar_wait_bounded(bar, parity, abort_flag, P.err, kAcWaitLimitNs, kDevErrTimeout)) != 0;
+    return __all_sync(0xffffffffu, mbar_wait_short(bar, parity, abort_flag, P.err, kAcWaitLimitNs)) != 0;
   };
   // A half's units end where its last row's keys end.
-  const auto half_units = [&](const Segment& g, int h) {
-    return ChunkTraits::units_of(g.s, P, g.it.rt * kRowsItem + (h + 1) * kHalf);
-  };
-  const auto halves = [&](const Segment& g) { return g.s.rows - g.it.rt * kRowsItem > kHalf ? 2 : 1; };
+  const auto half_end = [&](const Segment& g, int h) { return min(g.tb, ChunkTraits::units_of(g.s, P, g.rt * kRowsItem + (h + 1) * kHalf)); };
+  const auto halves = [&](const Segment& g) { return g.s.rows - g.rt * kRowsItem > kHalf ? 2 : 1; };
 
   if (warp < 4) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsOther));
@@ -178,7 +207,10 @@ __global__ void __launch_bounds__(kAcThreads, 1) k_attn_chunk(const __grid_const
       Walker<ChunkTraits> walk(P, shares, work, cta);
       Segment g;
       const int32_t no_row = (int32_t)((P.pages * P.kv_heads) << P.page_shift);   // past the last: reads as zeros
-      uint32_t slot = keys ? 0 : 1, ph = 1u;
+      uint64_t* full_bar = keys ? kfull_bar : vfull_bar;
+      uint64_t* empty_bar = keys ? kempty_bar : vempty_bar;
+      uint8_t* ring = keys ? ring_k : ring_v;
+      uint32_t slot = 0, ph = 1u;
       bool ok = true;
       while (ok) {
         if (keys) {
@@ -206,27 +238,27 @@ __global__ void __launch_bounds__(kAcThreads, 1) k_attn_chunk(const __grid_const
         int held = -1, page = -1;   // lane i holds table entry 32 held + i
         for (int t = g.ta; t < g.tb; ++t) {
           const int valid = min(kCT, max(0, len - t * kCT));
-          const int boxes = (valid + box - 1) >> box_shift;   // at most 8
+          const int boxes = (valid + box - 1) >> box_shift;   // at most 4
           const int e0 = (t * kCT) >> P.page_shift;
           if (e0 >> 5 != held) {
             held = e0 >> 5;
             const int e = 32 * held + lane;
             page = e < P.width && ((int64_t)e << P.page_shift) < len ? __ldg(P.table + trow + e) : -1;
           }
-          const int key = t * kCT + ((lane & 7) << box_shift);
+          const int key = t * kCT + ((lane & 3) << box_shift);
           const int pg = __shfl_sync(0xffffffffu, page, (key >> P.page_shift) & 31);
           const int32_t row = pg >= 0 && pg < P.pages
-                                  ? (int32_t)((((int64_t)pg * P.kv_heads + g.it.h) << P.page_shift) + (key & ((1 << P.page_shift) - 1)))
+                                  ? (int32_t)((((int64_t)pg * P.kv_heads + g.h) << P.page_shift) + (key & ((1 << P.page_shift) - 1)))
                                   : no_row;
           if (!wait_warp(&empty_bar[slot], ph)) {
             ok = false;
             break;
           }
           uint8_t* dst = ring + slot * C::kOpBytes;
-          uint64_t* full = keys ? &kfull_bar[slot] : &vfull_bar[slot];
+          uint64_t* full = &full_bar[slot];
           if (elect_one()) mbar_arrive_expect_tx(full, (uint32_t)(boxes * box * D * 2));
           __syncwarp();
-          // Keys: slabs of 64 channels x 128 keys.  Values: box after box, each with its slabs.
+          // Keys: slabs of 64 channels x 64 keys.  Values: box after box, each with its slabs.
           for (int b = 0; b < boxes; ++b) {
             const int32_t r = __shfl_sync(0xffffffffu, row, b);
             if (elect_one()) {
@@ -236,15 +268,13 @@ __global__ void __launch_bounds__(kAcThreads, 1) k_attn_chunk(const __grid_const
                 tma_load_3d(dst, &P.kmap, full, 0, r, 0);
               } else {
 #pragma unroll
-                for (int sl = 0; sl < C::kSlabs; ++sl)
-                  tma_load_3d(dst + sl * (kCT * 128) + b * (box * 128), &P.kmap, full, 0, r, sl);
+                for (int sl = 0; sl < C::kSlabs; ++sl) tma_load_3d(dst + sl * (kCT * 128) + b * (box * 128), &P.kmap, full, 0, r, sl);
               }
             }
             __syncwarp();
           }
-          slot += 2;
-          if (slot >= kRing) {
-            slot -= kRing;
+          if (++slot == kRing) {
+            slot = 0;
             ph ^= 1u;
           }
         }
@@ -253,95 +283,106 @@ __global__ void __launch_bounds__(kAcThreads, 1) k_attn_chunk(const __grid_const
       // ---------------------------------------------------------- MMA issuer
       const uint32_t idesc_s = idesc_bf16_f32(kHalf, kCT);
       const uint32_t idesc_o = idesc_bf16_f32(kHalf, D) | (1u << 16);   // bit 16: B is MN-major
-      uint32_t ks = 0, kturn = 0u, vs = 1, vturn = 0u;   // slots, and turns of the ring
-      uint32_t qph[2] = {0u, 0u}, pph[2] = {0u, 0u}, oph[2] = {0u, 0u};
       const uint32_t vblock = (uint32_t)box * 128u;
+      const auto test_warp = [&](uint64_t* bar, uint32_t parity) { return __all_sync(0xffffffffu, mbar_test_wait(bar, parity)) != 0; };
+      // Per half, counted over all segments: products of S and of P V issued, and P V known to be over.  The n-th S goes to
+      // buffer n & 1, where the (n - 2)-th P was read.  The slots of keys and values follow from the units of the segments
+      // before (used) and the unit.
+      uint32_t ns[2] = {0u, 0u}, no[2] = {0u, 0u}, over[2] = {0u, 0u}, qph[2] = {0u, 0u};
+      uint32_t used = 0;
       bool ok = true;
-      // S of half h against the keys in slot k
-      const auto issue_s = [&](int h, uint32_t k, bool last) {
-        if (elect_one()) {
-          const uint64_t a = sdesc_sw128(smem_u32(smem + h * C::kQBytes)), b = sdesc_sw128(smem_u32(ring + k * C::kOpBytes));
-#pragma unroll
-          for (int kk = 0; kk < D / 16; ++kk) {
-            const uint64_t off = (uint64_t)(((kk >> 2) * (kHalf * 128) + (kk & 3) * 32) >> 4);
-            mma_bf16_ss(tmem + h * 128, a + off, b + off, idesc_s, kk == 0 ? 0u : 1u);
-          }
-          mma_commit(&s_bar[h]);
-          if (last) mma_commit(&empty_bar[k]);
-        }
-        __syncwarp();
-      };
-      static_assert(kHalf == kCT, "one slab size for queries and keys");
       while (ok) {
         if (!wait_warp(&seg_full[sg], sph)) break;
         const Segment g = segs[sg];
         next_seg();
         if (g.r < 0) break;
-        const int nh = halves(g);
-        int end[2];   // units [ta, end) of a half; the last half has them all
-        for (int h = 0; h < 2; ++h) end[h] = h < nh ? min(g.tb, half_units(g, h)) : 0;
-        if (!wait_warp(&kfull_bar[ks], (kturn >> 1) & 1u)) break;
-        for (int h = 0; h < nh && ok; ++h) {
-          if (g.ta >= end[h]) continue;
-          ok = wait_warp(&q_bar[h], qph[h]);
-          qph[h] ^= 1u;
-          tc_fence_after();
-          if (ok) issue_s(h, ks, h == nh - 1);
-        }
-        for (int t = g.ta; t < g.tb && ok; ++t) {
-          uint32_t kn = ks + 2, kn_turn = kturn;   // the next unit's keys
-          if (kn >= kRing) {
-            kn -= kRing;
-            ++kn_turn;
-          }
-          if (!wait_warp(&clean_bar[vs], (vturn >> 1) & 1u)) {
-            ok = false;
-            break;
-          }
-          if (t + 1 < g.tb && !wait_warp(&kfull_bar[kn], (kn_turn >> 1) & 1u)) {
-            ok = false;
-            break;
-          }
-          for (int h = 0; h < nh; ++h) {
-            if (t >= end[h]) continue;
-            if (!wait_warp(&p_bar[h], pph[h])) {
-              ok = false;
-              break;
-            }
-            pph[h] ^= 1u;
-            tc_fence_after();
-            if (elect_one()) {
-              const uint32_t v = smem_u32(ring + vs * C::kOpBytes);
+        const int n_units = g.tb - g.ta, nh = halves(g);
+        int units[2];   // of a half; the last half has them all
+        units[0] = max(0, half_end(g, 0) - g.ta);
+        units[1] = nh > 1 ? n_units : 0;
+        if (nh == 1) units[0] = n_units;
+        int us[2] = {0, 0}, uo[2] = {0, 0};   // the next unit's S, P V
+        bool have_q[2] = {false, false};
+        uint32_t ks[2], kp[2], vs[2], vp[2];
 #pragma unroll
-              for (int kk = 0; kk < kCT / 16; ++kk) {
-                const int key = 16 * kk;
-                const uint32_t off = (uint32_t)(key >> box_shift) * (vblock * C::kSlabs) + (uint32_t)(key & (box - 1)) * 128u;
-                mma_bf16_ts(tmem + 256 + h * 128, tmem + h * 128 + 8 * kk, sdesc_v(v + off, vblock), idesc_o,
-                            t == g.ta && kk == 0 ? 0u : 1u);
+        for (int h = 0; h < 2; ++h) {
+          ks[h] = vs[h] = used % kRing;
+          kp[h] = vp[h] = (used / kRing) & 1u;
+        }
+        uint64_t t0 = 0;
+        uint32_t idle = 0;
+        while (ok && (uo[0] < units[0] || uo[1] < units[1])) {
+          bool did = false;
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            if (over[h] != no[h] && test_warp(&o_bar[h], over[h] & 1u)) ++over[h];
+            // P V of the oldest unit, once P and the values are there; the one before is over (one at a time in flight)
+            if (uo[h] < us[h] && over[h] == no[h] && test_warp(&p_bar[h][no[h] & 1u], (no[h] >> 1) & 1u) &&
+                test_warp(&clean_bar[vs[h]], vp[h])) {
+              tc_fence_after();
+              if (elect_one()) {
+                const uint32_t v = smem_u32(ring_v + vs[h] * C::kOpBytes), p = tmem + h * 128 + (no[h] & 1u) * kCT;
+#pragma unroll
+                for (int kk = 0; kk < kCT / 16; ++kk) {
+                  const int key = 16 * kk;
+                  const uint32_t off = (uint32_t)(key >> box_shift) * (vblock * C::kSlabs) + (uint32_t)(key & (box - 1)) * 128u;
+                  mma_bf16_ts(tmem + 256 + h * 128, p + 8 * kk, sdesc_v(v + off, vblock), idesc_o, uo[h] == 0 && kk == 0 ? 0u : 1u);
+                }
+                mma_commit(&o_bar[h]);
+                // a slot goes back with the second of the halves that use it
+                if (uo[h] >= units[h ^ 1] || uo[h ^ 1] > uo[h]) mma_commit(&vempty_bar[vs[h]]);
               }
-              mma_commit(&o_bar[h]);
-              if (h == nh - 1) mma_commit(&empty_bar[vs]);
+              __syncwarp();
+              ++no[h];
+              ++uo[h];
+              if (++vs[h] == kRing) {
+                vs[h] = 0;
+                vp[h] ^= 1u;
+              }
+              did = true;
             }
-            __syncwarp();
-            if (t + 1 < end[h]) {
-              // S goes where P is being read: not before that product is over
-              if (!wait_warp(&o_bar[h], oph[h])) {
-                ok = false;
-                break;
+            // S of the next unit: its buffer is free once the P before last has been read
+            if (us[h] < units[h] && ns[h] <= over[h] + 1u && test_warp(&kfull_bar[ks[h]], kp[h])) {
+              if (!have_q[h]) {
+                if (!test_warp(&q_bar[h], qph[h])) continue;
+                have_q[h] = true;
+                qph[h] ^= 1u;
               }
               tc_fence_after();
-              issue_s(h, kn, h == nh - 1);
+              if (elect_one()) {
+                const uint64_t a = sdesc_sw128(smem_u32(smem + h * C::kQBytes)), b = sdesc_sw128(smem_u32(ring_k + ks[h] * C::kOpBytes));
+#pragma unroll
+                for (int kk = 0; kk < D / 16; ++kk)
+                  mma_bf16_ss(tmem + h * 128 + (ns[h] & 1u) * kCT, a + (uint64_t)(((kk >> 2) * (kHalf * 128) + (kk & 3) * 32) >> 4),
+                              b + (uint64_t)(((kk >> 2) * (kCT * 128) + (kk & 3) * 32) >> 4), idesc_s, kk == 0 ? 0u : 1u);
+                mma_commit(&s_bar[h][ns[h] & 1u]);
+                if (us[h] >= units[h ^ 1] || us[h ^ 1] > us[h]) mma_commit(&kempty_bar[ks[h]]);
+              }
+              __syncwarp();
+              ++ns[h];
+              ++us[h];
+              if (++ks[h] == kRing) {
+                ks[h] = 0;
+                kp[h] ^= 1u;
+              }
+              did = true;
             }
-            oph[h] ^= 1u;
           }
-          ks = kn;
-          kturn = kn_turn;
-          vs += 2;
-          if (vs >= kRing) {
-            vs -= kRing;
-            ++vturn;
+          if (did) {
+            idle = 0;
+          } else if ((++idle & 1023u) == 0) {   // bounded, like every wait
+            const uint64_t now = globaltimer_ns();
+            if (idle == 1024u) t0 = now;
+            if (*abort_flag) ok = false;
+            if (now - t0 > kAcWaitLimitNs) {
+              *abort_flag = 1;
+              atomicExch(P.err, kDevErrTimeout);
+              ok = false;
+            }
+            ok = __all_sync(0xffffffffu, ok);
           }
         }
+        used += (uint32_t)n_units;
       }
       // whatever was issued is over before TMEM goes back
       if (elect_one()) {
@@ -351,44 +392,53 @@ __global__ void __launch_bounds__(kAcThreads, 1) k_attn_chunk(const __grid_const
       __syncwarp();
     } else {
       // ---------------------------------------------------------- values that some row does not see
-      uint32_t vs = 1, vturn = 0u;
+      uint32_t vs = 0, vph = 0u;
       bool ok = true;
       while (ok) {
         if (!wait_warp(&seg_full[sg], sph)) break;
         const Segment g = segs[sg];
         const uint32_t at = sg;
         if (g.r >= 0 && lane == 0) bad_s[at] = 0;
-        __syncwarp();
         next_seg();
         if (g.r < 0) break;
-        const int len = g.s.len(), all_see = g.s.seen(g.it.rt * kRowsItem / P.group);
+        const int len = g.s.len(), all_see = g.s.seen(g.rt * kRowsItem / P.group);
         for (int t = g.ta; t < g.tb; ++t) {
-          if (!wait_warp(&vfull_bar[vs], (vturn >> 1) & 1u)) {
+          if (!wait_warp(&vfull_bar[vs], vph)) {
             ok = false;
             break;
           }
           const int key0 = t * kCT;
           if (key0 + kCT > all_see) {
-            uint8_t* v = ring + vs * C::kOpBytes;
-            // a key's row is kSlabs pieces of 128 bytes; their swizzle does not matter here
-            const auto piece = [&](int k, int i) {   // 16-byte piece i of key k of the unit
-              return reinterpret_cast<uint4*>(v + (((k >> box_shift) * C::kSlabs + (i >> 3)) << box_shift) * 128 +
-                                              (k & (box - 1)) * 128 + (i & 7) * 16);
-            };
-            constexpr int kPieces = D / 8, kStep = 32 / kPieces;   // keys of a step of the warp
-            const int end = min(kCT, max(0, len - key0));
+            const uint32_t v = smem_u32(ring_v + vs * C::kOpBytes);
+            constexpr int kPieces = D / 8, kStep = 32 / kPieces, kDeep = 8;   // keys of a step of the warp; steps at once
+            const int end = min(kCT, max(0, len - key0)), piece = lane % kPieces;
             bool bad = false;
-            for (int k = max(0, all_see - key0) + lane / kPieces; k < kCT; k += kStep) {
-              uint4* p = piece(k, lane % kPieces);
-              if (k >= end) {
-                *p = make_uint4(0u, 0u, 0u, 0u);
-              } else {
-                uint4 x = *p;
-                const uint4 n = make_uint4(nonfinite2(x.x), nonfinite2(x.y), nonfinite2(x.z), nonfinite2(x.w));
-                if (n.x | n.y | n.z | n.w) {
-                  *p = make_uint4(x.x & ~n.x, x.y & ~n.y, x.z & ~n.z, x.w & ~n.w);
-                  bad = true;
-                }
+            for (int k0 = max(0, all_see - key0); k0 < kCT; k0 += kDeep * kStep) {
+              uint4 x[kDeep];
+              uint32_t at16[kDeep];
+#pragma unroll
+              for (int i = 0; i < kDeep; ++i) {
+                // a key's row is kSlabs pieces of 128 bytes; their swizzle does not matter here
+                const int k = k0 + i * kStep + lane / kPieces;
+                at16[i] = v + (uint32_t)((((k >> box_shift) * C::kSlabs + (piece >> 3)) << box_shift) * 128 + (k & (box - 1)) * 128 +
+                                         (piece & 7) * 16);
+                x[i] = make_uint4(0u, 0u, 0u, 0u);
+                if (k < end)
+                  asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];"
+                               : "=r"(x[i].x), "=r"(x[i].y), "=r"(x[i].z), "=r"(x[i].w)
+                               : "r"(at16[i])
+                               : "memory");
+              }
+#pragma unroll
+              for (int i = 0; i < kDeep; ++i) {
+                const int k = k0 + i * kStep + lane / kPieces;
+                const uint4 n = make_uint4(nonfinite2(x[i].x), nonfinite2(x[i].y), nonfinite2(x[i].z), nonfinite2(x[i].w));
+                const bool hit = (n.x | n.y | n.z | n.w) != 0u;
+                if (k < kCT && (hit || k >= end))
+                  asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(at16[i]), "r"(x[i].x & ~n.x), "r"(x[i].y & ~n.y),
+                               "r"(x[i].z & ~n.z), "r"(x[i].w & ~n.w)
+                               : "memory");
+                bad |= hit;
               }
             }
             if (bad) bad_s[at] = 1;
@@ -396,10 +446,9 @@ __global__ void __launch_bounds__(kAcThreads, 1) k_attn_chunk(const __grid_const
           }
           __syncwarp();
           if (lane == 0) mbar_arrive(&clean_bar[vs]);
-          vs += 2;
-          if (vs >= kRing) {
-            vs -= kRing;
-            ++vturn;
+          if (++vs == kRing) {
+            vs = 0;
+            vph ^= 1u;
           }
         }
       }
@@ -409,9 +458,9 @@ __global__ void __launch_bounds__(kAcThreads, 1) k_attn_chunk(const __grid_const
     // ------------------------------------------------------------ softmax: a row a thread
     asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegsSoftmax));
     const int h = (warp - 4) >> 2, quarter = warp & 3;
-    const uint32_t ts = tmem + h * 128 + ((uint32_t)(32 * quarter) << 16);
-    const uint32_t to = tmem + 256 + h * 128 + ((uint32_t)(32 * quarter) << 16);
-    uint32_t sg = 0, sph = 0, s_ph = 0u, o_ph = 0u, j_ph = 0u;
+    const uint32_t lane_base = (uint32_t)(32 * quarter) << 16;
+    const uint32_t ts = tmem + h * 128 + lane_base, to = tmem + 256 + h * 128 + lane_base;
+    uint32_t sg = 0, sph = 0, n = 0, j_ph = 0u;   // n: units so far
     const auto meet = [&]() {   // the warpgroup's barrier, bounded like every wait
       __syncwarp();
       if (lane == 0) mbar_arrive(&join_bar[h]);
@@ -420,86 +469,102 @@ __global__ void __launch_bounds__(kAcThreads, 1) k_attn_chunk(const __grid_const
       return met;
     };
     const float c = P.scale_log2;
-    bool ok = true;
-    while (ok) {
-      if (!wait_warp(&seg_full[sg], sph)) break;
-      const Segment g = segs[sg];
-      const uint32_t at = sg;
-      if (++sg == kSegs) {
-        sg = 0;
-        sph ^= 1u;
-      }
-      const auto seg_done = [&]() {
+    const uint64_t c2 = pair(__float_as_uint(c), __float_as_uint(c));
+    // this half's next segment and its slot; false: no more, or some role gave up
+    const auto next_segment = [&](Segment& g, uint32_t& at) {
+      while (true) {
+        if (!wait_warp(&seg_full[sg], sph)) return false;
+        g = segs[sg];
+        at = sg;
+        if (++sg == kSegs) {
+          sg = 0;
+          sph ^= 1u;
+        }
+        if (g.r < 0) return false;
+        if (h < halves(g)) return true;
         __syncwarp();
         if (lane == 0) mbar_arrive(&seg_empty[at]);
-      };
-      if (g.r < 0) break;
-      if (h >= halves(g)) {
-        seg_done();
-        continue;
       }
-      const int row_h = g.it.rt * kRowsItem + h * kHalf;        // the half's first row
-      const int end = min(g.tb, half_units(g, h));
-      const int row = row_h + 32 * quarter + lane;              // this thread's
-      const bool row_on = row < g.s.rows;
-      const int tok = row_on ? row / P.group : 0, hd = row_on ? row - tok * P.group : 0;
-      const int vis = row_on ? g.s.seen(tok) : 0;
-      const int all_see = g.s.seen(row_h / P.group);
+    };
+    // this thread's row of a segment
+    struct Row {
+      int tok, hd, vis;
+      bool on;
+    };
+    const auto row_of = [&](const Segment& g) {
+      const int row = g.rt * kRowsItem + h * kHalf + 32 * quarter + lane;
+      Row r;
+      r.on = row < g.s.rows;
+      r.tok = r.on ? row / P.group : 0;
+      r.hd = r.on ? row - r.tok * P.group : 0;
+      r.vis = r.on ? g.s.seen(r.tok) : 0;
+      return r;
+    };
+    // the warp's 32 rows of queries, swizzled as the MMA reads them
+    const auto load_q = [&](const Segment& g, const Row& row) {
+      if (g.ta >= half_end(g, h)) return;
+      constexpr int kPieces = D / 8, kStep = 32 / kPieces;
+      const uint32_t flip = P.negate ? 0x80008000u : 0u;
+      const uint64_t mine = row.on ? (uint64_t)((int64_t)(g.s.tok0 + row.tok) * P.q_stride + (int64_t)(g.h * P.group + row.hd) * D) : ~0ull;
+      uint4 x[32 / kStep];
+#pragma unroll
+      for (int i = 0; i < 32 / kStep; ++i) {
+        const uint64_t at = __shfl_sync(0xffffffffu, mine, i * kStep + lane / kPieces);
+        x[i] = make_uint4(0u, 0u, 0u, 0u);
+        if (at != ~0ull) x[i] = __ldg(reinterpret_cast<const uint4*>(P.q + at) + lane % kPieces);
+      }
+#pragma unroll
+      for (int i = 0; i < 32 / kStep; ++i) {
+        const int r = 32 * quarter + i * kStep + lane / kPieces, p = lane % kPieces;
+        *reinterpret_cast<uint4*>(smem + h * C::kQBytes + (p >> 3) * (kHalf * 128) + r * 128 + (((p & 7) ^ (r & 7)) << 4)) =
+            make_uint4(x[i].x ^ flip, x[i].y ^ flip, x[i].z ^ flip, x[i].w ^ flip);
+      }
+      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&q_bar[h]);
+    };
+    Segment g;
+    uint32_t at;
+    bool more = next_segment(g, at);
+    Row row = {0, 0, 0, false};
+    if (more) {
+      row = row_of(g);
+      load_q(g, row);
+    }
+    while (more) {
+      const int end = half_end(g, h);
+      const int all_see = g.s.seen((g.rt * kRowsItem + h * kHalf) / P.group);
       float m = -INFINITY, l = 0.f;
-      if (g.ta < end) {
-        // ---- the warp's 32 rows of queries, swizzled as the MMA reads them
-        constexpr int kPieces = D / 8, kStep = 32 / kPieces;
-        const uint32_t flip = P.negate ? 0x80008000u : 0u;
-        uint4 x[32 / kStep];
-#pragma unroll
-        for (int i = 0; i < 32 / kStep; ++i) {
-          const int r = row_h + 32 * quarter + i * kStep + lane / kPieces;
-          x[i] = make_uint4(0u, 0u, 0u, 0u);
-          if (r < g.s.rows) {
-            const int tk = r / P.group, hq = r - tk * P.group;
-            x[i] = __ldg(reinterpret_cast<const uint4*>(P.q + (int64_t)(g.s.tok0 + tk) * P.q_stride +
-                                                        (int64_t)(g.it.h * P.group + hq) * D) + lane % kPieces);
-          }
-        }
-#pragma unroll
-        for (int i = 0; i < 32 / kStep; ++i) {
-          const int r = 32 * quarter + i * kStep + lane / kPieces, p = lane % kPieces;
-          *reinterpret_cast<uint4*>(smem + h * C::kQBytes + (p >> 3) * (kHalf * 128) + r * 128 + (((p & 7) ^ (r & 7)) << 4)) =
-              make_uint4(x[i].x ^ flip, x[i].y ^ flip, x[i].z ^ flip, x[i].w ^ flip);
-        }
-        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-        __syncwarp();
-        if (lane == 0) mbar_arrive(&q_bar[h]);
-      }
-      for (int t = g.ta; t < end; ++t) {
-        if (!wait_warp(&s_bar[h], s_ph)) {
+      bool ok = true;
+      for (int t = g.ta; t < end; ++t, ++n) {
+        const uint32_t sb = ts + (n & 1u) * kCT;
+        if (!wait_warp(&s_bar[h][n & 1u], (n >> 1) & 1u)) {
           ok = false;
           break;
         }
-        s_ph ^= 1u;
         tc_fence_after();
-        uint32_t s[4][32];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) tmem_ld_x32(ts + 32 * i, s[i]);
+        uint32_t s[2][32];
+        tmem_ld_x32(sb, s[0]);
+        tmem_ld_x32(sb + 32, s[1]);
         tmem_wait_ld();
-#pragma unroll
-        for (int i = 0; i < 4; ++i) reg_fence(s[i]);
+        reg_fence(s[0]);
+        reg_fence(s[1]);
         const int key0 = t * kCT;
         if (key0 + kCT > all_see) {
-          const int n = vis - key0;
+          const int v = row.vis - key0;
 #pragma unroll
-          for (int i = 0; i < 4; ++i)
+          for (int i = 0; i < 2; ++i)
 #pragma unroll
             for (int e = 0; e < 32; ++e)
-              if (32 * i + e >= n) s[i][e] = 0xFF800000u;   // -inf
+              if (32 * i + e >= v) s[i][e] = 0xFF800000u;   // -inf
         }
         float top[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          top[i] = __uint_as_float(s[i][0]);
+          const uint32_t* q = &s[i >> 1][16 * (i & 1)];
+          top[i] = fmaxf(__uint_as_float(q[0]), __uint_as_float(q[1]));
 #pragma unroll
-          for (int e = 1; e < 31; e += 2) top[i] = max3(top[i], __uint_as_float(s[i][e]), __uint_as_float(s[i][e + 1]));
-          top[i] = fmaxf(top[i], __uint_as_float(s[i][31]));
+          for (int e = 2; e < 16; e += 2) top[i] = max3(top[i], __uint_as_float(q[e]), __uint_as_float(q[e + 1]));
         }
         const float mt = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
         float f = 1.f;
@@ -507,8 +572,16 @@ __global__ void __launch_bounds__(kAcThreads, 1) k_attn_chunk(const __grid_const
           f = ex2((m - mt) * c);
           m = mt;
         }
-        if (t > g.ta && __any_sync(0xffffffffu, f != 1.f)) {
-#pragma unroll
+        // The product before is waited for once a unit (a barrier that moved twice between two waits would look as if it
+        // had not): here if O has to be rescaled, else after the exponentials.
+        const bool rescale = t > g.ta && __any_sync(0xffffffffu, f != 1.f);
+        if (rescale) {
+          if (!wait_warp(&o_bar[h], (n - 1u) & 1u)) {
+            ok = false;
+            break;
+          }
+          tc_fence_after();
+#pragma unroll 1
           for (int i = 0; i < D / 32; ++i) {
             uint32_t o[32];
             tmem_ld_x32(to + 32 * i, o);
@@ -520,58 +593,71 @@ __global__ void __launch_bounds__(kAcThreads, 1) k_attn_chunk(const __grid_const
           }
         }
         const float mc = m == -INFINITY ? 0.f : m * c;
+        const uint64_t mc2 = pair(__float_as_uint(-mc), __float_as_uint(-mc));
+        uint32_t p[32];
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
+        for (int i = 0; i < 2; ++i)
 #pragma unroll
-          for (int e = 0; e < 32; ++e) s[i][e] = __float_as_uint(ex2(fmaf(__uint_as_float(s[i][e]), c, -mc)));
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          uint32_t p[32];
-#pragma unroll
-          for (int e = 0; e < 16; ++e) {
-            p[e] = pack_bf16(__uint_as_float(s[2 * i][2 * e]), __uint_as_float(s[2 * i][2 * e + 1]));
-            p[16 + e] = pack_bf16(__uint_as_float(s[2 * i + 1][2 * e]), __uint_as_float(s[2 * i + 1][2 * e + 1]));
+          for (int e = 0; e < 32; e += 2) {
+            uint32_t a, b;
+            unpair(fma2(pair(s[i][e], s[i][e + 1]), c2, mc2), a, b);
+            s[i][e] = __float_as_uint(ex2(__uint_as_float(a)));
+            s[i][e + 1] = __float_as_uint(ex2(__uint_as_float(b)));
+            p[16 * i + e / 2] = pack_bf16(__uint_as_float(s[i][e]), __uint_as_float(s[i][e + 1]));
           }
-          tmem_st_x32(ts + 32 * i, p);
+        if (t > g.ta && !rescale && !wait_warp(&o_bar[h], (n - 1u) & 1u)) {
+          ok = false;
+          break;
         }
+        tmem_st_x32(sb, p);
         tmem_wait_st();
         tc_fence_before();
         __syncwarp();
-        if (lane == 0) mbar_arrive(&p_bar[h]);
-        float sum[4] = {0.f, 0.f, 0.f, 0.f};
+        if (lane == 0) mbar_arrive(&p_bar[h][n & 1u]);
+        uint64_t sum[4] = {0ull, 0ull, 0ull, 0ull};
 #pragma unroll
         for (int i = 0; i < 4; ++i)
 #pragma unroll
-          for (int e = 0; e < 32; ++e) sum[i] += __uint_as_float(s[i][e]);
-        l = l * f + ((sum[0] + sum[1]) + (sum[2] + sum[3]));
-        if (t + 1 < end) o_ph ^= 1u;   // P V of this unit is over when the next S is there
+          for (int e = 0; e < 16; e += 2) sum[i] = add2(sum[i], pair(s[i >> 1][16 * (i & 1) + e], s[i >> 1][16 * (i & 1) + e + 1]));
+        uint32_t s0, s1;
+        unpair(add2(add2(sum[0], sum[1]), add2(sum[2], sum[3])), s0, s1);
+        l = l * f + (__uint_as_float(s0) + __uint_as_float(s1));
       }
       if (!ok) break;
-      // ---- the segment's result
+      // ---- the next segment's queries: every S of this one has been read
+      Segment g2;
+      uint32_t at2 = 0;
+      const bool more2 = next_segment(g2, at2);
+      Row row2 = {0, 0, 0, false};
+      if (more2) {
+        row2 = row_of(g2);
+        load_q(g2, row2);
+      }
+      // ---- this segment's result
       float o[D];
       if (g.ta < end) {
-        if (!wait_warp(&o_bar[h], o_ph)) break;
-        o_ph ^= 1u;
+        if (!wait_warp(&o_bar[h], (n - 1u) & 1u)) break;
         tc_fence_after();
+        uint32_t v[D / 32][32];
+#pragma unroll
+        for (int i = 0; i < D / 32; ++i) tmem_ld_x32(to + 32 * i, v[i]);
+        tmem_wait_ld();
 #pragma unroll
         for (int i = 0; i < D / 32; ++i) {
-          uint32_t v[32];
-          tmem_ld_x32(to + 32 * i, v);
-          tmem_wait_ld();
-          reg_fence(v);
+          reg_fence(v[i]);
 #pragma unroll
-          for (int e = 0; e < 32; ++e) o[32 * i + e] = __uint_as_float(v[e]);
+          for (int e = 0; e < 32; ++e) o[32 * i + e] = __uint_as_float(v[i][e]);
         }
       } else {
 #pragma unroll
         for (int e = 0; e < D; ++e) o[e] = 0.f;
       }
       if (bad_s[at]) {   // infinities and NaN of keys that only some rows see
-        const int stop = min(g.tb * kCT, vis);
-        for (int key = max(g.s.seen(g.it.rt * kRowsItem / P.group), g.ta * kCT); key < stop; ++key) {
+        const int stop = min(g.tb * kCT, row.vis);
+        for (int key = max(g.s.seen(g.rt * kRowsItem / P.group), g.ta * kCT); key < stop; ++key) {
           const int pg = __ldg(P.table + (int64_t)g.r * P.width + (key >> P.page_shift));
           if (pg < 0 || pg >= P.pages) continue;
-          const uint16_t* vr = P.v + ((((int64_t)pg * P.kv_heads + g.it.h) << P.page_shift) + (key & ((1 << P.page_shift) - 1))) * D;
+          const uint16_t* vr = P.v + ((((int64_t)pg * P.kv_heads + g.h) << P.page_shift) + (key & ((1 << P.page_shift) - 1))) * D;
 #pragma unroll
           for (int e = 0; e < D; ++e) {
             const float x = bf16_lo(__ldg(vr + e));
@@ -579,10 +665,9 @@ __global__ void __launch_bounds__(kAcThreads, 1) k_attn_chunk(const __grid_const
           }
         }
       }
-      seg_done();
-      uint16_t* dst = P.out + ((int64_t)(g.s.tok0 + tok) * P.q_heads + g.it.h * P.group + hd) * D;
+      uint16_t* dst = P.out + ((int64_t)(g.s.tok0 + row.tok) * P.q_heads + g.h * P.group + row.hd) * D;
       const auto store = [&](float inv) {
-        if (!row_on) return;
+        if (!row.on) return;
 #pragma unroll
         for (int e = 0; e < D; e += 8)
           *reinterpret_cast<uint4*>(dst + e) =
@@ -590,7 +675,7 @@ __global__ void __launch_bounds__(kAcThreads, 1) k_attn_chunk(const __grid_const
                          pack_bf16(o[e + 4] * inv, o[e + 5] * inv), pack_bf16(o[e + 6] * inv, o[e + 7] * inv));
       };
       if (g.parts == 1) {
-        store(vis > 0 ? 1.f / l : 0.f);
+        store(row.vis > 0 ? 1.f / l : 0.f);
       } else {
         // parts: [D / 4][256 rows][4], then [256][2]; the warpgroup that arrives last joins its half
         const int ri = h * kHalf + 32 * quarter + lane;
@@ -615,6 +700,7 @@ __global__ void __launch_bounds__(kAcThreads, 1) k_attn_chunk(const __grid_const
           const float base = mm == -INFINITY ? 0.f : mm;
 #pragma unroll
           for (int e = 0; e < D; ++e) o[e] = 0.f;
+#pragma unroll 1
           for (int p = 0; p < g.parts; ++p) {
             const float* sp = part_slot(P, g.first_cta, p, kRowsItem, D);
             const float2 ml = __ldcg(reinterpret_cast<const float2*>(sp + D * kRowsItem + 2 * ri));
@@ -629,11 +715,16 @@ __global__ void __launch_bounds__(kAcThreads, 1) k_attn_chunk(const __grid_const
               o[e + 3] = fmaf(v.w, fp, o[e + 3]);
             }
           }
-          store(vis > 0 ? 1.f / ll : 0.f);
+          store(row.vis > 0 ? 1.f / ll : 0.f);
         }
       }
-      // the next segment's S may overwrite this one's: every read of TMEM is behind
-      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&seg_empty[at]);
+      tc_fence_before();   // O may be overwritten once the next P is announced
+      g = g2;
+      at = at2;
+      row = row2;
+      more = more2;
     }
   }
   tc_fence_before();

@@ -19,7 +19,7 @@ constexpr int kTile = 128;
 constexpr uint64_t kArWaitLimitNs = 2000000000ull;
 
 struct FewTraits {
-  static constexpr int kLeast = 2, kSnap = 1;
+  static constexpr int kLeast = 2, kSnap = 1, kOver = 0;
   static __device__ __forceinline__ int row_tiles(const SeqInfo& s, const AttnParams& P) {
     return s.rows >= P.min_rows && s.rows <= P.max_rows ? 1 : 0;
   }
@@ -142,7 +142,7 @@ __global__ void __launch_bounds__(RowsCfg<D, WR>::kThreads, 1) k_attn_rows(const
   volatile int* abort_flag = &abort_s;
   const int chunk_shift = min(P.page_shift, 7), chunk = 1 << chunk_shift;   // rows of a TMA box
   const auto wait_warp = [&](uint64_t* bar, uint32_t parity) {
-    return __all_sync(0xffffffffu, mbar_wait_bounded(bar, parity, abort_flag, P.err, kArWaitLimitNs, kDevErrTimeout)) != 0;
+    return __all_sync(0xffffffffu, mbar_wait_short(bar, parity, abort_flag, P.err, kArWaitLimitNs)) != 0;
   };
 
   if (warp == C::kWarps) {
@@ -182,7 +182,7 @@ __global__ void __launch_bounds__(RowsCfg<D, WR>::kThreads, 1) k_attn_rows(const
         const int pg = __shfl_sync(0xffffffffu, page, (key >> P.page_shift) & 31);
         if (b < boxes) {
           const int32_t row = pg >= 0 && pg < P.pages
-                                  ? (int32_t)((((int64_t)pg * P.kv_heads + g.it.h) << P.page_shift) + (key & ((1 << P.page_shift) - 1)))
+                                  ? (int32_t)((((int64_t)pg * P.kv_heads + g.h) << P.page_shift) + (key & ((1 << P.page_shift) - 1)))
                                   : no_row;
           tma_load_3d(stage + b * (chunk * D * 2) + (lane >> 4) * C::kOpBytes, lane < 16 ? &P.kmap : &P.vmap, &full_bar[st], 0, row, 0);
         }
@@ -190,7 +190,7 @@ __global__ void __launch_bounds__(RowsCfg<D, WR>::kThreads, 1) k_attn_rows(const
           for (int row = lane; row < g.s.rows; row += 32) {
             const int tok = row / P.group, hd = row - tok * P.group;
             bulk_load(qsm + qs * C::kQBytes + row * C::kQRow,
-                      P.q + (int64_t)(g.s.tok0 + tok) * P.q_stride + (int64_t)(g.it.h * P.group + hd) * D, D * 2, &full_bar[st]);
+                      P.q + (int64_t)(g.s.tok0 + tok) * P.q_stride + (int64_t)(g.h * P.group + hd) * D, D * 2, &full_bar[st]);
           }
           if (++qs == C::kQSlots) {
             qs = 0;
@@ -439,7 +439,7 @@ __global__ void __launch_bounds__(RowsCfg<D, WR>::kThreads, 1) k_attn_rows(const
             const int pg = __ldg(P.table + (int64_t)g.r * P.width + (key >> P.page_shift));
             if (pg < 0 || pg >= P.pages) continue;
             const uint16_t* vr =
-                P.v + ((((int64_t)pg * P.kv_heads + g.it.h) << P.page_shift) + (key & ((1 << P.page_shift) - 1))) * D + kC * lane;
+                P.v + ((((int64_t)pg * P.kv_heads + g.h) << P.page_shift) + (key & ((1 << P.page_shift) - 1))) * D + kC * lane;
 #pragma unroll
             for (int c = 0; c < kC; ++c) {
               const float v = bf16_lo(vr[c]);
@@ -451,7 +451,7 @@ __global__ void __launch_bounds__(RowsCfg<D, WR>::kThreads, 1) k_attn_rows(const
           reinterpret_cast<typename L::V*>(slot + (size_t)row * D)[lane] = L::pack(a);
           if (lane == 0) *reinterpret_cast<float2*>(slot + (size_t)C::kRows * D + 2 * row) = make_float2(mm, ll);
         } else {
-          L::store_bf16(P.out + ((int64_t)(g.s.tok0 + tok) * P.q_heads + g.it.h * P.group + hd) * D + kC * lane, a,
+          L::store_bf16(P.out + ((int64_t)(g.s.tok0 + tok) * P.q_heads + g.h * P.group + hd) * D + kC * lane, a,
                         vis > 0 ? 1.f / ll : 0.f);
         }
       }
@@ -492,7 +492,7 @@ __global__ void __launch_bounds__(RowsCfg<D, WR>::kThreads, 1) k_attn_rows(const
               mm = mn;
             }
             const int tok = row / P.group, hd = row - tok * P.group;
-            L::store_bf16(P.out + ((int64_t)(g.s.tok0 + tok) * P.q_heads + g.it.h * P.group + hd) * D + kC * lane, a,
+            L::store_bf16(P.out + ((int64_t)(g.s.tok0 + tok) * P.q_heads + g.h * P.group + hd) * D + kC * lane, a,
                           g.s.seen(tok) > 0 ? 1.f / ll : 0.f);
           }
         }
