@@ -61,6 +61,7 @@ gs_status launch_paged_attention(const gs_paged_cache& c, const gs_seq_batch& b,
   P.q_heads = q_heads;
   P.kv_heads = c.kv_heads;
   P.group = q_heads / c.kv_heads;
+  P.group_inv = 0xFFFFFFFFu / (uint32_t)P.group;
   // a scale of zero weighs all keys alike: so does one this small, and masked scores (-inf) stay what they are
   P.scale_log2 = std::max(std::fabs(scale) * 1.4426950408889634f, 1e-36f);
   P.negate = scale < 0.f;

@@ -29,6 +29,7 @@ struct AttnParams {
   int* err;
   int64_t q_stride, tokens, pages;
   int32_t n_seqs, width, page_shift, q_heads, kv_heads, group;
+  uint32_t group_inv;       // floor((2^32 - 1) / group)
   int32_t min_rows, max_rows;   // sequences with that many rows (new tokens x query heads a key head) are this kernel's
   int32_t zero_rest;            // no other kernel runs: zeros for the tokens of sequences above max_rows, and of none
   float scale_log2;             // |scale| log2(e)
@@ -71,6 +72,13 @@ __device__ __forceinline__ SeqInfo seq_info(const AttnParams& P, int r) {
   return s;
 }
 
+// row / group for row >= 0: the quotient by the rounded-down inverse is short by one at most
+__device__ __forceinline__ int row_token(const AttnParams& P, int row) {
+  int q = (int)__umulhi((uint32_t)row, P.group_inv);
+  if (row - q * P.group >= P.group) ++q;
+  return q;
+}
+
 __device__ __forceinline__ float ex2(float x) {
   float y;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
@@ -102,12 +110,33 @@ __device__ __forceinline__ bool mbar_wait_short(uint64_t* bar, uint32_t parity, 
 //   row_tiles(s, P)   tiles of rows of a sequence (0: not this kernel's)
 //   tiles(s, P, rt)   units of row tile rt, at least 1
 //   kLeast, kSnap     the least units worth a CTA; boundaries this close to an item's end move there
+//   kOneTile          no sequence has more than one tile of rows
 //   kOver             what an item costs beside its units, in units: they lie before its first one and hold no work
+//
+// Units of a key head of one sequence per lane (a warp; on: the lane has one).  Long
+// sequences, of many row tiles, are summed by the whole warp one after another.
 template <class Traits>
-__device__ __forceinline__ int head_units(const AttnParams& P, const SeqInfo& s) {
-  const int nr = Traits::row_tiles(s, P);
+__device__ __forceinline__ int head_units(const AttnParams& P, const SeqInfo& s, bool on) {
+  const int lane = threadIdx.x & 31;
+  const int nr = on ? Traits::row_tiles(s, P) : 0;
   int u = 0;
-  for (int i = 0; i < nr; ++i) u += Traits::tiles(s, P, i) + Traits::kOver;
+  if (nr <= 2)
+    for (int i = 0; i < nr; ++i) u += Traits::tiles(s, P, i) + Traits::kOver;
+  if constexpr (!Traits::kOneTile) {
+    for (uint32_t many = __ballot_sync(0xffffffffu, nr > 2); many; many &= many - 1) {
+      const int src = __ffs(many) - 1, n = __shfl_sync(0xffffffffu, nr, src);
+      SeqInfo t;
+      t.tok0 = 0;
+      t.n = __shfl_sync(0xffffffffu, s.n, src);
+      t.rows = __shfl_sync(0xffffffffu, s.rows, src);
+      t.kv = __shfl_sync(0xffffffffu, s.kv, src);
+      t.cap = __shfl_sync(0xffffffffu, s.cap, src);
+      int part = 0;
+      for (int i = lane; i < n; i += 32) part += Traits::tiles(t, P, i) + Traits::kOver;
+      part = __reduce_add_sync(0xffffffffu, part);
+      if (lane == src) u = part;
+    }
+  }
   return u;
 }
 
@@ -116,19 +145,39 @@ struct Item {
   int h, rt, nt;       // nt: its units, kOver among them
   int first;           // its first unit, from the sequence's first
 };
-// the item that holds unit `off` of the sequence
+// the item that holds unit `off` of the sequence, looked up by a whole warp
 template <class Traits>
 __device__ __forceinline__ Item item_at(const AttnParams& P, const SeqInfo& s, int off, int per_head) {
+  const int lane = threadIdx.x & 31;
   Item it;
   it.h = off / per_head;
   it.first = it.h * per_head;
-  const int nr = Traits::row_tiles(s, P);
-  for (it.rt = 0; it.rt < nr; ++it.rt) {
-    it.nt = Traits::tiles(s, P, it.rt) + Traits::kOver;
-    if (off < it.first + it.nt) break;
-    it.first += it.nt;
+  it.rt = 0;
+  if constexpr (Traits::kOneTile) {
+    it.nt = per_head;
+    return it;
   }
-  return it;
+  const int nr = Traits::row_tiles(s, P);
+  while (true) {
+    const int mine = it.rt + lane < nr ? Traits::tiles(s, P, it.rt + lane) + Traits::kOver : 0;
+    int incl = mine;
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+      const int o = __shfl_up_sync(0xffffffffu, incl, d);
+      if (lane >= d) incl += o;
+    }
+    const uint32_t past = __ballot_sync(0xffffffffu, it.first + incl > off);   // the first of these lanes has it
+    if (past) {
+      const int src = __ffs(past) - 1;
+      it.rt += src;
+      it.nt = __shfl_sync(0xffffffffu, mine, src);
+      it.first += __shfl_sync(0xffffffffu, incl - mine, src);
+      return it;
+    }
+    it.first += __shfl_sync(0xffffffffu, incl, 31);
+    it.rt += 32;
+    if (it.rt >= nr) return it;   // not reached: off lies in the head
+  }
 }
 
 // total units over `ctas` CTAs: CTA c begins at c share + min(c, rest)
@@ -153,8 +202,9 @@ struct Shares {
 struct WorkSlot {
   int at;         // the boundary, moved to an item's end where that is near
   int base;       // units before sequence r
-  int r;          // the sequence that holds it (n_seqs: past the last)
-  int per_head;   // and its units a key head
+  int r;          // the sequence that holds it; n_seqs: it is the end of all
+  int per_head;   // the sequence's units a key head
+  Item it;        // the item that holds it
   SeqInfo s;
 };
 struct WorkShared {
@@ -169,17 +219,19 @@ template <class Traits, int THREADS>
 __device__ __forceinline__ Shares divide_work(const AttnParams& P, int cta, WorkShared& w) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   constexpr int kW = THREADS / 32;
-  static_assert(kW <= 32 && THREADS % 32 == 0, "block");
+  static_assert(kW >= 2 && kW <= 32 && THREADS % 32 == 0, "block");
   const bool one_pass = P.n_seqs <= THREADS;   // a sequence a thread
-  SeqInfo mine;
+  SeqInfo mine = {0, 0, 0, 0, 0};
   int per_head = 0, total = 0, items = 0;
-  if (threadIdx.x < 2) w.slot[threadIdx.x].at = INT32_MAX;   // past the last: the total
+  if (threadIdx.x < 2) w.slot[threadIdx.x].r = P.n_seqs;
   if (!one_pass) {
     int u = 0, n = 0;
-    for (int r = threadIdx.x; r < P.n_seqs; r += THREADS) {
-      mine = seq_info(P, r);
-      u += head_units<Traits>(P, mine);
-      n += Traits::row_tiles(mine, P);
+    for (int r0 = 0; r0 < P.n_seqs; r0 += THREADS) {
+      const int r = r0 + (int)threadIdx.x;
+      const bool on = r < P.n_seqs;
+      if (on) mine = seq_info(P, r);
+      u += head_units<Traits>(P, mine, on);
+      n += on ? Traits::row_tiles(mine, P) : 0;
     }
     u = __reduce_add_sync(0xffffffffu, u);
     n = __reduce_add_sync(0xffffffffu, n);
@@ -197,13 +249,10 @@ __device__ __forceinline__ Shares divide_work(const AttnParams& P, int cta, Work
   int carry = 0;
   for (int r0 = 0; r0 < P.n_seqs; r0 += THREADS) {
     const int r = r0 + (int)threadIdx.x;
-    per_head = 0;
-    int n = 0;
-    if (r < P.n_seqs) {
-      mine = seq_info(P, r);
-      per_head = head_units<Traits>(P, mine);
-      n = Traits::row_tiles(mine, P);
-    }
+    const bool on = r < P.n_seqs;
+    if (on) mine = seq_info(P, r);
+    per_head = head_units<Traits>(P, mine, on);
+    int n = on ? Traits::row_tiles(mine, P) : 0;
     const int u = per_head * P.kv_heads;
     int incl = u;
 #pragma unroll
@@ -228,17 +277,36 @@ __device__ __forceinline__ Shares divide_work(const AttnParams& P, int cta, Work
 #pragma unroll
     for (int e = 0; e < 2; ++e) {
       const int off = sh.cut(min(cta + e, sh.ctas)) - base;
-      if (off < 0 || off >= u) continue;
-      const Item it = item_at<Traits>(P, mine, off, per_head);
-      const int at = off - it.first <= Traits::kSnap + Traits::kOver ? it.first
-                     : it.first + it.nt - off <= Traits::kSnap      ? it.first + it.nt
-                                                                    : off;
-      w.slot[e] = WorkSlot{base + at, base, r, per_head, mine};
+      if (off >= 0 && off < u) {
+        w.slot[e].r = r;
+        w.slot[e].base = base;
+        w.slot[e].per_head = per_head;
+        w.slot[e].s = mine;
+      }
     }
     __syncthreads();
     if (carry > sh.cut(min(cta + 1, sh.ctas))) break;   // both boundaries are behind
   }
-  return Shares(total, items, (int)gridDim.x, Traits::kLeast);
+  const Shares sh(total, items, (int)gridDim.x, Traits::kLeast);
+  if (warp < 2) {   // a warp a boundary
+    WorkSlot& sl = w.slot[warp];
+    const int cut = sh.cut(min(cta + warp, sh.ctas));
+    int at = cut;
+    Item it = {0, 0, 0, 0};
+    if (sl.r < P.n_seqs) {
+      const int off = cut - sl.base;
+      it = item_at<Traits>(P, sl.s, off, sl.per_head);
+      if (off - it.first <= Traits::kSnap + Traits::kOver) at = sl.base + it.first;
+      else if (it.first + it.nt - off <= Traits::kSnap) at = sl.base + it.first + it.nt;
+    }
+    __syncwarp();
+    if (lane == 0) {
+      sl.at = at;
+      sl.it = it;
+    }
+  }
+  __syncthreads();
+  return sh;
 }
 
 // A stretch of one item's units in a CTA.
@@ -251,35 +319,47 @@ struct Segment {
   int first_cta;       // the CTA of part 0
 };
 
+// The segments of a CTA, one after another; for a whole warp.
 template <class Traits>
 struct Walker {
   const AttnParams& P;
   const Shares sh;
-  int cta, pos, end, base, per_head, r;
+  int cta, pos, end, first, r;   // first: the item's first unit
+  int nr;                        // row tiles of the sequence
+  Item it;
   SeqInfo s;
   __device__ __forceinline__ Walker(const AttnParams& p, const Shares& shares, const WorkShared& w, int c)
       : P(p), sh(shares), cta(c) {
-    pos = min(w.slot[0].at, sh.total);
-    end = min(w.slot[1].at, sh.total);
-    base = w.slot[0].base;
+    pos = w.slot[0].at;
+    end = w.slot[1].at;
+    it = w.slot[0].it;
     r = w.slot[0].r;
-    per_head = w.slot[0].per_head;
     s = w.slot[0].s;
+    first = w.slot[0].base + it.first;
+    nr = pos < end ? Traits::row_tiles(s, P) : 0;
   }
   __device__ __forceinline__ bool next(Segment& g) {
     if (pos >= end) return false;
-    while (pos >= base + per_head * P.kv_heads) {   // `end` lies inside some sequence, so r stays in range
-      base += per_head * P.kv_heads;
-      if (++r >= P.n_seqs) return false;
-      s = seq_info(P, r);
-      per_head = head_units<Traits>(P, s);
+    while (pos >= first + it.nt) {   // the next item: row tiles, then key heads, then sequences
+      first += it.nt;
+      if (++it.rt >= nr) {
+        it.rt = 0;
+        if (++it.h >= P.kv_heads) {
+          it.h = 0;
+          do {
+            if (++r >= P.n_seqs) return false;   // not reached: `end` lies inside some sequence
+            s = seq_info(P, r);
+            nr = Traits::row_tiles(s, P);
+          } while (nr == 0);
+        }
+      }
+      it.nt = Traits::tiles(s, P, it.rt) + Traits::kOver;
     }
     g.s = s;
     g.r = r;
-    const Item it = item_at<Traits>(P, s, pos - base, per_head);
     g.h = it.h;
     g.rt = it.rt;
-    const int first = base + it.first, last = first + it.nt, stop = min(last, end);
+    const int last = first + it.nt, stop = min(last, end);
     g.ta = max(0, pos - first - Traits::kOver);
     g.tb = stop - first - Traits::kOver;
     g.parts = 1;

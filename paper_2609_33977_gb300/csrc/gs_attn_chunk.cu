@@ -9,9 +9,10 @@
 //     reads its row of S, writes P = exp2(c S - m) over it as bf16, and
 //     O += P V (A = P in TMEM, B = V as stored, i.e. MN-major), O stays in TMEM.
 // Each half has two S, so that the next unit's S is there when the softmax comes to
-// it; the MMA warp issues whatever is ready, of either half.  (Units of 128 keys
-// leave room for one S a half, which then waits for P V: twice the time.)  O is
-// rescaled only when a row's maximum grew by more than 2^8 (each row for itself),
+// it, and its own MMA warp (a product of 64 keys is 100 cycles of issue a 16-deep
+// step short of the tensor cores' pace: one warp for both halves held them up).
+// (Units of 128 keys leave room for one S a half, which then waits for P V: twice
+// the time.)  O is rescaled only when a row's maximum grew by more than 2^8 (each row for itself),
 // else the old maximum stays in use: exact, since both the sum and O carry it.
 //
 // Keys and values arrive page by page (TMA) in rings of five 16 KB slots each.  Values
@@ -28,21 +29,22 @@ using namespace sm100;
 
 constexpr int kCT = 64;                        // keys of a unit
 constexpr int kHalf = 128, kRowsItem = 256;
-constexpr int kAcThreads = 384;                // warps: keys, MMA, values, value check, then two softmax warpgroups
+constexpr int kAcThreads = 512;                // warps: keys, values, two MMA; four value checkers; two softmax warpgroups
 constexpr int kRing = 5;                       // slots of keys, and as many of values
 constexpr int kSegs = 4;
 constexpr uint64_t kAcWaitLimitNs = 2000000000ull;
-constexpr int kRegsOther = 72, kRegsSoftmax = 216;
-static_assert(4 * 32 * kRegsOther + 8 * 32 * kRegsSoftmax <= kAcThreads * 168, "register split");
+constexpr int kRegsOther = 56, kRegsSoftmax = 200;
+static_assert(8 * 32 * (kRegsOther + kRegsSoftmax) <= kAcThreads * 128, "register split");
 
 struct ChunkTraits {
   static constexpr int kLeast = 8, kSnap = 3, kOver = 2;
+  static constexpr bool kOneTile = false;
   static __device__ __forceinline__ int row_tiles(const SeqInfo& s, const AttnParams& P) {
     return s.rows >= P.min_rows && s.rows <= P.max_rows ? (s.rows + kRowsItem - 1) / kRowsItem : 0;
   }
   // units that the rows up to `row_end` of a sequence see
   static __device__ __forceinline__ int units_of(const SeqInfo& s, const AttnParams& P, int row_end) {
-    return max(1, (s.seen((min(row_end, s.rows) - 1) / P.group) + kCT - 1) / kCT);
+    return max(1, (s.seen(row_token(P, min(row_end, s.rows) - 1)) + kCT - 1) / kCT);
   }
   static __device__ __forceinline__ int tiles(const SeqInfo& s, const AttnParams& P, int rt) {
     return units_of(s, P, (rt + 1) * kRowsItem);
@@ -76,28 +78,11 @@ __device__ __forceinline__ void tmem_st_x32(uint32_t taddr, const uint32_t (&v)[
       "r"(v[31])
       : "memory");
 }
-// Shared-memory descriptor of the values as an MN-major operand, 128-byte swizzle: 64-channel
-// blocks of `block` bytes, 8-key groups 1024 bytes apart
-__device__ __forceinline__ uint64_t sdesc_v(uint32_t saddr, uint32_t block) {
-  uint64_t d = 0;
-  d |= (uint64_t)((saddr >> 4) & 0x3FFFu);
-  d |= (uint64_t)(block >> 4) << 16;
-  d |= (uint64_t)(1024 >> 4) << 32;
-  d |= (uint64_t)1 << 46;
-  d |= (uint64_t)2 << 61;
-  return d;
-}
-__device__ __forceinline__ bool mbar_test_wait(uint64_t* bar, uint32_t parity) {   // does not suspend
-  uint32_t ok;
-  asm volatile(
-      "{\n\t.reg .pred p;\n\t"
-      "mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
-      "selp.u32 %0, 1, 0, p;\n\t}"
-      : "=r"(ok)
-      : "r"(smem_u32(bar)), "r"(parity)
-      : "memory");
-  return ok != 0;
-}
+// Shared-memory descriptors, 128-byte swizzle, 8-row groups 1024 bytes apart: the upper word is the same for all, the lower
+// one has the address and, for the values (MN-major), the distance of their 64-channel blocks.
+constexpr uint32_t kDescHi = (1024u >> 4) | (1u << 14) | (2u << 29);
+__device__ __forceinline__ uint32_t desc_lo(uint32_t saddr, uint32_t block) { return (saddr >> 4) | ((block >> 4) << 16); }
+__device__ __forceinline__ uint64_t desc(uint32_t lo) { return ((uint64_t)kDescHi << 32) | lo; }
 __device__ __forceinline__ float max3(float a, float b, float c) { return fmaxf(fmaxf(a, b), c); }
 __device__ __forceinline__ uint32_t nonfinite2(uint32_t v) {   // bits of the halves that are an infinity or NaN
   const uint32_t e = v & 0x7F807F80u;
@@ -135,7 +120,7 @@ __global__ void __launch_bounds__(kAcThreads, 1) k_attn_chunk(const __grid_const
   __shared__ __align__(8) uint64_t p_bar[2][2];        // P is in TMEM, O is rescaled
   __shared__ __align__(8) uint64_t o_bar[2];           // P V is done
   __shared__ __align__(8) uint64_t join_bar[2];
-  __shared__ __align__(8) uint64_t drain_bar;
+  __shared__ __align__(8) uint64_t drain_bar[2];
   __shared__ Segment segs[kSegs];
   __shared__ WorkShared work;
   __shared__ uint32_t tmem_base_s;
@@ -148,14 +133,14 @@ __global__ void __launch_bounds__(kAcThreads, 1) k_attn_chunk(const __grid_const
   if (threadIdx.x == 0) {
     for (int s = 0; s < kRing; ++s) {
       mbar_init(&kfull_bar[s], 1);
-      mbar_init(&kempty_bar[s], 1);
+      mbar_init(&kempty_bar[s], 2);   // both MMA warps
       mbar_init(&vfull_bar[s], 1);
-      mbar_init(&vempty_bar[s], 1);
-      mbar_init(&clean_bar[s], 1);
+      mbar_init(&vempty_bar[s], 2);
+      mbar_init(&clean_bar[s], 4);
     }
     for (int s = 0; s < kSegs; ++s) {
       mbar_init(&seg_full[s], 1);
-      mbar_init(&seg_empty[s], 11);   // every warp but the one that fills it
+      mbar_init(&seg_empty[s], 15);   // every warp but the one that fills it
     }
     for (int h = 0; h < 2; ++h) {
       mbar_init(&q_bar[h], 4);
@@ -166,13 +151,14 @@ __global__ void __launch_bounds__(kAcThreads, 1) k_attn_chunk(const __grid_const
       mbar_init(&o_bar[h], 1);
       mbar_init(&join_bar[h], 4);
     }
-    mbar_init(&drain_bar, 1);
+    mbar_init(&drain_bar[0], 1);
+    mbar_init(&drain_bar[1], 1);
     abort_s = 0;
     fence_mbar_init();
     prefetch_tmap(&P.kmap);
     prefetch_tmap(&P.vmap);
   }
-  if (warp == 1) {
+  if (warp == 2) {
     tmem_alloc(&tmem_base_s, 512);
     tmem_relinquish();
   }
@@ -190,7 +176,7 @@ __global__ void __launch_bounds__(kAcThreads, 1) k_attn_chunk(const __grid_const
   const auto half_end = [&](const Segment& g, int h) { return min(g.tb, ChunkTraits::units_of(g.s, P, g.rt * kRowsItem + (h + 1) * kHalf)); };
   const auto halves = [&](const Segment& g) { return g.s.rows - g.rt * kRowsItem > kHalf ? 2 : 1; };
 
-  if (warp < 4) {
+  if (warp < 8) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsOther));
     uint32_t sg = 0, sph = 0;          // segment slot and its phase
     const auto next_seg = [&]() {
@@ -201,8 +187,8 @@ __global__ void __launch_bounds__(kAcThreads, 1) k_attn_chunk(const __grid_const
         sph ^= 1u;
       }
     };
-    if (warp == 0 || warp == 2) {
-      // ---------------------------------------------------------- copies: warp 0 keys (it also divides the work), warp 2 values
+    if (warp < 2) {
+      // ---------------------------------------------------------- copies: warp 0 keys (it also walks the work), warp 1 values
       const bool keys = warp == 0;
       Walker<ChunkTraits> walk(P, shares, work, cta);
       Segment g;
@@ -219,6 +205,7 @@ __global__ void __launch_bounds__(kAcThreads, 1) k_attn_chunk(const __grid_const
           if (lane == 0) {
             if (!more) g.r = -1;
             segs[sg] = g;
+            bad_s[sg] = 0;
             mbar_arrive(&seg_full[sg]);
           }
           __syncwarp();
@@ -279,129 +266,123 @@ __global__ void __launch_bounds__(kAcThreads, 1) k_attn_chunk(const __grid_const
           }
         }
       }
-    } else if (warp == 1) {
-      // ---------------------------------------------------------- MMA issuer
+    } else if (warp < 4) {
+      // ---------------------------------------------------------- MMA issuer of a half
+      const int h = warp - 2;
       const uint32_t idesc_s = idesc_bf16_f32(kHalf, kCT);
       const uint32_t idesc_o = idesc_bf16_f32(kHalf, D) | (1u << 16);   // bit 16: B is MN-major
       const uint32_t vblock = (uint32_t)box * 128u;
-      const auto test_warp = [&](uint64_t* bar, uint32_t parity) { return __all_sync(0xffffffffu, mbar_test_wait(bar, parity)) != 0; };
-      // Per half, counted over all segments: products of S and of P V issued, and P V known to be over.  The n-th S goes to
-      // buffer n & 1, where the (n - 2)-th P was read.  The slots of keys and values follow from the units of the segments
-      // before (used) and the unit.
-      uint32_t ns[2] = {0u, 0u}, no[2] = {0u, 0u}, over[2] = {0u, 0u}, qph[2] = {0u, 0u};
-      uint32_t used = 0;
+      const uint32_t q_lo = desc_lo(smem_u32(smem + h * C::kQBytes), 16), k_lo = desc_lo(smem_u32(ring_k), 16);
+      const uint32_t v_lo = desc_lo(smem_u32(ring_v), vblock);
+      uint32_t v_off[kCT / 16];   // of 16 keys in a slot
+#pragma unroll
+      for (int kk = 0; kk < kCT / 16; ++kk)
+        v_off[kk] = ((uint32_t)((16 * kk) >> box_shift) * (vblock * C::kSlabs) + (uint32_t)((16 * kk) & (box - 1)) * 128u) >> 4;
+      const uint32_t t_s = tmem + h * 128, t_o = tmem + 256 + h * 128;
+      // Units are counted over all segments (n): the n-th S goes to buffer n & 1.  The order within a unit is
+      //     P V of the unit before is over -> S of the next unit (into the buffer that product read)
+      //     P is there                     -> P V
+      // so that the softmax finds its next S ready, and every P V is waited for once, before the next one.
+      uint32_t n = 0, qph = 0u, ks = 0, kph = 0u, vs = 0, vph = 0u;
       bool ok = true;
+      const auto keys_used = [&](bool used) {   // this half's part of handing the slot back
+        if (!used) {
+          __syncwarp();
+          if (lane == 0) mbar_arrive(&kempty_bar[ks]);
+        }
+        if (++ks == kRing) {
+          ks = 0;
+          kph ^= 1u;
+        }
+      };
+      const auto issue_s = [&](uint32_t buf) {
+        if (elect_one()) {
+          const uint32_t b = k_lo + ks * (C::kOpBytes >> 4), d = t_s + buf * kCT;
+#pragma unroll
+          for (int kk = 0; kk < D / 16; ++kk)
+            mma_bf16_ss(d, desc(q_lo + (((kk >> 2) * (kHalf * 128) + (kk & 3) * 32) >> 4)),
+                        desc(b + (((kk >> 2) * (kCT * 128) + (kk & 3) * 32) >> 4)), idesc_s, kk == 0 ? 0u : 1u);
+          mma_commit(&s_bar[h][buf]);
+          mma_commit(&kempty_bar[ks]);
+        }
+        __syncwarp();
+      };
       while (ok) {
         if (!wait_warp(&seg_full[sg], sph)) break;
         const Segment g = segs[sg];
         next_seg();
         if (g.r < 0) break;
-        const int n_units = g.tb - g.ta, nh = halves(g);
-        int units[2];   // of a half; the last half has them all
-        units[0] = max(0, half_end(g, 0) - g.ta);
-        units[1] = nh > 1 ? n_units : 0;
-        if (nh == 1) units[0] = n_units;
-        int us[2] = {0, 0}, uo[2] = {0, 0};   // the next unit's S, P V
-        bool have_q[2] = {false, false};
-        uint32_t ks[2], kp[2], vs[2], vp[2];
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          ks[h] = vs[h] = used % kRing;
-          kp[h] = vp[h] = (used / kRing) & 1u;
+        const int n_units = g.tb - g.ta;
+        const int units = h < halves(g) ? max(0, half_end(g, h) - g.ta) : 0;   // this half's
+        if (!wait_warp(&kfull_bar[ks], kph)) break;
+        if (units > 0) {
+          if (!wait_warp(&q_bar[h], qph)) break;
+          qph ^= 1u;
+          tc_fence_after();
+          issue_s(n & 1u);
         }
-        uint64_t t0 = 0;
-        uint32_t idle = 0;
-        while (ok && (uo[0] < units[0] || uo[1] < units[1])) {
-          bool did = false;
-#pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            if (over[h] != no[h] && test_warp(&o_bar[h], over[h] & 1u)) ++over[h];
-            // P V of the oldest unit, once P and the values are there; the one before is over (one at a time in flight)
-            if (uo[h] < us[h] && over[h] == no[h] && test_warp(&p_bar[h][no[h] & 1u], (no[h] >> 1) & 1u) &&
-                test_warp(&clean_bar[vs[h]], vp[h])) {
-              tc_fence_after();
-              if (elect_one()) {
-                const uint32_t v = smem_u32(ring_v + vs[h] * C::kOpBytes), p = tmem + h * 128 + (no[h] & 1u) * kCT;
-#pragma unroll
-                for (int kk = 0; kk < kCT / 16; ++kk) {
-                  const int key = 16 * kk;
-                  const uint32_t off = (uint32_t)(key >> box_shift) * (vblock * C::kSlabs) + (uint32_t)(key & (box - 1)) * 128u;
-                  mma_bf16_ts(tmem + 256 + h * 128, p + 8 * kk, sdesc_v(v + off, vblock), idesc_o, uo[h] == 0 && kk == 0 ? 0u : 1u);
-                }
-                mma_commit(&o_bar[h]);
-                // a slot goes back with the second of the halves that use it
-                if (uo[h] >= units[h ^ 1] || uo[h ^ 1] > uo[h]) mma_commit(&vempty_bar[vs[h]]);
-              }
-              __syncwarp();
-              ++no[h];
-              ++uo[h];
-              if (++vs[h] == kRing) {
-                vs[h] = 0;
-                vp[h] ^= 1u;
-              }
-              did = true;
-            }
-            // S of the next unit: its buffer is free once the P before last has been read
-            if (us[h] < units[h] && ns[h] <= over[h] + 1u && test_warp(&kfull_bar[ks[h]], kp[h])) {
-              if (!have_q[h]) {
-                if (!test_warp(&q_bar[h], qph[h])) continue;
-                have_q[h] = true;
-                qph[h] ^= 1u;
-              }
-              tc_fence_after();
-              if (elect_one()) {
-                const uint64_t a = sdesc_sw128(smem_u32(smem + h * C::kQBytes)), b = sdesc_sw128(smem_u32(ring_k + ks[h] * C::kOpBytes));
-#pragma unroll
-                for (int kk = 0; kk < D / 16; ++kk)
-                  mma_bf16_ss(tmem + h * 128 + (ns[h] & 1u) * kCT, a + (uint64_t)(((kk >> 2) * (kHalf * 128) + (kk & 3) * 32) >> 4),
-                              b + (uint64_t)(((kk >> 2) * (kCT * 128) + (kk & 3) * 32) >> 4), idesc_s, kk == 0 ? 0u : 1u);
-                mma_commit(&s_bar[h][ns[h] & 1u]);
-                if (us[h] >= units[h ^ 1] || us[h ^ 1] > us[h]) mma_commit(&kempty_bar[ks[h]]);
-              }
-              __syncwarp();
-              ++ns[h];
-              ++us[h];
-              if (++ks[h] == kRing) {
-                ks[h] = 0;
-                kp[h] ^= 1u;
-              }
-              did = true;
-            }
+        keys_used(units > 0);
+        for (int u = 0; u < n_units; ++u) {
+          if (u + 1 < n_units && !wait_warp(&kfull_bar[ks], kph)) {
+            ok = false;
+            break;
           }
-          if (did) {
-            idle = 0;
-          } else if ((++idle & 1023u) == 0) {   // bounded, like every wait
-            const uint64_t now = globaltimer_ns();
-            if (idle == 1024u) t0 = now;
-            if (*abort_flag) ok = false;
-            if (now - t0 > kAcWaitLimitNs) {
-              *abort_flag = 1;
-              atomicExch(P.err, kDevErrTimeout);
+          if (u < units && n > 0u) {
+            if (!wait_warp(&o_bar[h], (n - 1u) & 1u)) {
               ok = false;
+              break;
             }
-            ok = __all_sync(0xffffffffu, ok);
+            tc_fence_after();
+          }
+          if (u + 1 < n_units) {
+            if (u + 1 < units) issue_s((n + 1u) & 1u);
+            keys_used(u + 1 < units);
+          }
+          if (!wait_warp(&clean_bar[vs], vph)) {
+            ok = false;
+            break;
+          }
+          if (u < units) {
+            if (!wait_warp(&p_bar[h][n & 1u], (n >> 1) & 1u)) {
+              ok = false;
+              break;
+            }
+            tc_fence_after();
+            if (elect_one()) {
+              const uint32_t v = v_lo + vs * (C::kOpBytes >> 4), p = t_s + (n & 1u) * kCT;
+#pragma unroll
+              for (int kk = 0; kk < kCT / 16; ++kk) mma_bf16_ts(t_o, p + 8 * kk, desc(v + v_off[kk]), idesc_o, kk > 0 ? 1u : (uint32_t)u);
+              mma_commit(&o_bar[h]);
+              mma_commit(&vempty_bar[vs]);
+            }
+            __syncwarp();
+            ++n;
+          } else if (lane == 0) {
+            mbar_arrive(&vempty_bar[vs]);
+          }
+          if (++vs == kRing) {
+            vs = 0;
+            vph ^= 1u;
           }
         }
-        used += (uint32_t)n_units;
       }
       // whatever was issued is over before TMEM goes back
       if (elect_one()) {
-        mma_commit(&drain_bar);
-        mbar_wait_bounded(&drain_bar, 0u, nullptr, P.err, kAcWaitLimitNs, kDevErrTimeout);
+        mma_commit(&drain_bar[h]);
+        mbar_wait_bounded(&drain_bar[h], 0u, nullptr, P.err, kAcWaitLimitNs, kDevErrTimeout);
       }
       __syncwarp();
     } else {
       // ---------------------------------------------------------- values that some row does not see
       uint32_t vs = 0, vph = 0u;
       bool ok = true;
+      const int mine = warp - 4;
       while (ok) {
         if (!wait_warp(&seg_full[sg], sph)) break;
         const Segment g = segs[sg];
         const uint32_t at = sg;
-        if (g.r >= 0 && lane == 0) bad_s[at] = 0;
-        next_seg();
         if (g.r < 0) break;
-        const int len = g.s.len(), all_see = g.s.seen(g.rt * kRowsItem / P.group);
+        const int len = g.s.len(), all_see = g.s.seen(row_token(P, g.rt * kRowsItem));
         for (int t = g.ta; t < g.tb; ++t) {
           if (!wait_warp(&vfull_bar[vs], vph)) {
             ok = false;
@@ -410,28 +391,27 @@ __global__ void __launch_bounds__(kAcThreads, 1) k_attn_chunk(const __grid_const
           const int key0 = t * kCT;
           if (key0 + kCT > all_see) {
             const uint32_t v = smem_u32(ring_v + vs * C::kOpBytes);
-            constexpr int kPieces = D / 8, kStep = 32 / kPieces, kDeep = 8;   // keys of a step of the warp; steps at once
+            constexpr int kPieces = D / 8, kStep = 32 / kPieces, kDeep = 16 / kStep;   // keys of a step of the warp; steps at once
             const int end = min(kCT, max(0, len - key0)), piece = lane % kPieces;
             bool bad = false;
-            for (int k0 = max(0, all_see - key0); k0 < kCT; k0 += kDeep * kStep) {
+            for (int k0 = max(0, all_see - key0) + mine * (kDeep * kStep); k0 < kCT; k0 += 4 * kDeep * kStep) {
               uint4 x[kDeep];
               uint32_t at16[kDeep];
 #pragma unroll
               for (int i = 0; i < kDeep; ++i) {
                 // a key's row is kSlabs pieces of 128 bytes; their swizzle does not matter here
-                const int k = k0 + i * kStep + lane / kPieces;
+                const int k = min(k0 + i * kStep + lane / kPieces, kCT - 1);
                 at16[i] = v + (uint32_t)((((k >> box_shift) * C::kSlabs + (piece >> 3)) << box_shift) * 128 + (k & (box - 1)) * 128 +
                                          (piece & 7) * 16);
-                x[i] = make_uint4(0u, 0u, 0u, 0u);
-                if (k < end)
-                  asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];"
-                               : "=r"(x[i].x), "=r"(x[i].y), "=r"(x[i].z), "=r"(x[i].w)
-                               : "r"(at16[i])
-                               : "memory");
+                asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];"
+                             : "=r"(x[i].x), "=r"(x[i].y), "=r"(x[i].z), "=r"(x[i].w)
+                             : "r"(at16[i])
+                             : "memory");
               }
 #pragma unroll
               for (int i = 0; i < kDeep; ++i) {
                 const int k = k0 + i * kStep + lane / kPieces;
+                if (k >= end) x[i] = make_uint4(0u, 0u, 0u, 0u);
                 const uint4 n = make_uint4(nonfinite2(x[i].x), nonfinite2(x[i].y), nonfinite2(x[i].z), nonfinite2(x[i].w));
                 const bool hit = (n.x | n.y | n.z | n.w) != 0u;
                 if (k < kCT && (hit || k >= end))
@@ -451,13 +431,14 @@ __global__ void __launch_bounds__(kAcThreads, 1) k_attn_chunk(const __grid_const
             vph ^= 1u;
           }
         }
+        next_seg();
       }
-      if (P.zero_rest) zero_rows(P, D, cta, lane, false);
+      if (P.zero_rest && mine == 0) zero_rows(P, D, cta, lane, false);
     }
   } else {
     // ------------------------------------------------------------ softmax: a row a thread
     asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegsSoftmax));
-    const int h = (warp - 4) >> 2, quarter = warp & 3;
+    const int h = (warp - 8) >> 2, quarter = warp & 3;
     const uint32_t lane_base = (uint32_t)(32 * quarter) << 16;
     const uint32_t ts = tmem + h * 128 + lane_base, to = tmem + 256 + h * 128 + lane_base;
     uint32_t sg = 0, sph = 0, n = 0, j_ph = 0u;   // n: units so far
@@ -495,7 +476,7 @@ __global__ void __launch_bounds__(kAcThreads, 1) k_attn_chunk(const __grid_const
       const int row = g.rt * kRowsItem + h * kHalf + 32 * quarter + lane;
       Row r;
       r.on = row < g.s.rows;
-      r.tok = r.on ? row / P.group : 0;
+      r.tok = r.on ? row_token(P, row) : 0;
       r.hd = r.on ? row - r.tok * P.group : 0;
       r.vis = r.on ? g.s.seen(r.tok) : 0;
       return r;
@@ -505,13 +486,14 @@ __global__ void __launch_bounds__(kAcThreads, 1) k_attn_chunk(const __grid_const
       if (g.ta >= half_end(g, h)) return;
       constexpr int kPieces = D / 8, kStep = 32 / kPieces;
       const uint32_t flip = P.negate ? 0x80008000u : 0u;
-      const uint64_t mine = row.on ? (uint64_t)((int64_t)(g.s.tok0 + row.tok) * P.q_stride + (int64_t)(g.h * P.group + row.hd) * D) : ~0ull;
+      // rows past the last read the first one's (a load that depends on a branch waits for the one before it); nobody
+      // reads their results
+      const int64_t mine = (int64_t)(g.s.tok0 + row.tok) * P.q_stride + (int64_t)(g.h * P.group + row.hd) * D;
       uint4 x[32 / kStep];
 #pragma unroll
       for (int i = 0; i < 32 / kStep; ++i) {
-        const uint64_t at = __shfl_sync(0xffffffffu, mine, i * kStep + lane / kPieces);
-        x[i] = make_uint4(0u, 0u, 0u, 0u);
-        if (at != ~0ull) x[i] = __ldg(reinterpret_cast<const uint4*>(P.q + at) + lane % kPieces);
+        const int64_t at = __shfl_sync(0xffffffffu, mine, i * kStep + lane / kPieces);
+        x[i] = __ldg(reinterpret_cast<const uint4*>(P.q + at) + lane % kPieces);
       }
 #pragma unroll
       for (int i = 0; i < 32 / kStep; ++i) {
@@ -533,7 +515,7 @@ __global__ void __launch_bounds__(kAcThreads, 1) k_attn_chunk(const __grid_const
     }
     while (more) {
       const int end = half_end(g, h);
-      const int all_see = g.s.seen((g.rt * kRowsItem + h * kHalf) / P.group);
+      const int all_see = g.s.seen(row_token(P, g.rt * kRowsItem + h * kHalf));
       float m = -INFINITY, l = 0.f;
       bool ok = true;
       for (int t = g.ta; t < end; ++t, ++n) {
@@ -654,7 +636,7 @@ __global__ void __launch_bounds__(kAcThreads, 1) k_attn_chunk(const __grid_const
       }
       if (bad_s[at]) {   // infinities and NaN of keys that only some rows see
         const int stop = min(g.tb * kCT, row.vis);
-        for (int key = max(g.s.seen(g.rt * kRowsItem / P.group), g.ta * kCT); key < stop; ++key) {
+        for (int key = max(g.s.seen(row_token(P, g.rt * kRowsItem)), g.ta * kCT); key < stop; ++key) {
           const int pg = __ldg(P.table + (int64_t)g.r * P.width + (key >> P.page_shift));
           if (pg < 0 || pg >= P.pages) continue;
           const uint16_t* vr = P.v + ((((int64_t)pg * P.kv_heads + g.h) << P.page_shift) + (key & ((1 << P.page_shift) - 1))) * D;
@@ -735,7 +717,7 @@ __global__ void __launch_bounds__(kAcThreads, 1) k_attn_chunk(const __grid_const
     while (globaltimer_ns() - t0 < 2000000ull) {
     }
   }
-  if (warp == 1) {
+  if (warp == 2) {
     tc_fence_after();
     tmem_dealloc(tmem, 512);
   }

@@ -20,6 +20,7 @@ constexpr uint64_t kArWaitLimitNs = 2000000000ull;
 
 struct FewTraits {
   static constexpr int kLeast = 2, kSnap = 1, kOver = 0;
+  static constexpr bool kOneTile = true;
   static __device__ __forceinline__ int row_tiles(const SeqInfo& s, const AttnParams& P) {
     return s.rows >= P.min_rows && s.rows <= P.max_rows ? 1 : 0;
   }
@@ -188,7 +189,7 @@ __global__ void __launch_bounds__(RowsCfg<D, WR>::kThreads, 1) k_attn_rows(const
         }
         if (first) {
           for (int row = lane; row < g.s.rows; row += 32) {
-            const int tok = row / P.group, hd = row - tok * P.group;
+            const int tok = row_token(P, row), hd = row - tok * P.group;
             bulk_load(qsm + qs * C::kQBytes + row * C::kQRow,
                       P.q + (int64_t)(g.s.tok0 + tok) * P.q_stride + (int64_t)(g.h * P.group + hd) * D, D * 2, &full_bar[st]);
           }
@@ -254,7 +255,7 @@ __global__ void __launch_bounds__(RowsCfg<D, WR>::kThreads, 1) k_attn_rows(const
 #pragma unroll
       for (int hf = 0; hf < 2; ++hf) {
         const int row = row0 + 8 * hf;
-        seen[hf] = row < g.s.rows ? g.s.seen(row / P.group) : 0;
+        seen[hf] = row < g.s.rows ? g.s.seen(row_token(P, row)) : 0;
         const uint32_t* src = reinterpret_cast<const uint32_t*>(qsm + qs * C::kQBytes + row * C::kQRow) + qd;
 #pragma unroll
         for (int ks = 0; ks < D / 16; ++ks) {
@@ -432,7 +433,7 @@ __global__ void __launch_bounds__(RowsCfg<D, WR>::kThreads, 1) k_attn_rows(const
 #pragma unroll
           for (int c = 0; c < kC; ++c) a[c] = fmaf(v[c], f, a[c]);
         }
-        const int tok = row / P.group, hd = row - tok * P.group, vis = g.s.seen(tok);
+        const int tok = row_token(P, row), hd = row - tok * P.group, vis = g.s.seen(tok);
         if (fix) {   // infinities and NaN of keys that only some rows see
           const int end = min(min(len, g.tb * kTile), vis);
           for (int key = max(all_see, g.ta * kTile); key < end; ++key) {
@@ -491,7 +492,7 @@ __global__ void __launch_bounds__(RowsCfg<D, WR>::kThreads, 1) k_attn_rows(const
               for (int c = 0; c < kC; ++c) a[c] = a[c] * f0 + v[c] * f1;
               mm = mn;
             }
-            const int tok = row / P.group, hd = row - tok * P.group;
+            const int tok = row_token(P, row), hd = row - tok * P.group;
             L::store_bf16(P.out + ((int64_t)(g.s.tok0 + tok) * P.q_heads + g.h * P.group + hd) * D + kC * lane, a,
                           g.s.seen(tok) > 0 ? 1.f / ll : 0.f);
           }
