@@ -85,26 +85,30 @@ __device__ __forceinline__ float ex2(float x) {
   return y;
 }
 
-// A bounded wait for barriers that complete within a microsecond or two: the clock and the
-// abort flag are only looked at after many tries (a try itself waits for a while).
-__device__ __forceinline__ bool mbar_wait_short(uint64_t* bar, uint32_t parity, volatile int* abort_flag, int* err,
-                                                uint64_t limit_ns) {
+// A whole warp's bounded wait, for barriers that complete within a microsecond or two: the
+// clock and the abort flag are only looked at after many tries (a try itself waits for a
+// while).  The same answer for all lanes.
+__device__ __forceinline__ bool mbar_wait_warp(uint64_t* bar, uint32_t parity, volatile int* abort_flag, int* err,
+                                               uint64_t limit_ns) {
+  if (__all_sync(0xffffffffu, sm100::mbar_try_wait(bar, parity))) return true;
+  uint64_t t0 = 0;
 #pragma unroll 1
-  for (int i = 0; i < 64; ++i)
-    if (sm100::mbar_try_wait(bar, parity)) return true;
-  const uint64_t t0 = sm100::globaltimer_ns();
-  while (true) {
-#pragma unroll 1
-    for (int i = 0; i < 64; ++i)
-      if (sm100::mbar_try_wait(bar, parity)) return true;
-    if (*abort_flag) return false;
-    if (sm100::globaltimer_ns() - t0 > limit_ns) {
+  for (uint32_t tries = 1;; ++tries) {
+    if (__all_sync(0xffffffffu, sm100::mbar_try_wait(bar, parity))) return true;
+    if ((tries & 63u) != 0) continue;
+    const uint64_t now = sm100::globaltimer_ns();
+    if (tries == 64u) t0 = now;
+    bool give_up = *abort_flag != 0;
+    if (now - t0 > limit_ns) {
       *abort_flag = 1;
       atomicExch(err, kDevErrTimeout);
-      return false;
+      give_up = true;
     }
+    if (__any_sync(0xffffffffu, give_up)) return false;
   }
 }
+// A value that all lanes share, known as such to the compiler
+__device__ __forceinline__ int uniform(int v) { return (int)__reduce_max_sync(0xffffffffu, (uint32_t)v); }
 
 // Units are counted in 32 bits (the host refuses steps that could have more).  Traits:
 //   row_tiles(s, P)   tiles of rows of a sequence (0: not this kernel's)

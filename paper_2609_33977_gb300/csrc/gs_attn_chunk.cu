@@ -37,7 +37,7 @@ constexpr int kRegsOther = 56, kRegsSoftmax = 200;
 static_assert(8 * 32 * (kRegsOther + kRegsSoftmax) <= kAcThreads * 128, "register split");
 
 struct ChunkTraits {
-  static constexpr int kLeast = 8, kSnap = 3, kOver = 2;
+  static constexpr int kLeast = 8, kSnap = 3, kOver = 5;
   static constexpr bool kOneTile = false;
   static __device__ __forceinline__ int row_tiles(const SeqInfo& s, const AttnParams& P) {
     return s.rows >= P.min_rows && s.rows <= P.max_rows ? (s.rows + kRowsItem - 1) / kRowsItem : 0;
@@ -59,13 +59,34 @@ struct ChunkCfg {
   static constexpr int kSlabs = D / 64;
 };
 
-// D[tmem] (+)= A[tmem] * B[smem], one CTA
-__device__ __forceinline__ void mma_bf16_ts(uint32_t d_tmem, uint32_t a_tmem, uint64_t bdesc, uint32_t idesc, uint32_t accumulate) {
+// The MMA warps run converged, and one lane (`on`) issues: guarded instructions instead of a branch keep the operands in
+// uniform registers, which the tensor instructions take.
+__device__ __forceinline__ void mma_ss(uint32_t d_tmem, uint64_t adesc, uint64_t bdesc, uint32_t idesc, uint32_t accumulate,
+                                       uint32_t on) {
   asm volatile(
-      "{\n\t.reg .pred p;\n\t"
+      "{\n\t.reg .pred p, q;\n\t"
       "setp.ne.b32 p, %4, 0;\n\t"
-      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
-      ::"r"(d_tmem), "r"(a_tmem), "l"(bdesc), "r"(idesc), "r"(accumulate)
+      "setp.ne.b32 q, %5, 0;\n\t"
+      "@q tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
+      ::"r"(d_tmem), "l"(adesc), "l"(bdesc), "r"(idesc), "r"(accumulate), "r"(on)
+      : "memory");
+}
+// A in TMEM
+__device__ __forceinline__ void mma_ts(uint32_t d_tmem, uint32_t a_tmem, uint64_t bdesc, uint32_t idesc, uint32_t accumulate,
+                                       uint32_t on) {
+  asm volatile(
+      "{\n\t.reg .pred p, q;\n\t"
+      "setp.ne.b32 p, %4, 0;\n\t"
+      "setp.ne.b32 q, %5, 0;\n\t"
+      "@q tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
+      ::"r"(d_tmem), "r"(a_tmem), "l"(bdesc), "r"(idesc), "r"(accumulate), "r"(on)
+      : "memory");
+}
+__device__ __forceinline__ void commit_to(uint64_t* bar, uint32_t on) {
+  asm volatile(
+      "{\n\t.reg .pred q;\n\t"
+      "setp.ne.b32 q, %1, 0;\n\t"
+      "@q tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n\t}" ::"r"(smem_u32(bar)), "r"(on)
       : "memory");
 }
 __device__ __forceinline__ void tmem_st_x32(uint32_t taddr, const uint32_t (&v)[32]) {
@@ -166,11 +187,11 @@ __global__ void __launch_bounds__(kAcThreads, 1) k_attn_chunk(const __grid_const
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
-  const uint32_t tmem = tmem_base_s;
+  const uint32_t tmem = (uint32_t)uniform((int)tmem_base_s);
   volatile int* abort_flag = &abort_s;
   const int box_shift = min(P.page_shift, 6), box = 1 << box_shift;   // rows of a TMA box
   const auto wait_warp = [&](uint64_t* bar, uint32_t parity) {
-    return __all_sync(0xffffffffu, mbar_wait_short(bar, parity, abort_flag, P.err, kAcWaitLimitNs)) != 0;
+    return mbar_wait_warp(bar, parity, abort_flag, P.err, kAcWaitLimitNs);
   };
   // A half's units end where its last row's keys end.
   const auto half_end = [&](const Segment& g, int h) { return min(g.tb, ChunkTraits::units_of(g.s, P, g.rt * kRowsItem + (h + 1) * kHalf)); };
@@ -268,7 +289,8 @@ __global__ void __launch_bounds__(kAcThreads, 1) k_attn_chunk(const __grid_const
       }
     } else if (warp < 4) {
       // ---------------------------------------------------------- MMA issuer of a half
-      const int h = warp - 2;
+      const int h = uniform(warp) - 2;
+      const uint32_t one = elect_one() ? 1u : 0u;
       const uint32_t idesc_s = idesc_bf16_f32(kHalf, kCT);
       const uint32_t idesc_o = idesc_bf16_f32(kHalf, D) | (1u << 16);   // bit 16: B is MN-major
       const uint32_t vblock = (uint32_t)box * 128u;
@@ -296,24 +318,21 @@ __global__ void __launch_bounds__(kAcThreads, 1) k_attn_chunk(const __grid_const
         }
       };
       const auto issue_s = [&](uint32_t buf) {
-        if (elect_one()) {
-          const uint32_t b = k_lo + ks * (C::kOpBytes >> 4), d = t_s + buf * kCT;
+        const uint32_t b = k_lo + ks * (C::kOpBytes >> 4), d = t_s + buf * kCT;
 #pragma unroll
-          for (int kk = 0; kk < D / 16; ++kk)
-            mma_bf16_ss(d, desc(q_lo + (((kk >> 2) * (kHalf * 128) + (kk & 3) * 32) >> 4)),
-                        desc(b + (((kk >> 2) * (kCT * 128) + (kk & 3) * 32) >> 4)), idesc_s, kk == 0 ? 0u : 1u);
-          mma_commit(&s_bar[h][buf]);
-          mma_commit(&kempty_bar[ks]);
-        }
-        __syncwarp();
+        for (int kk = 0; kk < D / 16; ++kk)
+          mma_ss(d, desc(q_lo + (((kk >> 2) * (kHalf * 128) + (kk & 3) * 32) >> 4)),
+                 desc(b + (((kk >> 2) * (kCT * 128) + (kk & 3) * 32) >> 4)), idesc_s, kk == 0 ? 0u : 1u, one);
+        commit_to(&s_bar[h][buf], one);
+        commit_to(&kempty_bar[ks], one);
       };
       while (ok) {
         if (!wait_warp(&seg_full[sg], sph)) break;
         const Segment g = segs[sg];
         next_seg();
         if (g.r < 0) break;
-        const int n_units = g.tb - g.ta;
-        const int units = h < halves(g) ? max(0, half_end(g, h) - g.ta) : 0;   // this half's
+        const int n_units = uniform(g.tb - g.ta);
+        const int units = uniform(h < halves(g) ? max(0, half_end(g, h) - g.ta) : 0);   // this half's
         if (!wait_warp(&kfull_bar[ks], kph)) break;
         if (units > 0) {
           if (!wait_warp(&q_bar[h], qph)) break;
@@ -348,14 +367,11 @@ __global__ void __launch_bounds__(kAcThreads, 1) k_attn_chunk(const __grid_const
               break;
             }
             tc_fence_after();
-            if (elect_one()) {
-              const uint32_t v = v_lo + vs * (C::kOpBytes >> 4), p = t_s + (n & 1u) * kCT;
+            const uint32_t v = v_lo + vs * (C::kOpBytes >> 4), p = t_s + (n & 1u) * kCT;
 #pragma unroll
-              for (int kk = 0; kk < kCT / 16; ++kk) mma_bf16_ts(t_o, p + 8 * kk, desc(v + v_off[kk]), idesc_o, kk > 0 ? 1u : (uint32_t)u);
-              mma_commit(&o_bar[h]);
-              mma_commit(&vempty_bar[vs]);
-            }
-            __syncwarp();
+            for (int kk = 0; kk < kCT / 16; ++kk) mma_ts(t_o, p + 8 * kk, desc(v + v_off[kk]), idesc_o, kk > 0 ? 1u : (uint32_t)u, one);
+            commit_to(&o_bar[h], one);
+            commit_to(&vempty_bar[vs], one);
             ++n;
           } else if (lane == 0) {
             mbar_arrive(&vempty_bar[vs]);

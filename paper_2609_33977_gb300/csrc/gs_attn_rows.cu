@@ -143,7 +143,7 @@ __global__ void __launch_bounds__(RowsCfg<D, WR>::kThreads, 1) k_attn_rows(const
   volatile int* abort_flag = &abort_s;
   const int chunk_shift = min(P.page_shift, 7), chunk = 1 << chunk_shift;   // rows of a TMA box
   const auto wait_warp = [&](uint64_t* bar, uint32_t parity) {
-    return __all_sync(0xffffffffu, mbar_wait_short(bar, parity, abort_flag, P.err, kArWaitLimitNs)) != 0;
+    return mbar_wait_warp(bar, parity, abort_flag, P.err, kArWaitLimitNs);
   };
 
   if (warp == C::kWarps) {
