@@ -80,8 +80,8 @@ gs_status launch_paged_attention(const gs_paged_cache& c, const gs_seq_batch& b,
     if (st != GS_OK || !k.chunk) return st;
   }
   const uint32_t box = (uint32_t)attn_chunk_box(c.page_size);
-  // keys arrive slab by slab
-  if (!encode_tmap_slabs_bf16(&P.kmap, c.k_dev, D, rows, box, 1u) ||
+  // keys of a page smaller than a unit arrive slab by slab
+  if (!encode_tmap_slabs_bf16(&P.kmap, c.k_dev, D, rows, box, (int)box == attn_chunk_tile() ? slabs : 1u) ||
       !encode_tmap_slabs_bf16(&P.vmap, c.v_dev, D, rows, box, slabs))
     return GS_ERR_CUDA;
   P.min_rows = k.few ? attn_rows_most() + 1 : 1;

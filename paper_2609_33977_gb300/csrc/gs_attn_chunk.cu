@@ -8,20 +8,19 @@
 //     S = Q K^T (tcgen05, both operands in shared memory, S in TMEM), the thread
 //     reads its row of S, writes P = exp2(c S - m) over it as bf16, and
 //     O += P V (A = P in TMEM, B = V as stored, i.e. MN-major), O stays in TMEM.
-// S is formed for two units at once: a product of 64 keys takes 100 cycles a 16-deep
-// step where one of 128 takes 80.  P V follows unit by unit, under the second unit's
-// exponentials; each half has its own MMA warp.  (S of single units in turn, so that
-// the next is there early, was a fifth slower: the tensor cores had no time left.)
+// P has its own columns (two buffers), so that S of the next unit can be formed as
+// soon as this one has been read, under its exponentials; each half has its own MMA
+// warp.  (P over S, in units of 64 or 128 keys, chains S, exponentials and P V
+// behind each other: 1.3 to 2 times the time.)
 // O is rescaled only when a row's maximum grew by more than 2^8 (each row for
 // itself), else the old maximum stays in use: exact, since both the sum and O carry it.
 //
-// Keys and values arrive page by page (TMA), in two slots of 128 keys and six of 64
-// values.  Values
+// Keys and values arrive page by page (TMA) in rings of five 16 KB slots each.  Values
 // of a unit that some row does not see are looked over first: rows past the sequence's
 // end become zeros, and infinities and NaN are taken out (a weight of zero would not
 // silence them) and added at the end to the rows that see them.
 //
-// TMEM: S of the halves at columns 0, 64 and 128, 192, O at 256 and 384.
+// TMEM: per half S (64 columns) and two P (32 each) from column 0 / 128, O from 256 / 384.
 #include "gs_attn.cuh"
 
 namespace gs {
@@ -31,8 +30,7 @@ using namespace sm100;
 constexpr int kCT = 64;                        // keys of a unit
 constexpr int kHalf = 128, kRowsItem = 256;
 constexpr int kAcThreads = 512;                // warps: keys, values, two MMA; four value checkers; two softmax warpgroups
-constexpr int kPair = 2 * kCT;                 // keys of one S
-constexpr int kKeySlots = 2, kValSlots = 6;    // of kPair keys, of kCT values
+constexpr int kRing = 5;                       // slots of keys, and as many of values
 constexpr int kSegs = 4;
 constexpr uint64_t kAcWaitLimitNs = 2000000000ull;
 constexpr int kRegsOther = 56, kRegsSoftmax = 200;
@@ -55,9 +53,9 @@ struct ChunkTraits {
 
 template <int D>
 struct ChunkCfg {
-  static constexpr int kValBytes = kCT * D * 2, kKeyBytes = kPair * D * 2;   // of a slot
+  static constexpr int kOpBytes = kCT * D * 2;         // a unit's keys or values
   static constexpr int kQBytes = kHalf * D * 2;        // a half's queries
-  static constexpr int kSmem = 2 * kQBytes + kKeySlots * kKeyBytes + kValSlots * kValBytes + 1024;
+  static constexpr int kSmem = 2 * kQBytes + 2 * kRing * kOpBytes + 1024;
   static constexpr int kSlabs = D / 64;
 };
 
@@ -134,14 +132,15 @@ template <int D>
 __global__ void __launch_bounds__(kAcThreads, 1) k_attn_chunk(const __grid_constant__ AttnParams P) {
   using C = ChunkCfg<D>;
   extern __shared__ uint8_t ac_smem_raw[];
-  __shared__ __align__(8) uint64_t kfull_bar[kKeySlots], kempty_bar[kKeySlots];   // keys: bytes have landed, slot is free
-  __shared__ __align__(8) uint64_t vfull_bar[kValSlots], vempty_bar[kValSlots];   // values
-  __shared__ __align__(8) uint64_t clean_bar[kValSlots];                          // values looked over
+  __shared__ __align__(8) uint64_t kfull_bar[kRing], kempty_bar[kRing];   // keys: bytes have landed, slot is free
+  __shared__ __align__(8) uint64_t vfull_bar[kRing], vempty_bar[kRing];   // values
+  __shared__ __align__(8) uint64_t clean_bar[kRing];                      // values looked over
   __shared__ __align__(8) uint64_t seg_full[kSegs], seg_empty[kSegs];
   __shared__ __align__(8) uint64_t q_bar[2];           // a half's queries are in shared memory
-  __shared__ __align__(8) uint64_t s_bar[2];           // S of one or two units is in TMEM
-  __shared__ __align__(8) uint64_t p_bar[2][2];        // P is in TMEM, O is rescaled
-  __shared__ __align__(8) uint64_t o_bar[2];           // P V is done
+  __shared__ __align__(8) uint64_t s_bar[2];           // S is in TMEM (and the product before the last P V is over)
+  __shared__ __align__(8) uint64_t sfree_bar[2];       // S has been read
+  __shared__ __align__(8) uint64_t p_bar[2][2];        // [half][buffer]: P is in TMEM, O is rescaled
+  __shared__ __align__(8) uint64_t o_bar[2][2];        // [half][buffer]: P V is over
   __shared__ __align__(8) uint64_t join_bar[2];
   __shared__ __align__(8) uint64_t drain_bar[2];
   __shared__ Segment segs[kSegs];
@@ -150,15 +149,13 @@ __global__ void __launch_bounds__(kAcThreads, 1) k_attn_chunk(const __grid_const
   __shared__ int abort_s, bad_s[kSegs], last_s[2];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(ac_smem_raw) + 1023) & ~uintptr_t(1023));
   uint8_t* ring_k = smem + 2 * C::kQBytes;
-  uint8_t* ring_v = ring_k + kKeySlots * C::kKeyBytes;
+  uint8_t* ring_v = ring_k + kRing * C::kOpBytes;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int cta = (int)blockIdx.x;
   if (threadIdx.x == 0) {
-    for (int s = 0; s < kKeySlots; ++s) {
+    for (int s = 0; s < kRing; ++s) {
       mbar_init(&kfull_bar[s], 1);
       mbar_init(&kempty_bar[s], 2);   // both MMA warps
-    }
-    for (int s = 0; s < kValSlots; ++s) {
       mbar_init(&vfull_bar[s], 1);
       mbar_init(&vempty_bar[s], 2);
       mbar_init(&clean_bar[s], 4);
@@ -170,8 +167,11 @@ __global__ void __launch_bounds__(kAcThreads, 1) k_attn_chunk(const __grid_const
     for (int h = 0; h < 2; ++h) {
       mbar_init(&q_bar[h], 4);
       mbar_init(&s_bar[h], 1);
-      for (int b = 0; b < 2; ++b) mbar_init(&p_bar[h][b], 4);
-      mbar_init(&o_bar[h], 1);
+      mbar_init(&sfree_bar[h], 4);
+      for (int b = 0; b < 2; ++b) {
+        mbar_init(&p_bar[h][b], 4);
+        mbar_init(&o_bar[h][b], 1);
+      }
       mbar_init(&join_bar[h], 4);
     }
     mbar_init(&drain_bar[0], 1);
@@ -216,14 +216,9 @@ __global__ void __launch_bounds__(kAcThreads, 1) k_attn_chunk(const __grid_const
       Walker<ChunkTraits> walk(P, shares, work, cta);
       Segment g;
       const int32_t no_row = (int32_t)((P.pages * P.kv_heads) << P.page_shift);   // past the last: reads as zeros
-      const auto entry = [&](int64_t trow, int len, int e) {
-        return e < P.width && ((int64_t)e << P.page_shift) < len ? __ldg(P.table + trow + e) : -1;
-      };
       uint64_t* full_bar = keys ? kfull_bar : vfull_bar;
       uint64_t* empty_bar = keys ? kempty_bar : vempty_bar;
       uint8_t* ring = keys ? ring_k : ring_v;
-      const int per = keys ? kPair : kCT;                       // keys of a slot
-      const uint32_t slots = keys ? kKeySlots : kValSlots, slot_bytes = keys ? C::kKeyBytes : C::kValBytes;
       uint32_t slot = 0, ph = 1u;
       bool ok = true;
       while (ok) {
@@ -250,20 +245,18 @@ __global__ void __launch_bounds__(kAcThreads, 1) k_attn_chunk(const __grid_const
         }
         const int len = g.s.len();
         const int64_t trow = (int64_t)g.r * P.width;
-        int held = -1, page = -1, page2 = -1;   // lane i holds table entries 32 held + i and + 32
-        for (int key0 = g.ta * kCT; key0 < g.tb * kCT; key0 += per) {
-          const int valid = min(min(per, g.tb * kCT - key0), max(0, len - key0));
-          const int boxes = (valid + box - 1) >> box_shift;   // at most 8
-          const int key = key0 + ((lane & 7) << box_shift), e = key >> P.page_shift;
-          // the boxes' table entries lie within two blocks of 32 (a segment may begin at any unit)
-          const int e0 = key0 >> P.page_shift;
+        int held = -1, page = -1;   // lane i holds table entry 32 held + i
+        for (int t = g.ta; t < g.tb; ++t) {
+          const int valid = min(kCT, max(0, len - t * kCT));
+          const int boxes = (valid + box - 1) >> box_shift;   // at most 4
+          const int e0 = (t * kCT) >> P.page_shift;
           if (e0 >> 5 != held) {
             held = e0 >> 5;
-            page = entry(trow, len, 32 * held + lane);
-            page2 = entry(trow, len, 32 * held + 32 + lane);
+            const int e = 32 * held + lane;
+            page = e < P.width && ((int64_t)e << P.page_shift) < len ? __ldg(P.table + trow + e) : -1;
           }
-          const int pg1 = __shfl_sync(0xffffffffu, page, e & 31), pg2 = __shfl_sync(0xffffffffu, page2, e & 31);
-          const int pg = e >> 5 == held ? pg1 : pg2;
+          const int key = t * kCT + ((lane & 3) << box_shift);
+          const int pg = __shfl_sync(0xffffffffu, page, (key >> P.page_shift) & 31);
           const int32_t row = pg >= 0 && pg < P.pages
                                   ? (int32_t)((((int64_t)pg * P.kv_heads + g.h) << P.page_shift) + (key & ((1 << P.page_shift) - 1)))
                                   : no_row;
@@ -271,24 +264,26 @@ __global__ void __launch_bounds__(kAcThreads, 1) k_attn_chunk(const __grid_const
             ok = false;
             break;
           }
-          uint8_t* dst = ring + slot * slot_bytes;
+          uint8_t* dst = ring + slot * C::kOpBytes;
           uint64_t* full = &full_bar[slot];
           if (elect_one()) mbar_arrive_expect_tx(full, (uint32_t)(boxes * box * D * 2));
           __syncwarp();
-          // Keys: slabs of 64 channels x 128 keys.  Values: box after box, each with its slabs.
+          // Keys: slabs of 64 channels x 64 keys.  Values: box after box, each with its slabs.
           for (int b = 0; b < boxes; ++b) {
             const int32_t r = __shfl_sync(0xffffffffu, row, b);
             if (elect_one()) {
               if (!keys) {
                 tma_load_3d(dst + b * (box * D * 2), &P.vmap, full, 0, r, 0);
+              } else if (box == kCT) {
+                tma_load_3d(dst, &P.kmap, full, 0, r, 0);
               } else {
 #pragma unroll
-                for (int sl = 0; sl < C::kSlabs; ++sl) tma_load_3d(dst + sl * (kPair * 128) + b * (box * 128), &P.kmap, full, 0, r, sl);
+                for (int sl = 0; sl < C::kSlabs; ++sl) tma_load_3d(dst + sl * (kCT * 128) + b * (box * 128), &P.kmap, full, 0, r, sl);
               }
             }
             __syncwarp();
           }
-          if (++slot == slots) {
+          if (++slot == kRing) {
             slot = 0;
             ph ^= 1u;
           }
@@ -298,7 +293,7 @@ __global__ void __launch_bounds__(kAcThreads, 1) k_attn_chunk(const __grid_const
       // ---------------------------------------------------------- MMA issuer of a half
       const int h = uniform(warp) - 2;
       const uint32_t one = elect_one() ? 1u : 0u;
-      const uint32_t idesc_s[2] = {idesc_bf16_f32(kHalf, kCT), idesc_bf16_f32(kHalf, kPair)};
+      const uint32_t idesc_s = idesc_bf16_f32(kHalf, kCT);
       const uint32_t idesc_o = idesc_bf16_f32(kHalf, D) | (1u << 16);   // bit 16: B is MN-major
       const uint32_t vblock = (uint32_t)box * 128u;
       const uint32_t q_lo = desc_lo(smem_u32(smem + h * C::kQBytes), 16), k_lo = desc_lo(smem_u32(ring_k), 16);
@@ -307,17 +302,36 @@ __global__ void __launch_bounds__(kAcThreads, 1) k_attn_chunk(const __grid_const
 #pragma unroll
       for (int kk = 0; kk < kCT / 16; ++kk)
         v_off[kk] = ((uint32_t)((16 * kk) >> box_shift) * (vblock * C::kSlabs) + (uint32_t)((16 * kk) & (box - 1)) * 128u) >> 4;
-      const uint32_t t_s = tmem + h * 128, t_o = tmem + 256 + h * 128;
-      // np[b]: units of buffer b so far, no: all units.  S of a pair goes over both P of the pair before: their products
-      // are over by then.  Every product is waited for once, before the next one or the next S.
-      uint32_t np[2] = {0u, 0u}, no = 0, seen = 0, qph = 0u, ks = 0, kph = 0u, vs = 0, vph = 0u;
+      const uint32_t t_s = tmem + h * 128, t_p = t_s + kCT, t_o = tmem + 256 + h * 128;
+      // Units are counted over all segments (n): the n-th P is in buffer n & 1, which P V of unit n - 2 has read before
+      // S of unit n is announced (a commit covers everything issued before it).
+      uint32_t n = 0, ns = 0, qph = 0u, ks = 0, kph = 0u, vs = 0, vph = 0u;   // ns: S issued
       bool ok = true;
-      const auto product_over = [&]() {   // the last one
-        if (seen == no) return true;
-        const bool over = wait_warp(&o_bar[h], seen & 1u);
-        ++seen;
-        tc_fence_after();
-        return over;
+      // S of the segment's unit u, or this half's part of handing its keys back
+      const auto next_s = [&](int u, int units) {
+        bool good = wait_warp(&kfull_bar[ks], kph);
+        if (u < units) {
+          if (ns > 0u) good = good && wait_warp(&sfree_bar[h], (ns - 1u) & 1u);
+          tc_fence_after();
+          if (good) {
+            const uint32_t b = k_lo + ks * (C::kOpBytes >> 4);
+#pragma unroll
+            for (int kk = 0; kk < D / 16; ++kk)
+              mma_ss(t_s, desc(q_lo + (((kk >> 2) * (kHalf * 128) + (kk & 3) * 32) >> 4)),
+                     desc(b + (((kk >> 2) * (kCT * 128) + (kk & 3) * 32) >> 4)), idesc_s, kk == 0 ? 0u : 1u, one);
+            commit_to(&s_bar[h], one);
+            commit_to(&kempty_bar[ks], one);
+          }
+          ++ns;
+        } else if (lane == 0) {
+          mbar_arrive(&kempty_bar[ks]);
+        }
+        __syncwarp();
+        if (++ks == kRing) {
+          ks = 0;
+          kph ^= 1u;
+        }
+        return good;
       };
       while (ok) {
         if (!wait_warp(&seg_full[sg], sph)) break;
@@ -329,53 +343,28 @@ __global__ void __launch_bounds__(kAcThreads, 1) k_attn_chunk(const __grid_const
         if (units > 0) {
           ok = wait_warp(&q_bar[h], qph);
           qph ^= 1u;
-          tc_fence_after();
         }
-        for (int u0 = 0; u0 < n_units && ok; u0 += 2) {
-          ok = wait_warp(&kfull_bar[ks], kph);
-          if (u0 < units && ok) {
-            ok = product_over();
+        ok = ok && next_s(0, units);
+        for (int u = 0; u < n_units && ok; ++u) {
+          if (u + 1 < n_units) ok = next_s(u + 1, units);
+          ok = ok && wait_warp(&clean_bar[vs], vph);
+          if (u < units && ok) {
+            ok = wait_warp(&p_bar[h][n & 1u], (n >> 1) & 1u);
             if (!ok) break;
             tc_fence_after();
-            const uint32_t b = k_lo + ks * (C::kKeyBytes >> 4), idesc = u0 + 1 < units ? idesc_s[1] : idesc_s[0];
+            const uint32_t v = v_lo + vs * (C::kOpBytes >> 4), p = t_p + (n & 1u) * (kCT / 2);
 #pragma unroll
-            for (int kk = 0; kk < D / 16; ++kk)
-              mma_ss(t_s, desc(q_lo + (((kk >> 2) * (kHalf * 128) + (kk & 3) * 32) >> 4)),
-                     desc(b + (((kk >> 2) * (kPair * 128) + (kk & 3) * 32) >> 4)), idesc, kk == 0 ? 0u : 1u, one);
-            commit_to(&s_bar[h], one);
-            commit_to(&kempty_bar[ks], one);
+            for (int kk = 0; kk < kCT / 16; ++kk) mma_ts(t_o, p + 8 * kk, desc(v + v_off[kk]), idesc_o, kk > 0 ? 1u : (uint32_t)u, one);
+            commit_to(&o_bar[h][n & 1u], one);
+            commit_to(&vempty_bar[vs], one);
+            ++n;
           } else if (lane == 0) {
-            mbar_arrive(&kempty_bar[ks]);   // this half's part of handing the slot back
+            mbar_arrive(&vempty_bar[vs]);
           }
           __syncwarp();
-          if (++ks == kKeySlots) {
-            ks = 0;
-            kph ^= 1u;
-          }
-#pragma unroll
-          for (int b = 0; b < 2; ++b) {
-            const int u = u0 + b;
-            if (u >= n_units || !ok) break;
-            ok = wait_warp(&clean_bar[vs], vph);
-            if (u < units) {
-              ok = ok && wait_warp(&p_bar[h][b], np[b] & 1u) && product_over();
-              if (!ok) break;
-              tc_fence_after();
-              const uint32_t v = v_lo + vs * (C::kValBytes >> 4), p = t_s + b * kCT;
-#pragma unroll
-              for (int kk = 0; kk < kCT / 16; ++kk) mma_ts(t_o, p + 8 * kk, desc(v + v_off[kk]), idesc_o, kk > 0 ? 1u : (uint32_t)u, one);
-              commit_to(&o_bar[h], one);
-              commit_to(&vempty_bar[vs], one);
-              ++np[b];
-              ++no;
-            } else if (lane == 0) {
-              mbar_arrive(&vempty_bar[vs]);
-            }
-            __syncwarp();
-            if (++vs == kValSlots) {
-              vs = 0;
-              vph ^= 1u;
-            }
+          if (++vs == kRing) {
+            vs = 0;
+            vph ^= 1u;
           }
         }
       }
@@ -403,7 +392,7 @@ __global__ void __launch_bounds__(kAcThreads, 1) k_attn_chunk(const __grid_const
           }
           const int key0 = t * kCT;
           if (key0 + kCT > all_see) {
-            const uint32_t v = smem_u32(ring_v + vs * C::kValBytes);
+            const uint32_t v = smem_u32(ring_v + vs * C::kOpBytes);
             constexpr int kPieces = D / 8, kStep = 32 / kPieces, kDeep = 16 / kStep;   // keys of a step of the warp; steps at once
             const int end = min(kCT, max(0, len - key0)), piece = lane % kPieces;
             bool bad = false;
@@ -439,7 +428,7 @@ __global__ void __launch_bounds__(kAcThreads, 1) k_attn_chunk(const __grid_const
           }
           __syncwarp();
           if (lane == 0) mbar_arrive(&clean_bar[vs]);
-          if (++vs == kValSlots) {
+          if (++vs == kRing) {
             vs = 0;
             vph ^= 1u;
           }
@@ -454,7 +443,7 @@ __global__ void __launch_bounds__(kAcThreads, 1) k_attn_chunk(const __grid_const
     const int h = (warp - 8) >> 2, quarter = warp & 3;
     const uint32_t lane_base = (uint32_t)(32 * quarter) << 16;
     const uint32_t ts = tmem + h * 128 + lane_base, to = tmem + 256 + h * 128 + lane_base;
-    uint32_t sg = 0, sph = 0, n = 0, j_ph = 0u, s_ph = 0u;   // n: units so far
+    uint32_t sg = 0, sph = 0, n = 0, j_ph = 0u;   // n: units so far
     const auto meet = [&]() {   // the warpgroup's barrier, bounded like every wait
       __syncwarp();
       if (lane == 0) mbar_arrive(&join_bar[h]);
@@ -532,21 +521,20 @@ __global__ void __launch_bounds__(kAcThreads, 1) k_attn_chunk(const __grid_const
       float m = -INFINITY, l = 0.f;
       bool ok = true;
       for (int t = g.ta; t < end; ++t, ++n) {
-        const uint32_t buf = (uint32_t)(t - g.ta) & 1u, sb = ts + buf * kCT;
-        if (buf == 0u) {
-          if (!wait_warp(&s_bar[h], s_ph)) {
-            ok = false;
-            break;
-          }
-          s_ph ^= 1u;
-          tc_fence_after();
+        if (!wait_warp(&s_bar[h], n & 1u)) {
+          ok = false;
+          break;
         }
+        tc_fence_after();
         uint32_t s[2][32];
-        tmem_ld_x32(sb, s[0]);
-        tmem_ld_x32(sb + 32, s[1]);
+        tmem_ld_x32(ts, s[0]);
+        tmem_ld_x32(ts + 32, s[1]);
         tmem_wait_ld();
         reg_fence(s[0]);
         reg_fence(s[1]);
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&sfree_bar[h]);
         const int key0 = t * kCT;
         if (key0 + kCT > all_see) {
           const int v = row.vis - key0;
@@ -570,11 +558,8 @@ __global__ void __launch_bounds__(kAcThreads, 1) k_attn_chunk(const __grid_const
           f = ex2((m - mt) * c);
           m = mt;
         }
-        // The product before is waited for once a unit (a barrier that moved twice between two waits would look as if it
-        // had not): here if O has to be rescaled, else after the exponentials.
-        const bool rescale = t > g.ta && __any_sync(0xffffffffu, f != 1.f);
-        if (rescale) {
-          if (!wait_warp(&o_bar[h], (n - 1u) & 1u)) {
+        if (t > g.ta && __any_sync(0xffffffffu, f != 1.f)) {
+          if (!wait_warp(&o_bar[h][(n - 1u) & 1u], ((n - 1u) >> 1) & 1u)) {   // the product before is in O
             ok = false;
             break;
           }
@@ -603,15 +588,11 @@ __global__ void __launch_bounds__(kAcThreads, 1) k_attn_chunk(const __grid_const
             s[i][e + 1] = __float_as_uint(ex2(__uint_as_float(b)));
             p[16 * i + e / 2] = pack_bf16(__uint_as_float(s[i][e]), __uint_as_float(s[i][e + 1]));
           }
-        if (t > g.ta && !rescale && !wait_warp(&o_bar[h], (n - 1u) & 1u)) {
-          ok = false;
-          break;
-        }
-        tmem_st_x32(sb, p);
+        tmem_st_x32(ts + kCT + (n & 1u) * (kCT / 2), p);
         tmem_wait_st();
         tc_fence_before();
         __syncwarp();
-        if (lane == 0) mbar_arrive(&p_bar[h][buf]);
+        if (lane == 0) mbar_arrive(&p_bar[h][n & 1u]);
         uint64_t sum[4] = {0ull, 0ull, 0ull, 0ull};
 #pragma unroll
         for (int i = 0; i < 4; ++i)
@@ -634,7 +615,7 @@ __global__ void __launch_bounds__(kAcThreads, 1) k_attn_chunk(const __grid_const
       // ---- this segment's result
       float o[D];
       if (g.ta < end) {
-        if (!wait_warp(&o_bar[h], (n - 1u) & 1u)) break;
+        if (!wait_warp(&o_bar[h][(n - 1u) & 1u], ((n - 1u) >> 1) & 1u)) break;
         tc_fence_after();
         uint32_t v[D / 32][32];
 #pragma unroll
