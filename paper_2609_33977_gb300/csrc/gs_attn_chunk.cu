@@ -9,8 +9,9 @@
 //     reads its row of S, writes P = exp2(c S - m) over it as bf16, and
 //     O += P V (A = P in TMEM, B = V as stored, i.e. MN-major), O stays in TMEM.
 // P has its own columns (two buffers), so that S of the next unit can be formed as
-// soon as this one has been read, under its exponentials; each half has its own MMA
-// warp.  (P over S, in units of 64 or 128 keys, chains S, exponentials and P V
+// soon as this one has been read, under its exponentials.  Each half has two MMA
+// warps, for S and for P V: a warp's waits and issue of both in turn took longer than
+// the exponentials.  (P over S, in units of 64 or 128 keys, chains S, exponentials and P V
 // behind each other: 1.3 to 2 times the time.)
 // O is rescaled only when a row's maximum grew by more than 2^8 (each row for
 // itself), else the old maximum stays in use: exact, since both the sum and O carry it.
@@ -29,9 +30,10 @@ using namespace sm100;
 
 constexpr int kCT = 64;                        // keys of a unit
 constexpr int kHalf = 128, kRowsItem = 256;
-constexpr int kAcThreads = 512;                // warps: keys, values, two MMA; four value checkers; two softmax warpgroups
+constexpr int kAcThreads = 512;                // warps: keys, values, S x 2, P V x 2, two value checkers; two softmax warpgroups
 constexpr int kRing = 5;                       // slots of keys, and as many of values
 constexpr int kSegs = 4;
+constexpr int kCheckers = 2;
 constexpr uint64_t kAcWaitLimitNs = 2000000000ull;
 constexpr int kRegsOther = 56, kRegsSoftmax = 200;
 static_assert(8 * 32 * (kRegsOther + kRegsSoftmax) <= kAcThreads * 128, "register split");
@@ -128,6 +130,13 @@ __device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
   return d;
 }
 
+// two bf16: 0 x + c
+__device__ __forceinline__ uint32_t times_zero(uint32_t x, uint32_t c) {
+  uint32_t d;
+  asm("fma.rn.bf16x2 %0, %1, %2, %3;" : "=r"(d) : "r"(x), "r"(0u), "r"(c));
+  return d;
+}
+
 template <int D>
 __global__ void __launch_bounds__(kAcThreads, 1) k_attn_chunk(const __grid_constant__ AttnParams P) {
   using C = ChunkCfg<D>;
@@ -137,12 +146,12 @@ __global__ void __launch_bounds__(kAcThreads, 1) k_attn_chunk(const __grid_const
   __shared__ __align__(8) uint64_t clean_bar[kRing];                      // values looked over
   __shared__ __align__(8) uint64_t seg_full[kSegs], seg_empty[kSegs];
   __shared__ __align__(8) uint64_t q_bar[2];           // a half's queries are in shared memory
-  __shared__ __align__(8) uint64_t s_bar[2];           // S is in TMEM (and the product before the last P V is over)
+  __shared__ __align__(8) uint64_t s_bar[2];           // S is in TMEM (and the P V is over whose P this unit's replaces)
   __shared__ __align__(8) uint64_t sfree_bar[2];       // S has been read
   __shared__ __align__(8) uint64_t p_bar[2][2];        // [half][buffer]: P is in TMEM, O is rescaled
   __shared__ __align__(8) uint64_t o_bar[2][2];        // [half][buffer]: P V is over
   __shared__ __align__(8) uint64_t join_bar[2];
-  __shared__ __align__(8) uint64_t drain_bar[2];
+  __shared__ __align__(8) uint64_t drain_bar[4];
   __shared__ Segment segs[kSegs];
   __shared__ WorkShared work;
   __shared__ uint32_t tmem_base_s;
@@ -158,7 +167,7 @@ __global__ void __launch_bounds__(kAcThreads, 1) k_attn_chunk(const __grid_const
       mbar_init(&kempty_bar[s], 2);   // both MMA warps
       mbar_init(&vfull_bar[s], 1);
       mbar_init(&vempty_bar[s], 2);
-      mbar_init(&clean_bar[s], 4);
+      mbar_init(&clean_bar[s], kCheckers);
     }
     for (int s = 0; s < kSegs; ++s) {
       mbar_init(&seg_full[s], 1);
@@ -174,8 +183,7 @@ __global__ void __launch_bounds__(kAcThreads, 1) k_attn_chunk(const __grid_const
       }
       mbar_init(&join_bar[h], 4);
     }
-    mbar_init(&drain_bar[0], 1);
-    mbar_init(&drain_bar[1], 1);
+    for (int i = 0; i < 4; ++i) mbar_init(&drain_bar[i], 1);
     abort_s = 0;
     fence_mbar_init();
     prefetch_tmap(&P.kmap);
@@ -289,96 +297,102 @@ __global__ void __launch_bounds__(kAcThreads, 1) k_attn_chunk(const __grid_const
           }
         }
       }
-    } else if (warp < 4) {
-      // ---------------------------------------------------------- MMA issuer of a half
-      const int h = uniform(warp) - 2;
+    } else if (warp < 6) {
+      // ---------------------------------------------------------- MMA issuers: S of half 0, 1, P V of half 0, 1
+      const int role = uniform(warp) - 2, h = role & 1;
       const uint32_t one = elect_one() ? 1u : 0u;
-      const uint32_t idesc_s = idesc_bf16_f32(kHalf, kCT);
-      const uint32_t idesc_o = idesc_bf16_f32(kHalf, D) | (1u << 16);   // bit 16: B is MN-major
-      const uint32_t vblock = (uint32_t)box * 128u;
-      const uint32_t q_lo = desc_lo(smem_u32(smem + h * C::kQBytes), 16), k_lo = desc_lo(smem_u32(ring_k), 16);
-      const uint32_t v_lo = desc_lo(smem_u32(ring_v), vblock);
-      uint32_t v_off[kCT / 16];   // of 16 keys in a slot
-#pragma unroll
-      for (int kk = 0; kk < kCT / 16; ++kk)
-        v_off[kk] = ((uint32_t)((16 * kk) >> box_shift) * (vblock * C::kSlabs) + (uint32_t)((16 * kk) & (box - 1)) * 128u) >> 4;
       const uint32_t t_s = tmem + h * 128, t_p = t_s + kCT, t_o = tmem + 256 + h * 128;
-      // Units are counted over all segments (n): the n-th P is in buffer n & 1, which P V of unit n - 2 has read before
-      // S of unit n is announced (a commit covers everything issued before it).
-      uint32_t n = 0, ns = 0, qph = 0u, ks = 0, kph = 0u, vs = 0, vph = 0u;   // ns: S issued
+      // Units are counted over all segments (n); P of unit n is in buffer n & 1.
+      uint32_t n = 0, slot = 0, ph = 0u;
       bool ok = true;
-      // S of the segment's unit u, or this half's part of handing its keys back
-      const auto next_s = [&](int u, int units) {
-        bool good = wait_warp(&kfull_bar[ks], kph);
-        if (u < units) {
-          if (ns > 0u) good = good && wait_warp(&sfree_bar[h], (ns - 1u) & 1u);
-          tc_fence_after();
-          if (good) {
-            const uint32_t b = k_lo + ks * (C::kOpBytes >> 4);
-#pragma unroll
-            for (int kk = 0; kk < D / 16; ++kk)
-              mma_ss(t_s, desc(q_lo + (((kk >> 2) * (kHalf * 128) + (kk & 3) * 32) >> 4)),
-                     desc(b + (((kk >> 2) * (kCT * 128) + (kk & 3) * 32) >> 4)), idesc_s, kk == 0 ? 0u : 1u, one);
-            commit_to(&s_bar[h], one);
-            commit_to(&kempty_bar[ks], one);
-          }
-          ++ns;
-        } else if (lane == 0) {
-          mbar_arrive(&kempty_bar[ks]);
+      const auto next_slot = [&]() {
+        if (++slot == kRing) {
+          slot = 0;
+          ph ^= 1u;
         }
-        __syncwarp();
-        if (++ks == kRing) {
-          ks = 0;
-          kph ^= 1u;
-        }
-        return good;
       };
-      while (ok) {
-        if (!wait_warp(&seg_full[sg], sph)) break;
-        const Segment g = segs[sg];
-        next_seg();
-        if (g.r < 0) break;
-        const int n_units = uniform(g.tb - g.ta);
-        const int units = uniform(h < halves(g) ? max(0, half_end(g, h) - g.ta) : 0);   // this half's
-        if (units > 0) {
-          ok = wait_warp(&q_bar[h], qph);
-          qph ^= 1u;
-        }
-        ok = ok && next_s(0, units);
-        for (int u = 0; u < n_units && ok; ++u) {
-          if (u + 1 < n_units) ok = next_s(u + 1, units);
-          ok = ok && wait_warp(&clean_bar[vs], vph);
-          if (u < units && ok) {
-            ok = wait_warp(&p_bar[h][n & 1u], (n >> 1) & 1u);
-            if (!ok) break;
-            tc_fence_after();
-            const uint32_t v = v_lo + vs * (C::kOpBytes >> 4), p = t_p + (n & 1u) * (kCT / 2);
-#pragma unroll
-            for (int kk = 0; kk < kCT / 16; ++kk) mma_ts(t_o, p + 8 * kk, desc(v + v_off[kk]), idesc_o, kk > 0 ? 1u : (uint32_t)u, one);
-            commit_to(&o_bar[h][n & 1u], one);
-            commit_to(&vempty_bar[vs], one);
-            ++n;
-          } else if (lane == 0) {
-            mbar_arrive(&vempty_bar[vs]);
+      const auto over = [&](uint32_t unit) { return wait_warp(&o_bar[h][unit & 1u], (unit >> 1) & 1u); };
+      if (role < 2) {
+        const uint32_t idesc = idesc_bf16_f32(kHalf, kCT);
+        const uint32_t q_lo = desc_lo(smem_u32(smem + h * C::kQBytes), 16), k_lo = desc_lo(smem_u32(ring_k), 16);
+        uint32_t qph = 0u;
+        while (ok) {
+          if (!wait_warp(&seg_full[sg], sph)) break;
+          const Segment g = segs[sg];
+          next_seg();
+          if (g.r < 0) break;
+          const int n_units = uniform(g.tb - g.ta);
+          const int units = uniform(h < halves(g) ? max(0, half_end(g, h) - g.ta) : 0);   // this half's
+          if (units > 0) {
+            ok = wait_warp(&q_bar[h], qph);
+            qph ^= 1u;
           }
-          __syncwarp();
-          if (++vs == kRing) {
-            vs = 0;
-            vph ^= 1u;
+          for (int u = 0; u < n_units && ok; ++u) {
+            ok = wait_warp(&kfull_bar[slot], ph);
+            if (u < units) {
+              ok = ok && (n == 0u || wait_warp(&sfree_bar[h], (n - 1u) & 1u)) && (n < 2u || over(n - 2u));
+              if (!ok) break;
+              tc_fence_after();
+              const uint32_t b = k_lo + slot * (C::kOpBytes >> 4);
+#pragma unroll
+              for (int kk = 0; kk < D / 16; ++kk)
+                mma_ss(t_s, desc(q_lo + (((kk >> 2) * (kHalf * 128) + (kk & 3) * 32) >> 4)),
+                       desc(b + (((kk >> 2) * (kCT * 128) + (kk & 3) * 32) >> 4)), idesc, kk == 0 ? 0u : 1u, one);
+              commit_to(&s_bar[h], one);
+              commit_to(&kempty_bar[slot], one);
+              ++n;
+            } else if (lane == 0) {
+              mbar_arrive(&kempty_bar[slot]);   // this half's part of handing the slot back
+            }
+            next_slot();
+          }
+        }
+      } else {
+        const uint32_t idesc = idesc_bf16_f32(kHalf, D) | (1u << 16);   // bit 16: B is MN-major
+        const uint32_t vblock = (uint32_t)box * 128u;
+        const uint32_t v_lo = desc_lo(smem_u32(ring_v), vblock);
+        uint32_t v_off[kCT / 16];   // of 16 keys in a slot
+#pragma unroll
+        for (int kk = 0; kk < kCT / 16; ++kk)
+          v_off[kk] = ((uint32_t)((16 * kk) >> box_shift) * (vblock * C::kSlabs) + (uint32_t)((16 * kk) & (box - 1)) * 128u) >> 4;
+        while (ok) {
+          if (!wait_warp(&seg_full[sg], sph)) break;
+          const Segment g = segs[sg];
+          next_seg();
+          if (g.r < 0) break;
+          const int n_units = uniform(g.tb - g.ta);
+          const int units = uniform(h < halves(g) ? max(0, half_end(g, h) - g.ta) : 0);
+          for (int u = 0; u < n_units && ok; ++u) {
+            ok = wait_warp(&clean_bar[slot], ph);
+            if (u < units) {
+              ok = ok && wait_warp(&p_bar[h][n & 1u], (n >> 1) & 1u);
+              if (!ok) break;
+              tc_fence_after();
+              const uint32_t v = v_lo + slot * (C::kOpBytes >> 4), p = t_p + (n & 1u) * (kCT / 2);
+#pragma unroll
+              for (int kk = 0; kk < kCT / 16; ++kk) mma_ts(t_o, p + 8 * kk, desc(v + v_off[kk]), idesc, kk > 0 ? 1u : (uint32_t)u, one);
+              commit_to(&o_bar[h][n & 1u], one);
+              commit_to(&vempty_bar[slot], one);
+              ++n;
+            } else if (lane == 0) {
+              mbar_arrive(&vempty_bar[slot]);
+            }
+            next_slot();
           }
         }
       }
       // whatever was issued is over before TMEM goes back
-      if (elect_one()) {
-        mma_commit(&drain_bar[h]);
-        mbar_wait_bounded(&drain_bar[h], 0u, nullptr, P.err, kAcWaitLimitNs, kDevErrTimeout);
+      __syncwarp();
+      if (one) {
+        mma_commit(&drain_bar[role]);
+        mbar_wait_bounded(&drain_bar[role], 0u, nullptr, P.err, kAcWaitLimitNs, kDevErrTimeout);
       }
       __syncwarp();
     } else {
       // ---------------------------------------------------------- values that some row does not see
       uint32_t vs = 0, vph = 0u;
       bool ok = true;
-      const int mine = warp - 4;
+      const int mine = warp - 6;
       while (ok) {
         if (!wait_warp(&seg_full[sg], sph)) break;
         const Segment g = segs[sg];
@@ -396,9 +410,10 @@ __global__ void __launch_bounds__(kAcThreads, 1) k_attn_chunk(const __grid_const
             constexpr int kPieces = D / 8, kStep = 32 / kPieces, kDeep = 16 / kStep;   // keys of a step of the warp; steps at once
             const int end = min(kCT, max(0, len - key0)), piece = lane % kPieces;
             bool bad = false;
-            for (int k0 = max(0, all_see - key0) + mine * (kDeep * kStep); k0 < kCT; k0 += 4 * kDeep * kStep) {
+            for (int k0 = max(0, all_see - key0) + mine * (kDeep * kStep); k0 < kCT; k0 += kCheckers * kDeep * kStep) {
               uint4 x[kDeep];
               uint32_t at16[kDeep];
+              uint32_t any = 0u;   // bf16 pairs: the sum of 0 x, NaN where some x is an infinity or NaN
 #pragma unroll
               for (int i = 0; i < kDeep; ++i) {
                 // a key's row is kSlabs pieces of 128 bytes; their swizzle does not matter here
@@ -410,6 +425,10 @@ __global__ void __launch_bounds__(kAcThreads, 1) k_attn_chunk(const __grid_const
                              : "r"(at16[i])
                              : "memory");
               }
+#pragma unroll
+              for (int i = 0; i < kDeep; ++i)
+                any = times_zero(x[i].w, times_zero(x[i].z, times_zero(x[i].y, times_zero(x[i].x, any))));
+              if (nonfinite2(any) == 0u && k0 + kDeep * kStep <= end) continue;   // the rule: nothing to do
 #pragma unroll
               for (int i = 0; i < kDeep; ++i) {
                 const int k = k0 + i * kStep + lane / kPieces;
@@ -589,11 +608,7 @@ __global__ void __launch_bounds__(kAcThreads, 1) k_attn_chunk(const __grid_const
             p[16 * i + e / 2] = pack_bf16(__uint_as_float(s[i][e]), __uint_as_float(s[i][e + 1]));
           }
         tmem_st_x32(ts + kCT + (n & 1u) * (kCT / 2), p);
-        tmem_wait_st();
-        tc_fence_before();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(&p_bar[h][n & 1u]);
-        uint64_t sum[4] = {0ull, 0ull, 0ull, 0ull};
+        uint64_t sum[4] = {0ull, 0ull, 0ull, 0ull};   // while the store is under way
 #pragma unroll
         for (int i = 0; i < 4; ++i)
 #pragma unroll
@@ -601,6 +616,10 @@ __global__ void __launch_bounds__(kAcThreads, 1) k_attn_chunk(const __grid_const
         uint32_t s0, s1;
         unpair(add2(add2(sum[0], sum[1]), add2(sum[2], sum[3])), s0, s1);
         l = l * f + (__uint_as_float(s0) + __uint_as_float(s1));
+        tmem_wait_st();
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&p_bar[h][n & 1u]);
       }
       if (!ok) break;
       // ---- the next segment's queries: every S of this one has been read
