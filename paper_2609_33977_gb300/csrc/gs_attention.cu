@@ -30,7 +30,7 @@ Kernels kernels_of(const gs_seq_batch& b, int32_t group) {
 
 bool attention_units_fit(const gs_paged_cache& c, const gs_seq_batch& b, int32_t q_heads) {
   const double rows = (double)b.tokens * (q_heads / c.kv_heads), cap = (double)b.table_width * c.page_size;
-  const double units = (rows / attn_chunk_rows() + b.n + 1.0) * c.kv_heads * (cap / std::min(attn_rows_tile(), attn_chunk_tile()) + 1.0);
+  const double units = (rows / (attn_chunk_rows() / 2) + b.n + 1.0) * c.kv_heads * (cap / std::min(attn_rows_tile(), attn_chunk_tile()) + 1.0);
   return rows < 1e9 && units < 2e9;
 }
 
@@ -62,6 +62,7 @@ gs_status launch_paged_attention(const gs_paged_cache& c, const gs_seq_batch& b,
   P.kv_heads = c.kv_heads;
   P.group = q_heads / c.kv_heads;
   P.group_inv = 0xFFFFFFFFu / (uint32_t)P.group;
+  P.half_tokens = 0;
   // a scale of zero weighs all keys alike: so does one this small, and masked scores (-inf) stay what they are
   P.scale_log2 = std::max(std::fabs(scale) * 1.4426950408889634f, 1e-36f);
   P.negate = scale < 0.f;
@@ -84,6 +85,10 @@ gs_status launch_paged_attention(const gs_paged_cache& c, const gs_seq_batch& b,
   if (!encode_tmap_slabs_bf16(&P.kmap, c.k_dev, D, rows, box, (int)box == attn_chunk_tile() ? slabs : 1u) ||
       !encode_tmap_slabs_bf16(&P.vmap, c.v_dev, D, rows, box, slabs))
     return GS_ERR_CUDA;
+  P.half_tokens = attn_chunk_half_tokens(P.group);
+  const uint64_t dims[3] = {D, (uint64_t)q_heads, (uint64_t)b.tokens}, strides[2] = {D * 2, (uint64_t)q_stride * 2};
+  const uint32_t qbox[3] = {64, (uint32_t)P.group, (uint32_t)P.half_tokens};
+  if (!encode_tmap_nd_bf16(&P.qmap, q, 3, dims, strides, qbox, 128)) return GS_ERR_CUDA;
   P.min_rows = k.few ? attn_rows_most() + 1 : 1;
   P.max_rows = INT32_MAX;
   P.zero_rest = !k.few;

@@ -18,6 +18,7 @@ namespace gs {
 
 struct AttnParams {
   CUtensorMap kmap, vmap;   // (64, rows, head_dim / 64) slabs over [pages * kv_heads * page_size][head_dim]
+  CUtensorMap qmap;         // chunk kernel: [tokens][q_heads][head_dim], boxes of half_tokens x group x 64
   const uint16_t* q;
   const uint16_t* v;        // the value pages (re-read where a masked tile holds an infinity or NaN)
   uint16_t* out;
@@ -30,6 +31,7 @@ struct AttnParams {
   int64_t q_stride, tokens, pages;
   int32_t n_seqs, width, page_shift, q_heads, kv_heads, group;
   uint32_t group_inv;       // floor((2^32 - 1) / group)
+  int32_t half_tokens;      // chunk kernel: whole tokens in 128 rows
   int32_t min_rows, max_rows;   // sequences with that many rows (new tokens x query heads a key head) are this kernel's
   int32_t zero_rest;            // no other kernel runs: zeros for the tokens of sequences above max_rows, and of none
   float scale_log2;             // |scale| log2(e)
@@ -45,7 +47,8 @@ gs_status launch_attn_rows(const AttnParams& P, int head_dim, int rows, int ctas
 // attn_chunk.cu: any number of rows
 int attn_chunk_box(int page_size);
 int attn_chunk_tile();
-int attn_chunk_rows();              // rows of an item
+int attn_chunk_half_tokens(int group);   // tokens of half an item
+int attn_chunk_rows();                   // rows of a part in the workspace
 gs_status launch_attn_chunk(const AttnParams& P, int head_dim, int ctas, cudaStream_t s);
 
 struct SeqInfo {

@@ -2,8 +2,8 @@
 // whole prompts.
 //
 // Bound by the tensor cores (4 head_dim FLOP a visible pair) and by the exponentials
-// beside them.  An item is 256 rows of a key head against its visible keys, a unit
-// 64 keys.  The rows are two halves of 128, one per softmax warpgroup, whose thread
+// beside them.  An item is up to 256 rows of a key head (whole tokens, two halves)
+// against its visible keys, a unit 64 keys.  A half has 128 lanes, one per softmax warpgroup, whose thread
 // i owns row i, so that maxima and sums need no exchange.  Per half and unit:
 //     S = Q K^T (tcgen05, both operands in shared memory, S in TMEM), the thread
 //     reads its row of S, writes P = exp2(c S - m) over it as bf16, and
@@ -29,7 +29,8 @@ namespace {
 using namespace sm100;
 
 constexpr int kCT = 64;                        // keys of a unit
-constexpr int kHalf = 128, kRowsItem = 256;
+constexpr int kHalf = 128;                     // lanes of a half
+constexpr int kPartRows = 2 * kHalf;           // rows of a part in the workspace
 constexpr int kAcThreads = 512;                // warps: keys, values, S x 2, P V x 2, two value checkers; two softmax warpgroups
 constexpr int kRing = 5;                       // slots of keys, and as many of values
 constexpr int kSegs = 4;
@@ -41,15 +42,18 @@ static_assert(8 * 32 * (kRegsOther + kRegsSoftmax) <= kAcThreads * 128, "registe
 struct ChunkTraits {
   static constexpr int kLeast = 8, kSnap = 3, kOver = 5;
   static constexpr bool kOneTile = false;
+  // A half holds whole tokens (P.half_tokens: group x that of its 128 lanes are used), an item two halves.
   static __device__ __forceinline__ int row_tiles(const SeqInfo& s, const AttnParams& P) {
-    return s.rows >= P.min_rows && s.rows <= P.max_rows ? (s.rows + kRowsItem - 1) / kRowsItem : 0;
+    if (s.rows < P.min_rows || s.rows > P.max_rows) return 0;
+    const int t = 2 * P.half_tokens;
+    return (s.n + t - 1) / t;
   }
-  // units that the rows up to `row_end` of a sequence see
-  static __device__ __forceinline__ int units_of(const SeqInfo& s, const AttnParams& P, int row_end) {
-    return max(1, (s.seen(row_token(P, min(row_end, s.rows) - 1)) + kCT - 1) / kCT);
+  // units that the tokens before `end` of a sequence see
+  static __device__ __forceinline__ int units_of(const SeqInfo& s, int end) {
+    return max(1, (s.seen(min(end, s.n) - 1) + kCT - 1) / kCT);
   }
   static __device__ __forceinline__ int tiles(const SeqInfo& s, const AttnParams& P, int rt) {
-    return units_of(s, P, (rt + 1) * kRowsItem);
+    return units_of(s, 2 * (rt + 1) * P.half_tokens);
   }
 };
 
@@ -145,7 +149,7 @@ __global__ void __launch_bounds__(kAcThreads, 1) k_attn_chunk(const __grid_const
   __shared__ __align__(8) uint64_t vfull_bar[kRing], vempty_bar[kRing];   // values
   __shared__ __align__(8) uint64_t clean_bar[kRing];                      // values looked over
   __shared__ __align__(8) uint64_t seg_full[kSegs], seg_empty[kSegs];
-  __shared__ __align__(8) uint64_t q_bar[2];           // a half's queries are in shared memory
+  __shared__ __align__(8) uint64_t q_bar[2], qempty_bar[2];   // a half's queries are in shared memory, are not needed any more
   __shared__ __align__(8) uint64_t s_bar[2];           // S is in TMEM (and the P V is over whose P this unit's replaces)
   __shared__ __align__(8) uint64_t sfree_bar[2];       // S has been read
   __shared__ __align__(8) uint64_t p_bar[2][2];        // [half][buffer]: P is in TMEM, O is rescaled
@@ -174,7 +178,8 @@ __global__ void __launch_bounds__(kAcThreads, 1) k_attn_chunk(const __grid_const
       mbar_init(&seg_empty[s], 15);   // every warp but the one that fills it
     }
     for (int h = 0; h < 2; ++h) {
-      mbar_init(&q_bar[h], 4);
+      mbar_init(&q_bar[h], 1);
+      mbar_init(&qempty_bar[h], 1);
       mbar_init(&s_bar[h], 1);
       mbar_init(&sfree_bar[h], 4);
       for (int b = 0; b < 2; ++b) {
@@ -188,6 +193,7 @@ __global__ void __launch_bounds__(kAcThreads, 1) k_attn_chunk(const __grid_const
     fence_mbar_init();
     prefetch_tmap(&P.kmap);
     prefetch_tmap(&P.vmap);
+    prefetch_tmap(&P.qmap);
   }
   if (warp == 2) {
     tmem_alloc(&tmem_base_s, 512);
@@ -204,8 +210,9 @@ __global__ void __launch_bounds__(kAcThreads, 1) k_attn_chunk(const __grid_const
     return mbar_wait_warp(bar, parity, abort_flag, P.err, kAcWaitLimitNs);
   };
   // A half's units end where its last row's keys end.
-  const auto half_end = [&](const Segment& g, int h) { return min(g.tb, ChunkTraits::units_of(g.s, P, g.rt * kRowsItem + (h + 1) * kHalf)); };
-  const auto halves = [&](const Segment& g) { return g.s.rows - g.rt * kRowsItem > kHalf ? 2 : 1; };
+  const auto half_tok = [&](const Segment& g, int h) { return (2 * g.rt + h) * P.half_tokens; };   // its first token
+  const auto half_end = [&](const Segment& g, int h) { return min(g.tb, ChunkTraits::units_of(g.s, half_tok(g, h + 1))); };
+  const auto halves = [&](const Segment& g) { return g.s.n > half_tok(g, 1) ? 2 : 1; };
 
   if (warp < 8) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsOther));
@@ -227,7 +234,7 @@ __global__ void __launch_bounds__(kAcThreads, 1) k_attn_chunk(const __grid_const
       uint64_t* full_bar = keys ? kfull_bar : vfull_bar;
       uint64_t* empty_bar = keys ? kempty_bar : vempty_bar;
       uint8_t* ring = keys ? ring_k : ring_v;
-      uint32_t slot = 0, ph = 1u;
+      uint32_t slot = 0, ph = 1u, qph0 = 1u, qph1 = 1u;
       bool ok = true;
       while (ok) {
         if (keys) {
@@ -245,6 +252,24 @@ __global__ void __launch_bounds__(kAcThreads, 1) k_attn_chunk(const __grid_const
             sph ^= 1u;
           }
           if (!more) break;
+          for (int h = 0; h < halves(g) && ok; ++h) {   // queries: rows of (token, head), a slab of 64 channels a box
+            if (g.ta >= half_end(g, h)) continue;
+            if (!wait_warp(&qempty_bar[h], h ? qph1 : qph0)) {
+              ok = false;
+              break;
+            }
+            if (h) qph1 ^= 1u;
+            else qph0 ^= 1u;
+            if (elect_one()) {
+              mbar_arrive_expect_tx(&q_bar[h], (uint32_t)(P.half_tokens * P.group * D * 2));
+#pragma unroll
+              for (int sl = 0; sl < C::kSlabs; ++sl)
+                tma_load_3d(smem + h * C::kQBytes + sl * (kHalf * 128), &P.qmap, &q_bar[h], 64 * sl, g.h * P.group,
+                            g.s.tok0 + half_tok(g, h));
+            }
+            __syncwarp();
+          }
+          if (!ok) break;
         } else {
           if (!wait_warp(&seg_full[sg], sph)) break;
           g = segs[sg];
@@ -313,7 +338,7 @@ __global__ void __launch_bounds__(kAcThreads, 1) k_attn_chunk(const __grid_const
       };
       const auto over = [&](uint32_t unit) { return wait_warp(&o_bar[h][unit & 1u], (unit >> 1) & 1u); };
       if (role < 2) {
-        const uint32_t idesc = idesc_bf16_f32(kHalf, kCT);
+        const uint32_t idesc = idesc_bf16_f32(kHalf, kCT) | (P.negate ? 1u << 13 : 0u);   // bit 13: minus A
         const uint32_t q_lo = desc_lo(smem_u32(smem + h * C::kQBytes), 16), k_lo = desc_lo(smem_u32(ring_k), 16);
         uint32_t qph = 0u;
         while (ok) {
@@ -340,6 +365,7 @@ __global__ void __launch_bounds__(kAcThreads, 1) k_attn_chunk(const __grid_const
                        desc(b + (((kk >> 2) * (kCT * 128) + (kk & 3) * 32) >> 4)), idesc, kk == 0 ? 0u : 1u, one);
               commit_to(&s_bar[h], one);
               commit_to(&kempty_bar[slot], one);
+              if (u == units - 1) commit_to(&qempty_bar[h], one);
               ++n;
             } else if (lane == 0) {
               mbar_arrive(&kempty_bar[slot]);   // this half's part of handing the slot back
@@ -398,7 +424,7 @@ __global__ void __launch_bounds__(kAcThreads, 1) k_attn_chunk(const __grid_const
         const Segment g = segs[sg];
         const uint32_t at = sg;
         if (g.r < 0) break;
-        const int len = g.s.len(), all_see = g.s.seen(row_token(P, g.rt * kRowsItem));
+        const int len = g.s.len(), all_see = g.s.seen(half_tok(g, 0));
         for (int t = g.ta; t < g.tb; ++t) {
           if (!wait_warp(&vfull_bar[vs], vph)) {
             ok = false;
@@ -494,66 +520,46 @@ __global__ void __launch_bounds__(kAcThreads, 1) k_attn_chunk(const __grid_const
       bool on;
     };
     const auto row_of = [&](const Segment& g) {
-      const int row = g.rt * kRowsItem + h * kHalf + 32 * quarter + lane;
+      const int i = 32 * quarter + lane, t = row_token(P, i);
       Row r;
-      r.on = row < g.s.rows;
-      r.tok = r.on ? row_token(P, row) : 0;
-      r.hd = r.on ? row - r.tok * P.group : 0;
+      r.tok = half_tok(g, h) + t;
+      r.hd = i - t * P.group;
+      r.on = t < P.half_tokens && r.tok < g.s.n;
       r.vis = r.on ? g.s.seen(r.tok) : 0;
       return r;
-    };
-    // the warp's 32 rows of queries, swizzled as the MMA reads them
-    const auto load_q = [&](const Segment& g, const Row& row) {
-      if (g.ta >= half_end(g, h)) return;
-      constexpr int kPieces = D / 8, kStep = 32 / kPieces;
-      const uint32_t flip = P.negate ? 0x80008000u : 0u;
-      // rows past the last read the first one's (a load that depends on a branch waits for the one before it); nobody
-      // reads their results
-      const int64_t mine = (int64_t)(g.s.tok0 + row.tok) * P.q_stride + (int64_t)(g.h * P.group + row.hd) * D;
-      uint4 x[32 / kStep];
-#pragma unroll
-      for (int i = 0; i < 32 / kStep; ++i) {
-        const int64_t at = __shfl_sync(0xffffffffu, mine, i * kStep + lane / kPieces);
-        x[i] = __ldg(reinterpret_cast<const uint4*>(P.q + at) + lane % kPieces);
-      }
-#pragma unroll
-      for (int i = 0; i < 32 / kStep; ++i) {
-        const int r = 32 * quarter + i * kStep + lane / kPieces, p = lane % kPieces;
-        *reinterpret_cast<uint4*>(smem + h * C::kQBytes + (p >> 3) * (kHalf * 128) + r * 128 + (((p & 7) ^ (r & 7)) << 4)) =
-            make_uint4(x[i].x ^ flip, x[i].y ^ flip, x[i].z ^ flip, x[i].w ^ flip);
-      }
-      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-      __syncwarp();
-      if (lane == 0) mbar_arrive(&q_bar[h]);
     };
     Segment g;
     uint32_t at;
     bool more = next_segment(g, at);
     Row row = {0, 0, 0, false};
-    if (more) {
-      row = row_of(g);
-      load_q(g, row);
-    }
+    if (more) row = row_of(g);
     while (more) {
       const int end = half_end(g, h);
-      const int all_see = g.s.seen(row_token(P, g.rt * kRowsItem + h * kHalf));
+      const int all_see = g.s.seen(half_tok(g, h));
       float m = -INFINITY, l = 0.f;
       bool ok = true;
-      for (int t = g.ta; t < end; ++t, ++n) {
-        if (!wait_warp(&s_bar[h], n & 1u)) {
-          ok = false;
-          break;
-        }
+      uint32_t s[2][32];
+      // S of unit n on its way to registers, and there
+      const auto fetch_s = [&]() {
+        if (!wait_warp(&s_bar[h], n & 1u)) return false;
         tc_fence_after();
-        uint32_t s[2][32];
         tmem_ld_x32(ts, s[0]);
         tmem_ld_x32(ts + 32, s[1]);
+        return true;
+      };
+      const auto have_s = [&]() {
         tmem_wait_ld();
         reg_fence(s[0]);
         reg_fence(s[1]);
         tc_fence_before();
         __syncwarp();
         if (lane == 0) mbar_arrive(&sfree_bar[h]);
+      };
+      if (g.ta < end) {
+        ok = fetch_s();
+        if (ok) have_s();
+      }
+      for (int t = g.ta; t < end && ok; ++t) {
         const int key0 = t * kCT;
         if (key0 + kCT > all_see) {
           const int v = row.vis - key0;
@@ -616,72 +622,97 @@ __global__ void __launch_bounds__(kAcThreads, 1) k_attn_chunk(const __grid_const
         uint32_t s0, s1;
         unpair(add2(add2(sum[0], sum[1]), add2(sum[2], sum[3])), s0, s1);
         l = l * f + (__uint_as_float(s0) + __uint_as_float(s1));
+        const uint32_t buf = n++ & 1u;
+        if (t + 1 < end) ok = fetch_s();   // the next one, beside the store
         tmem_wait_st();
         tc_fence_before();
         __syncwarp();
-        if (lane == 0) mbar_arrive(&p_bar[h][n & 1u]);
+        if (lane == 0) mbar_arrive(&p_bar[h][buf]);
+        if (t + 1 < end && ok) have_s();
       }
       if (!ok) break;
-      // ---- the next segment's queries: every S of this one has been read
-      Segment g2;
-      uint32_t at2 = 0;
-      const bool more2 = next_segment(g2, at2);
-      Row row2 = {0, 0, 0, false};
-      if (more2) {
-        row2 = row_of(g2);
-        load_q(g2, row2);
-      }
-      // ---- this segment's result
-      float o[D];
+      // ---- this segment's result, 64 channels at a time
       if (g.ta < end) {
         if (!wait_warp(&o_bar[h][(n - 1u) & 1u], ((n - 1u) >> 1) & 1u)) break;
         tc_fence_after();
-        uint32_t v[D / 32][32];
-#pragma unroll
-        for (int i = 0; i < D / 32; ++i) tmem_ld_x32(to + 32 * i, v[i]);
-        tmem_wait_ld();
-#pragma unroll
-        for (int i = 0; i < D / 32; ++i) {
-          reg_fence(v[i]);
-#pragma unroll
-          for (int e = 0; e < 32; ++e) o[32 * i + e] = __uint_as_float(v[i][e]);
-        }
-      } else {
-#pragma unroll
-        for (int e = 0; e < D; ++e) o[e] = 0.f;
       }
-      if (bad_s[at]) {   // infinities and NaN of keys that only some rows see
-        const int stop = min(g.tb * kCT, row.vis);
-        for (int key = max(g.s.seen(row_token(P, g.rt * kRowsItem)), g.ta * kCT); key < stop; ++key) {
-          const int pg = __ldg(P.table + (int64_t)g.r * P.width + (key >> P.page_shift));
-          if (pg < 0 || pg >= P.pages) continue;
-          const uint16_t* vr = P.v + ((((int64_t)pg * P.kv_heads + g.h) << P.page_shift) + (key & ((1 << P.page_shift) - 1))) * D;
+      // Rows to memory: a lane has a whole row, so four lanes first exchange 16-byte pieces until each has one piece of
+      // four rows, and write 64 bytes of a row together.
+      const int64_t mine = row.on ? ((int64_t)(g.s.tok0 + row.tok) * P.q_heads + g.h * P.group + row.hd) * D : -1;
+      const auto store = [&](const float (&o)[64], int c0, float inv) {
+        int64_t dst[4];
 #pragma unroll
-          for (int e = 0; e < D; ++e) {
-            const float x = bf16_lo(__ldg(vr + e));
-            if (!isfinite(x)) o[e] += x;
+        for (int r = 0; r < 4; ++r) dst[r] = __shfl_sync(0xffffffffu, mine, (lane & ~3) + r);
+#pragma unroll
+        for (int e = 0; e < 64; e += 32) {
+          uint32_t w[4][4];   // [piece, then row][word]
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int k = 0; k < 4; ++k) w[i][k] = pack_bf16(o[e + 8 * i + 2 * k] * inv, o[e + 8 * i + 2 * k + 1] * inv);
+#pragma unroll
+          for (int d = 1; d <= 2; d <<= 1)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              if (i & d) continue;
+#pragma unroll
+              for (int k = 0; k < 4; ++k) {
+                const bool up = (lane & d) != 0;
+                const uint32_t got = __shfl_xor_sync(0xffffffffu, up ? w[i][k] : w[i + d][k], d);
+                if (up) w[i][k] = got;
+                else w[i + d][k] = got;
+              }
+            }
+#pragma unroll
+          for (int r = 0; r < 4; ++r)
+            if (dst[r] >= 0)
+              *reinterpret_cast<uint4*>(P.out + dst[r] + c0 + e + 8 * (lane & 3)) = make_uint4(w[r][0], w[r][1], w[r][2], w[r][3]);
+        }
+      };
+      // parts: [D / 4][256 rows][4], then [256][2]
+      const int ri = h * kHalf + 32 * quarter + lane;
+      float* slot = g.parts > 1 ? part_slot(P, g.first_cta, g.part, kPartRows, D) : nullptr;
+      const float inv = row.vis > 0 ? 1.f / l : 0.f;
+#pragma unroll 1
+      for (int c0 = 0; c0 < D; c0 += 64) {
+        float o[64];
+        if (g.ta < end) {
+          uint32_t v[2][32];
+          tmem_ld_x32(to + c0, v[0]);
+          tmem_ld_x32(to + c0 + 32, v[1]);
+          tmem_wait_ld();
+          reg_fence(v[0]);
+          reg_fence(v[1]);
+#pragma unroll
+          for (int e = 0; e < 64; ++e) o[e] = __uint_as_float(v[e >> 5][e & 31]);
+        } else {
+#pragma unroll
+          for (int e = 0; e < 64; ++e) o[e] = 0.f;
+        }
+        if (bad_s[at]) {   // infinities and NaN of keys that only some rows see
+          const int stop = min(g.tb * kCT, row.vis);
+          for (int key = max(g.s.seen(half_tok(g, 0)), g.ta * kCT); key < stop; ++key) {
+            const int pg = __ldg(P.table + (int64_t)g.r * P.width + (key >> P.page_shift));
+            if (pg < 0 || pg >= P.pages) continue;
+            const uint16_t* vr = P.v + ((((int64_t)pg * P.kv_heads + g.h) << P.page_shift) + (key & ((1 << P.page_shift) - 1))) * D + c0;
+#pragma unroll
+            for (int e = 0; e < 64; ++e) {
+              const float x = bf16_lo(__ldg(vr + e));
+              if (!isfinite(x)) o[e] += x;
+            }
           }
         }
+        if (slot) {
+#pragma unroll
+          for (int e = 0; e < 64; e += 4)
+            *reinterpret_cast<float4*>(slot + (size_t)((c0 + e) * kPartRows + 4 * ri)) = make_float4(o[e], o[e + 1], o[e + 2], o[e + 3]);
+        } else {
+          store(o, c0, inv);
+        }
       }
-      uint16_t* dst = P.out + ((int64_t)(g.s.tok0 + row.tok) * P.q_heads + g.h * P.group + row.hd) * D;
-      const auto store = [&](float inv) {
-        if (!row.on) return;
-#pragma unroll
-        for (int e = 0; e < D; e += 8)
-          *reinterpret_cast<uint4*>(dst + e) =
-              make_uint4(pack_bf16(o[e] * inv, o[e + 1] * inv), pack_bf16(o[e + 2] * inv, o[e + 3] * inv),
-                         pack_bf16(o[e + 4] * inv, o[e + 5] * inv), pack_bf16(o[e + 6] * inv, o[e + 7] * inv));
-      };
-      if (g.parts == 1) {
-        store(row.vis > 0 ? 1.f / l : 0.f);
-      } else {
-        // parts: [D / 4][256 rows][4], then [256][2]; the warpgroup that arrives last joins its half
-        const int ri = h * kHalf + 32 * quarter + lane;
-        float* slot = part_slot(P, g.first_cta, g.part, kRowsItem, D);
-#pragma unroll
-        for (int e = 0; e < D; e += 4)
-          *reinterpret_cast<float4*>(slot + (size_t)(e * kRowsItem + 4 * ri)) = make_float4(o[e], o[e + 1], o[e + 2], o[e + 3]);
-        *reinterpret_cast<float2*>(slot + (size_t)(D * kRowsItem + 2 * ri)) = make_float2(m, l);
+      if (slot) {
+        // the warpgroup that arrives last joins its half, in the parts' order
+        *reinterpret_cast<float2*>(slot + (size_t)(D * kPartRows + 2 * ri)) = make_float2(m, l);
         __threadfence();
         if (!meet()) break;
         if (quarter == 0 && lane == 0) {
@@ -692,37 +723,39 @@ __global__ void __launch_bounds__(kAcThreads, 1) k_attn_chunk(const __grid_const
         }
         if (!meet()) break;
         if (last_s[h]) {
-          float mm = -INFINITY, ll = 0.f;
+          float mm = -INFINITY;
           for (int p = 0; p < g.parts; ++p)
-            mm = fmaxf(mm, __ldcg(part_slot(P, g.first_cta, p, kRowsItem, D) + D * kRowsItem + 2 * ri));
+            mm = fmaxf(mm, __ldcg(part_slot(P, g.first_cta, p, kPartRows, D) + D * kPartRows + 2 * ri));
           const float base = mm == -INFINITY ? 0.f : mm;
-#pragma unroll
-          for (int e = 0; e < D; ++e) o[e] = 0.f;
 #pragma unroll 1
-          for (int p = 0; p < g.parts; ++p) {
-            const float* sp = part_slot(P, g.first_cta, p, kRowsItem, D);
-            const float2 ml = __ldcg(reinterpret_cast<const float2*>(sp + D * kRowsItem + 2 * ri));
-            const float fp = ml.x == mm ? 1.f : ex2((ml.x - base) * c);
-            ll = fmaf(ml.y, fp, ll);
+          for (int c0 = 0; c0 < D; c0 += 64) {
+            float o[64], ll = 0.f;
 #pragma unroll
-            for (int e = 0; e < D; e += 4) {
-              const float4 v = __ldcg(reinterpret_cast<const float4*>(sp + (size_t)(e * kRowsItem + 4 * ri)));
-              o[e] = fmaf(v.x, fp, o[e]);
-              o[e + 1] = fmaf(v.y, fp, o[e + 1]);
-              o[e + 2] = fmaf(v.z, fp, o[e + 2]);
-              o[e + 3] = fmaf(v.w, fp, o[e + 3]);
+            for (int e = 0; e < 64; ++e) o[e] = 0.f;
+#pragma unroll 1
+            for (int p = 0; p < g.parts; ++p) {
+              const float* sp = part_slot(P, g.first_cta, p, kPartRows, D);
+              const float2 ml = __ldcg(reinterpret_cast<const float2*>(sp + D * kPartRows + 2 * ri));
+              const float fp = ml.x == mm ? 1.f : ex2((ml.x - base) * c);
+              ll = fmaf(ml.y, fp, ll);
+#pragma unroll
+              for (int e = 0; e < 64; e += 4) {
+                const float4 v = __ldcg(reinterpret_cast<const float4*>(sp + (size_t)((c0 + e) * kPartRows + 4 * ri)));
+                o[e] = fmaf(v.x, fp, o[e]);
+                o[e + 1] = fmaf(v.y, fp, o[e + 1]);
+                o[e + 2] = fmaf(v.z, fp, o[e + 2]);
+                o[e + 3] = fmaf(v.w, fp, o[e + 3]);
+              }
             }
+            store(o, c0, row.vis > 0 ? 1.f / ll : 0.f);
           }
-          store(row.vis > 0 ? 1.f / ll : 0.f);
         }
       }
       __syncwarp();
       if (lane == 0) mbar_arrive(&seg_empty[at]);
       tc_fence_before();   // O may be overwritten once the next P is announced
-      g = g2;
-      at = at2;
-      row = row2;
-      more = more2;
+      more = next_segment(g, at);
+      if (more) row = row_of(g);
     }
   }
   tc_fence_before();
@@ -755,7 +788,9 @@ int attn_chunk_box(int page_size) { return page_size < kCT ? page_size : kCT; }
 
 int attn_chunk_tile() { return kCT; }
 
-int attn_chunk_rows() { return kRowsItem; }
+int attn_chunk_rows() { return kPartRows; }
+
+int attn_chunk_half_tokens(int group) { return kHalf / group; }
 
 gs_status launch_attn_chunk(const AttnParams& P, int head_dim, int ctas, cudaStream_t s) {
   return head_dim == 128 ? chunk_launch<128>(P, ctas, s) : chunk_launch<64>(P, ctas, s);
