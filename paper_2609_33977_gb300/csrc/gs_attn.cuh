@@ -88,27 +88,20 @@ __device__ __forceinline__ float ex2(float x) {
   return y;
 }
 
-// A whole warp's bounded wait, for barriers that complete within a microsecond or two: the
-// clock and the abort flag are only looked at after many tries (a try itself waits for a
-// while).  The same answer for all lanes.
-__device__ __forceinline__ bool mbar_wait_warp(uint64_t* bar, uint32_t parity, volatile int* abort_flag, int* err,
-                                               uint64_t limit_ns) {
-  if (__all_sync(0xffffffffu, sm100::mbar_try_wait(bar, parity))) return true;
-  uint64_t t0 = 0;
+// A whole warp's bounded wait, the same answer for all lanes: at most kWaitTries tries of
+// up to a microsecond (0.1 s or more in all, 2 s at most).  Short code: it is inlined
+// wherever a warp waits, and the kernels' loops share the instruction cache with it.
+constexpr int kWaitTries = 2000000;
+__device__ __forceinline__ bool mbar_wait_warp(uint64_t* bar, uint32_t parity, volatile int* abort_flag, int* err) {
 #pragma unroll 1
-  for (uint32_t tries = 1;; ++tries) {
-    if (__all_sync(0xffffffffu, sm100::mbar_try_wait(bar, parity))) return true;
-    if ((tries & 63u) != 0) continue;
-    const uint64_t now = sm100::globaltimer_ns();
-    if (tries == 64u) t0 = now;
-    bool give_up = *abort_flag != 0;
-    if (now - t0 > limit_ns) {
+  for (int left = kWaitTries; !__all_sync(0xffffffffu, sm100::mbar_try_wait_sleep(bar, parity, 1000u)); --left) {
+    if (left == 0) {
       *abort_flag = 1;
       atomicExch(err, kDevErrTimeout);
-      give_up = true;
     }
-    if (__any_sync(0xffffffffu, give_up)) return false;
+    if (__any_sync(0xffffffffu, *abort_flag != 0)) return false;
   }
+  return true;
 }
 // A value that all lanes share, known as such to the compiler
 __device__ __forceinline__ int uniform(int v) { return (int)__reduce_max_sync(0xffffffffu, (uint32_t)v); }
@@ -128,6 +121,7 @@ __device__ __forceinline__ int head_units(const AttnParams& P, const SeqInfo& s,
   const int nr = on ? Traits::row_tiles(s, P) : 0;
   int u = 0;
   if (nr <= 2)
+#pragma unroll 1
     for (int i = 0; i < nr; ++i) u += Traits::tiles(s, P, i) + Traits::kOver;
   if constexpr (!Traits::kOneTile) {
     for (uint32_t many = __ballot_sync(0xffffffffu, nr > 2); many; many &= many - 1) {
@@ -139,6 +133,7 @@ __device__ __forceinline__ int head_units(const AttnParams& P, const SeqInfo& s,
       t.kv = __shfl_sync(0xffffffffu, s.kv, src);
       t.cap = __shfl_sync(0xffffffffu, s.cap, src);
       int part = 0;
+#pragma unroll 1
       for (int i = lane; i < n; i += 32) part += Traits::tiles(t, P, i) + Traits::kOver;
       part = __reduce_add_sync(0xffffffffu, part);
       if (lane == src) u = part;
@@ -247,6 +242,7 @@ __device__ __forceinline__ Shares divide_work(const AttnParams& P, int cta, Work
       w.sums[1][warp] = n;
     }
     __syncthreads();
+#pragma unroll 1
     for (int i = 0; i < kW; ++i) {
       total += w.sums[0][i] * P.kv_heads;
       items += w.sums[1][i] * P.kv_heads;
@@ -274,6 +270,7 @@ __device__ __forceinline__ Shares divide_work(const AttnParams& P, int cta, Work
     }
     __syncthreads();
     int base = carry + incl - u;
+#pragma unroll 1
     for (int i = 0; i < kW; ++i) {
       if (i < warp) base += w.sums[0][i];
       carry += w.sums[0][i];
@@ -281,7 +278,7 @@ __device__ __forceinline__ Shares divide_work(const AttnParams& P, int cta, Work
     }
     if (one_pass) total = carry;
     const Shares sh(total, items, (int)gridDim.x, Traits::kLeast);
-#pragma unroll
+#pragma unroll 1
     for (int e = 0; e < 2; ++e) {
       const int off = sh.cut(min(cta + e, sh.ctas)) - base;
       if (off >= 0 && off < u) {
@@ -388,6 +385,7 @@ struct Walker {
 __device__ __forceinline__ void zero_rows(const AttnParams& P, int head_dim, int cta, int lane, bool large) {
   const int64_t row16 = (int64_t)P.q_heads * head_dim / 8;   // 16-byte pieces of a token's output
   const auto zero = [&](int64_t t0, int64_t t1) {
+#pragma unroll 1
     for (int64_t i = t0 * row16 + lane; i < t1 * row16; i += 32) reinterpret_cast<uint4*>(P.out)[i] = make_uint4(0u, 0u, 0u, 0u);
   };
   const int64_t before = min((int64_t)max(0, __ldg(P.offsets)), P.tokens), after = max(0, __ldg(P.offsets + P.n_seqs));

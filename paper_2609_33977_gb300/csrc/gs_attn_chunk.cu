@@ -207,7 +207,7 @@ __global__ void __launch_bounds__(kAcThreads, 1) k_attn_chunk(const __grid_const
   volatile int* abort_flag = &abort_s;
   const int box_shift = min(P.page_shift, 6), box = 1 << box_shift;   // rows of a TMA box
   const auto wait_warp = [&](uint64_t* bar, uint32_t parity) {
-    return mbar_wait_warp(bar, parity, abort_flag, P.err, kAcWaitLimitNs);
+    return mbar_wait_warp(bar, parity, abort_flag, P.err);
   };
   // A half's units end where its last row's keys end.
   const auto half_tok = [&](const Segment& g, int h) { return (2 * g.rt + h) * P.half_tokens; };   // its first token
@@ -302,6 +302,7 @@ __global__ void __launch_bounds__(kAcThreads, 1) k_attn_chunk(const __grid_const
           if (elect_one()) mbar_arrive_expect_tx(full, (uint32_t)(boxes * box * D * 2));
           __syncwarp();
           // Keys: slabs of 64 channels x 64 keys.  Values: box after box, each with its slabs.
+#pragma unroll 1
           for (int b = 0; b < boxes; ++b) {
             const int32_t r = __shfl_sync(0xffffffffu, row, b);
             if (elect_one()) {
@@ -432,40 +433,36 @@ __global__ void __launch_bounds__(kAcThreads, 1) k_attn_chunk(const __grid_const
           }
           const int key0 = t * kCT;
           if (key0 + kCT > all_see) {
-            const uint32_t v = smem_u32(ring_v + vs * C::kOpBytes);
             constexpr int kPieces = D / 8, kStep = 32 / kPieces, kDeep = 16 / kStep;   // keys of a step of the warp; steps at once
             const int end = min(kCT, max(0, len - key0)), piece = lane % kPieces;
             bool bad = false;
+            // a key's row is kSlabs pieces of 128 bytes; their swizzle does not matter here
+            const auto piece_at = [&](int k) {
+              return ring_v + vs * C::kOpBytes + (((k >> box_shift) * C::kSlabs + (piece >> 3)) << box_shift) * 128 +
+                     (k & (box - 1)) * 128 + (piece & 7) * 16;
+            };
             for (int k0 = max(0, all_see - key0) + mine * (kDeep * kStep); k0 < kCT; k0 += kCheckers * kDeep * kStep) {
               uint4 x[kDeep];
-              uint32_t at16[kDeep];
               uint32_t any = 0u;   // bf16 pairs: the sum of 0 x, NaN where some x is an infinity or NaN
 #pragma unroll
               for (int i = 0; i < kDeep; ++i) {
-                // a key's row is kSlabs pieces of 128 bytes; their swizzle does not matter here
-                const int k = min(k0 + i * kStep + lane / kPieces, kCT - 1);
-                at16[i] = v + (uint32_t)((((k >> box_shift) * C::kSlabs + (piece >> 3)) << box_shift) * 128 + (k & (box - 1)) * 128 +
-                                         (piece & 7) * 16);
-                asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];"
-                             : "=r"(x[i].x), "=r"(x[i].y), "=r"(x[i].z), "=r"(x[i].w)
-                             : "r"(at16[i])
-                             : "memory");
+                x[i] = *reinterpret_cast<const uint4*>(piece_at(min(k0 + i * kStep + lane / kPieces, kCT - 1)));
               }
 #pragma unroll
               for (int i = 0; i < kDeep; ++i)
                 any = times_zero(x[i].w, times_zero(x[i].z, times_zero(x[i].y, times_zero(x[i].x, any))));
               if (nonfinite2(any) == 0u && k0 + kDeep * kStep <= end) continue;   // the rule: nothing to do
-#pragma unroll
+#pragma unroll 1
               for (int i = 0; i < kDeep; ++i) {
                 const int k = k0 + i * kStep + lane / kPieces;
-                if (k >= end) x[i] = make_uint4(0u, 0u, 0u, 0u);
-                const uint4 n = make_uint4(nonfinite2(x[i].x), nonfinite2(x[i].y), nonfinite2(x[i].z), nonfinite2(x[i].w));
-                const bool hit = (n.x | n.y | n.z | n.w) != 0u;
-                if (k < kCT && (hit || k >= end))
-                  asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(at16[i]), "r"(x[i].x & ~n.x), "r"(x[i].y & ~n.y),
-                               "r"(x[i].z & ~n.z), "r"(x[i].w & ~n.w)
-                               : "memory");
-                bad |= hit;
+                if (k >= kCT) break;
+#pragma unroll 1
+                for (int j = 0; j < 4; ++j) {
+                  uint32_t* w = reinterpret_cast<uint32_t*>(piece_at(k)) + j;
+                  const uint32_t x = k < end ? *w : 0u, n = nonfinite2(x);
+                  bad |= n != 0u;
+                  *w = x & ~n;
+                }
               }
             }
             if (bad) bad_s[at] = 1;
@@ -631,113 +628,44 @@ __global__ void __launch_bounds__(kAcThreads, 1) k_attn_chunk(const __grid_const
         if (t + 1 < end && ok) have_s();
       }
       if (!ok) break;
-      // ---- this segment's result, 64 channels at a time
+      // ---- this segment's result, 64 channels at a time: to the output, or (phase 0) to the item's parts in the workspace,
+      // which the warpgroup that arrives last joins in their order (phase 1).
+      // Parts: [D / 4][256 rows][4], then [256][2].
       if (g.ta < end) {
         if (!wait_warp(&o_bar[h][(n - 1u) & 1u], ((n - 1u) >> 1) & 1u)) break;
         tc_fence_after();
       }
-      // Rows to memory: a lane has a whole row, so four lanes first exchange 16-byte pieces until each has one piece of
-      // four rows, and write 64 bytes of a row together.
       const int64_t mine = row.on ? ((int64_t)(g.s.tok0 + row.tok) * P.q_heads + g.h * P.group + row.hd) * D : -1;
-      const auto store = [&](const float (&o)[64], int c0, float inv) {
-        int64_t dst[4];
-#pragma unroll
-        for (int r = 0; r < 4; ++r) dst[r] = __shfl_sync(0xffffffffu, mine, (lane & ~3) + r);
-#pragma unroll
-        for (int e = 0; e < 64; e += 32) {
-          uint32_t w[4][4];   // [piece, then row][word]
-#pragma unroll
-          for (int i = 0; i < 4; ++i)
-#pragma unroll
-            for (int k = 0; k < 4; ++k) w[i][k] = pack_bf16(o[e + 8 * i + 2 * k] * inv, o[e + 8 * i + 2 * k + 1] * inv);
-#pragma unroll
-          for (int d = 1; d <= 2; d <<= 1)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              if (i & d) continue;
-#pragma unroll
-              for (int k = 0; k < 4; ++k) {
-                const bool up = (lane & d) != 0;
-                const uint32_t got = __shfl_xor_sync(0xffffffffu, up ? w[i][k] : w[i + d][k], d);
-                if (up) w[i][k] = got;
-                else w[i + d][k] = got;
-              }
-            }
-#pragma unroll
-          for (int r = 0; r < 4; ++r)
-            if (dst[r] >= 0)
-              *reinterpret_cast<uint4*>(P.out + dst[r] + c0 + e + 8 * (lane & 3)) = make_uint4(w[r][0], w[r][1], w[r][2], w[r][3]);
-        }
-      };
-      // parts: [D / 4][256 rows][4], then [256][2]
       const int ri = h * kHalf + 32 * quarter + lane;
       float* slot = g.parts > 1 ? part_slot(P, g.first_cta, g.part, kPartRows, D) : nullptr;
-      const float inv = row.vis > 0 ? 1.f / l : 0.f;
+      float mm = 0.f;
 #pragma unroll 1
-      for (int c0 = 0; c0 < D; c0 += 64) {
-        float o[64];
-        if (g.ta < end) {
-          uint32_t v[2][32];
-          tmem_ld_x32(to + c0, v[0]);
-          tmem_ld_x32(to + c0 + 32, v[1]);
-          tmem_wait_ld();
-          reg_fence(v[0]);
-          reg_fence(v[1]);
-#pragma unroll
-          for (int e = 0; e < 64; ++e) o[e] = __uint_as_float(v[e >> 5][e & 31]);
-        } else {
+      for (int phase = 0; phase < 2; ++phase) {
+#pragma unroll 1
+        for (int c0 = 0; c0 < D; c0 += 64) {
+          float o[64], sum = l;
 #pragma unroll
           for (int e = 0; e < 64; ++e) o[e] = 0.f;
-        }
-        if (bad_s[at]) {   // infinities and NaN of keys that only some rows see
-          const int stop = min(g.tb * kCT, row.vis);
-          for (int key = max(g.s.seen(half_tok(g, 0)), g.ta * kCT); key < stop; ++key) {
-            const int pg = __ldg(P.table + (int64_t)g.r * P.width + (key >> P.page_shift));
-            if (pg < 0 || pg >= P.pages) continue;
-            const uint16_t* vr = P.v + ((((int64_t)pg * P.kv_heads + g.h) << P.page_shift) + (key & ((1 << P.page_shift) - 1))) * D + c0;
+          if (phase == 0) {
+            if (g.ta < end) {
+              uint32_t v[2][32];
+              tmem_ld_x32(to + c0, v[0]);
+              tmem_ld_x32(to + c0 + 32, v[1]);
+              tmem_wait_ld();
+              reg_fence(v[0]);
+              reg_fence(v[1]);
 #pragma unroll
-            for (int e = 0; e < 64; ++e) {
-              const float x = bf16_lo(__ldg(vr + e));
-              if (!isfinite(x)) o[e] += x;
+              for (int e = 0; e < 64; ++e) o[e] = __uint_as_float(v[e >> 5][e & 31]);
             }
-          }
-        }
-        if (slot) {
-#pragma unroll
-          for (int e = 0; e < 64; e += 4)
-            *reinterpret_cast<float4*>(slot + (size_t)((c0 + e) * kPartRows + 4 * ri)) = make_float4(o[e], o[e + 1], o[e + 2], o[e + 3]);
-        } else {
-          store(o, c0, inv);
-        }
-      }
-      if (slot) {
-        // the warpgroup that arrives last joins its half, in the parts' order
-        *reinterpret_cast<float2*>(slot + (size_t)(D * kPartRows + 2 * ri)) = make_float2(m, l);
-        __threadfence();
-        if (!meet()) break;
-        if (quarter == 0 && lane == 0) {
-          const int got = atomicAdd(P.cnt + 2 * g.first_cta + h, 1);
-          last_s[h] = got == g.parts - 1;
-          if (last_s[h]) P.cnt[2 * g.first_cta + h] = 0;
-          __threadfence();
-        }
-        if (!meet()) break;
-        if (last_s[h]) {
-          float mm = -INFINITY;
-          for (int p = 0; p < g.parts; ++p)
-            mm = fmaxf(mm, __ldcg(part_slot(P, g.first_cta, p, kPartRows, D) + D * kPartRows + 2 * ri));
-          const float base = mm == -INFINITY ? 0.f : mm;
-#pragma unroll 1
-          for (int c0 = 0; c0 < D; c0 += 64) {
-            float o[64], ll = 0.f;
-#pragma unroll
-            for (int e = 0; e < 64; ++e) o[e] = 0.f;
+          } else {
+            sum = 0.f;
+            const float base = mm == -INFINITY ? 0.f : mm;
 #pragma unroll 1
             for (int p = 0; p < g.parts; ++p) {
               const float* sp = part_slot(P, g.first_cta, p, kPartRows, D);
               const float2 ml = __ldcg(reinterpret_cast<const float2*>(sp + D * kPartRows + 2 * ri));
               const float fp = ml.x == mm ? 1.f : ex2((ml.x - base) * c);
-              ll = fmaf(ml.y, fp, ll);
+              sum = fmaf(ml.y, fp, sum);
 #pragma unroll
               for (int e = 0; e < 64; e += 4) {
                 const float4 v = __ldcg(reinterpret_cast<const float4*>(sp + (size_t)((c0 + e) * kPartRows + 4 * ri)));
@@ -747,10 +675,84 @@ __global__ void __launch_bounds__(kAcThreads, 1) k_attn_chunk(const __grid_const
                 o[e + 3] = fmaf(v.w, fp, o[e + 3]);
               }
             }
-            store(o, c0, row.vis > 0 ? 1.f / ll : 0.f);
+          }
+          if (slot && phase == 0) {
+#pragma unroll
+            for (int e = 0; e < 64; e += 4)
+              *reinterpret_cast<float4*>(slot + (size_t)((c0 + e) * kPartRows + 4 * ri)) = make_float4(o[e], o[e + 1], o[e + 2], o[e + 3]);
+            continue;
+          }
+          // A lane has a whole row: four lanes exchange 16-byte pieces until each has one piece of four rows, and write
+          // 64 bytes of a row together.
+          const float inv = row.vis > 0 ? 1.f / sum : 0.f;
+#pragma unroll
+          for (int e = 0; e < 64; e += 32) {
+            uint32_t w[4][4];   // [piece, then row][word]
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+              for (int k = 0; k < 4; ++k) w[i][k] = pack_bf16(o[e + 8 * i + 2 * k] * inv, o[e + 8 * i + 2 * k + 1] * inv);
+#pragma unroll
+            for (int d = 1; d <= 2; d <<= 1)
+#pragma unroll
+              for (int i = 0; i < 4; ++i) {
+                if (i & d) continue;
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                  const bool up = (lane & d) != 0;
+                  const uint32_t got = __shfl_xor_sync(0xffffffffu, up ? w[i][k] : w[i + d][k], d);
+                  w[i][k] = up ? got : w[i][k];
+                  w[i + d][k] = up ? w[i + d][k] : got;
+                }
+              }
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+              const int64_t dst = __shfl_sync(0xffffffffu, mine, (lane & ~3) + r);
+              if (dst >= 0)
+                *reinterpret_cast<uint4*>(P.out + dst + c0 + e + 8 * (lane & 3)) = make_uint4(w[r][0], w[r][1], w[r][2], w[r][3]);
+            }
           }
         }
+        if (phase == 0 && bad_s[at]) {
+          // infinities and NaN of keys that only some rows see: added to what has just been written
+          __syncwarp();
+          const int stop = min(g.tb * kCT, row.vis);
+#pragma unroll 1
+          for (int key = max(g.s.seen(half_tok(g, 0)), g.ta * kCT); key < stop; ++key) {
+            const int pg = __ldg(P.table + (int64_t)g.r * P.width + (key >> P.page_shift));
+            if (pg < 0 || pg >= P.pages) continue;
+            const uint16_t* vr = P.v + ((((int64_t)pg * P.kv_heads + g.h) << P.page_shift) + (key & ((1 << P.page_shift) - 1))) * D;
+#pragma unroll 1
+            for (int e = 0; e < D; ++e) {
+              const float x = bf16_lo(__ldg(vr + e));
+              if (isfinite(x)) continue;
+              if (slot) {
+                slot[(size_t)((e & ~3) * kPartRows + 4 * ri + (e & 3))] += x;
+              } else {
+                volatile uint16_t* to16 = P.out + mine + e;
+                *to16 = (uint16_t)pack_bf16(bf16_lo(*to16) + x, 0.f);
+              }
+            }
+          }
+        }
+        if (!slot || phase == 1) break;
+        *reinterpret_cast<float2*>(slot + (size_t)(D * kPartRows + 2 * ri)) = make_float2(m, l);
+        __threadfence();
+        if (!(ok = meet())) break;
+        if (quarter == 0 && lane == 0) {
+          const int got = atomicAdd(P.cnt + 2 * g.first_cta + h, 1);
+          last_s[h] = got == g.parts - 1;
+          if (last_s[h]) P.cnt[2 * g.first_cta + h] = 0;
+          __threadfence();
+        }
+        if (!(ok = meet())) break;
+        if (!last_s[h]) break;
+        mm = -INFINITY;
+#pragma unroll 1
+        for (int p = 0; p < g.parts; ++p)
+          mm = fmaxf(mm, __ldcg(part_slot(P, g.first_cta, p, kPartRows, D) + D * kPartRows + 2 * ri));
       }
+      if (!ok) break;
       __syncwarp();
       if (lane == 0) mbar_arrive(&seg_empty[at]);
       tc_fence_before();   // O may be overwritten once the next P is announced

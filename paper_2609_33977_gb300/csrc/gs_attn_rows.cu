@@ -16,7 +16,6 @@ namespace {
 using namespace sm100;
 
 constexpr int kTile = 128;
-constexpr uint64_t kArWaitLimitNs = 2000000000ull;
 
 struct FewTraits {
   static constexpr int kLeast = 2, kSnap = 1, kOver = 0;
@@ -143,7 +142,7 @@ __global__ void __launch_bounds__(RowsCfg<D, WR>::kThreads, 1) k_attn_rows(const
   volatile int* abort_flag = &abort_s;
   const int chunk_shift = min(P.page_shift, 7), chunk = 1 << chunk_shift;   // rows of a TMA box
   const auto wait_warp = [&](uint64_t* bar, uint32_t parity) {
-    return mbar_wait_warp(bar, parity, abort_flag, P.err, kArWaitLimitNs);
+    return mbar_wait_warp(bar, parity, abort_flag, P.err);
   };
 
   if (warp == C::kWarps) {
@@ -436,6 +435,7 @@ __global__ void __launch_bounds__(RowsCfg<D, WR>::kThreads, 1) k_attn_rows(const
         const int tok = row_token(P, row), hd = row - tok * P.group, vis = g.s.seen(tok);
         if (fix) {   // infinities and NaN of keys that only some rows see
           const int end = min(min(len, g.tb * kTile), vis);
+#pragma unroll 1
           for (int key = max(all_see, g.ta * kTile); key < end; ++key) {
             const int pg = __ldg(P.table + (int64_t)g.r * P.width + (key >> P.page_shift));
             if (pg < 0 || pg >= P.pages) continue;
@@ -479,7 +479,7 @@ __global__ void __launch_bounds__(RowsCfg<D, WR>::kThreads, 1) k_attn_rows(const
             float mm = -INFINITY, ll = 0.f, a[kC];
 #pragma unroll
             for (int c = 0; c < kC; ++c) a[c] = 0.f;
-#pragma unroll 4
+#pragma unroll 2
             for (int p = 0; p < g.parts; ++p) {
               const float* sp = part_slot(P, g.first_cta, p, C::kRows, D);
               const float2 ml = __ldcg(reinterpret_cast<const float2*>(sp + (size_t)C::kRows * D + 2 * row));
