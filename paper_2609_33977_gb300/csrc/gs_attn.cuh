@@ -89,19 +89,26 @@ __device__ __forceinline__ float ex2(float x) {
 }
 
 // A whole warp's bounded wait, the same answer for all lanes: at most kWaitTries tries of
-// up to a microsecond (0.1 s or more in all, 2 s at most).  Short code: it is inlined
-// wherever a warp waits, and the kernels' loops share the instruction cache with it.
+// up to a microsecond (0.1 s or more in all, 2 s at most), after which the block's abort
+// flag is up and every wait ends.  Short code: it is inlined wherever a warp waits, and the
+// kernels' loops share the instruction cache with it.
 constexpr int kWaitTries = 2000000;
-__device__ __forceinline__ bool mbar_wait_warp(uint64_t* bar, uint32_t parity, volatile int* abort_flag, int* err) {
+__device__ __forceinline__ bool mbar_wait_warp(uint64_t* bar, uint32_t parity, volatile int* abort_flag) {
 #pragma unroll 1
   for (int left = kWaitTries; !__all_sync(0xffffffffu, sm100::mbar_try_wait_sleep(bar, parity, 1000u)); --left) {
-    if (left == 0) {
-      *abort_flag = 1;
-      atomicExch(err, kDevErrTimeout);
-    }
+    if (left == 0) *abort_flag = 1;
     if (__any_sync(0xffffffffu, *abort_flag != 0)) return false;
   }
   return true;
+}
+// At a kernel's end, after a block barrier: records that some wait ran out, and gives
+// copies in flight time to land.
+__device__ __forceinline__ void end_of_waits(volatile int* abort_flag, int* err) {
+  if (!*abort_flag) return;
+  if (threadIdx.x == 0) atomicExch(err, kDevErrTimeout);
+  const uint64_t t0 = sm100::globaltimer_ns();
+  while (sm100::globaltimer_ns() - t0 < 2000000ull) {
+  }
 }
 // A value that all lanes share, known as such to the compiler
 __device__ __forceinline__ int uniform(int v) { return (int)__reduce_max_sync(0xffffffffu, (uint32_t)v); }
@@ -222,76 +229,60 @@ __device__ __forceinline__ Shares divide_work(const AttnParams& P, int cta, Work
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   constexpr int kW = THREADS / 32;
   static_assert(kW >= 2 && kW <= 32 && THREADS % 32 == 0, "block");
-  const bool one_pass = P.n_seqs <= THREADS;   // a sequence a thread
+  const bool one_pass = P.n_seqs <= THREADS;   // a sequence a thread: looked at once
   SeqInfo mine = {0, 0, 0, 0, 0};
-  int per_head = 0, total = 0, items = 0;
+  int per_head = 0, tiles = 0, items = 0;
+  Shares sh(0, 0, 1, 1);
   if (threadIdx.x < 2) w.slot[threadIdx.x].r = P.n_seqs;
-  if (!one_pass) {
-    int u = 0, n = 0;
+  // first the sums, then the sequences that hold this CTA's boundaries
+#pragma unroll 1
+  for (int pass = 0; pass < 2; ++pass) {
+    int carry = 0;
+#pragma unroll 1
     for (int r0 = 0; r0 < P.n_seqs; r0 += THREADS) {
       const int r = r0 + (int)threadIdx.x;
-      const bool on = r < P.n_seqs;
-      if (on) mine = seq_info(P, r);
-      u += head_units<Traits>(P, mine, on);
-      n += on ? Traits::row_tiles(mine, P) : 0;
-    }
-    u = __reduce_add_sync(0xffffffffu, u);
-    n = __reduce_add_sync(0xffffffffu, n);
-    if (lane == 0) {
-      w.sums[0][warp] = u;
-      w.sums[1][warp] = n;
-    }
-    __syncthreads();
-#pragma unroll 1
-    for (int i = 0; i < kW; ++i) {
-      total += w.sums[0][i] * P.kv_heads;
-      items += w.sums[1][i] * P.kv_heads;
-    }
-    __syncthreads();
-  }
-  int carry = 0;
-  for (int r0 = 0; r0 < P.n_seqs; r0 += THREADS) {
-    const int r = r0 + (int)threadIdx.x;
-    const bool on = r < P.n_seqs;
-    if (on) mine = seq_info(P, r);
-    per_head = head_units<Traits>(P, mine, on);
-    int n = on ? Traits::row_tiles(mine, P) : 0;
-    const int u = per_head * P.kv_heads;
-    int incl = u;
-#pragma unroll
-    for (int d = 1; d < 32; d <<= 1) {
-      const int o = __shfl_up_sync(0xffffffffu, incl, d);
-      if (lane >= d) incl += o;
-    }
-    n = __reduce_add_sync(0xffffffffu, n);
-    if (lane == 31) {
-      w.sums[0][warp] = incl;
-      w.sums[1][warp] = n;
-    }
-    __syncthreads();
-    int base = carry + incl - u;
-#pragma unroll 1
-    for (int i = 0; i < kW; ++i) {
-      if (i < warp) base += w.sums[0][i];
-      carry += w.sums[0][i];
-      if (one_pass) items += w.sums[1][i] * P.kv_heads;
-    }
-    if (one_pass) total = carry;
-    const Shares sh(total, items, (int)gridDim.x, Traits::kLeast);
-#pragma unroll 1
-    for (int e = 0; e < 2; ++e) {
-      const int off = sh.cut(min(cta + e, sh.ctas)) - base;
-      if (off >= 0 && off < u) {
-        w.slot[e].r = r;
-        w.slot[e].base = base;
-        w.slot[e].per_head = per_head;
-        w.slot[e].s = mine;
+      if (pass == 0 || !one_pass) {
+        const bool on = r < P.n_seqs;
+        if (on) mine = seq_info(P, r);
+        per_head = head_units<Traits>(P, mine, on);
+        tiles = on ? Traits::row_tiles(mine, P) : 0;
       }
+      const int u = per_head * P.kv_heads;
+      int incl = u;
+#pragma unroll
+      for (int d = 1; d < 32; d <<= 1) {
+        const int o = __shfl_up_sync(0xffffffffu, incl, d);
+        if (lane >= d) incl += o;
+      }
+      const int n = __reduce_add_sync(0xffffffffu, tiles);
+      if (lane == 31) {
+        w.sums[0][warp] = incl;
+        w.sums[1][warp] = n;
+      }
+      __syncthreads();
+      int base = carry + incl - u;
+#pragma unroll 1
+      for (int i = 0; i < kW; ++i) {
+        if (i < warp) base += w.sums[0][i];
+        carry += w.sums[0][i];
+        if (pass == 0) items += w.sums[1][i] * P.kv_heads;
+      }
+      if (pass == 1) {
+#pragma unroll 1
+        for (int e = 0; e < 2; ++e) {
+          const int off = sh.cut(min(cta + e, sh.ctas)) - base;
+          if (off >= 0 && off < u) {
+            w.slot[e].r = r;
+            w.slot[e].base = base;
+            w.slot[e].per_head = per_head;
+            w.slot[e].s = mine;
+          }
+        }
+      }
+      __syncthreads();
     }
-    __syncthreads();
-    if (carry > sh.cut(min(cta + 1, sh.ctas))) break;   // both boundaries are behind
+    if (pass == 0) sh = Shares(carry, items, (int)gridDim.x, Traits::kLeast);
   }
-  const Shares sh(total, items, (int)gridDim.x, Traits::kLeast);
   if (warp < 2) {   // a warp a boundary
     WorkSlot& sl = w.slot[warp];
     const int cut = sh.cut(min(cta + warp, sh.ctas));

@@ -35,7 +35,6 @@ constexpr int kAcThreads = 512;                // warps: keys, values, S x 2, P 
 constexpr int kRing = 5;                       // slots of keys, and as many of values
 constexpr int kSegs = 4;
 constexpr int kCheckers = 2;
-constexpr uint64_t kAcWaitLimitNs = 2000000000ull;
 constexpr int kRegsOther = 56, kRegsSoftmax = 200;
 static_assert(8 * 32 * (kRegsOther + kRegsSoftmax) <= kAcThreads * 128, "register split");
 
@@ -207,7 +206,7 @@ __global__ void __launch_bounds__(kAcThreads, 1) k_attn_chunk(const __grid_const
   volatile int* abort_flag = &abort_s;
   const int box_shift = min(P.page_shift, 6), box = 1 << box_shift;   // rows of a TMA box
   const auto wait_warp = [&](uint64_t* bar, uint32_t parity) {
-    return mbar_wait_warp(bar, parity, abort_flag, P.err);
+    return mbar_wait_warp(bar, parity, abort_flag);
   };
   // A half's units end where its last row's keys end.
   const auto half_tok = [&](const Segment& g, int h) { return (2 * g.rt + h) * P.half_tokens; };   // its first token
@@ -410,11 +409,10 @@ __global__ void __launch_bounds__(kAcThreads, 1) k_attn_chunk(const __grid_const
       }
       // whatever was issued is over before TMEM goes back
       __syncwarp();
-      if (one) {
-        mma_commit(&drain_bar[role]);
-        mbar_wait_bounded(&drain_bar[role], 0u, nullptr, P.err, kAcWaitLimitNs, kDevErrTimeout);
+      commit_to(&drain_bar[role], one);
+#pragma unroll 1
+      for (int left = kWaitTries; left > 0 && !__all_sync(0xffffffffu, mbar_try_wait_sleep(&drain_bar[role], 0u, 1000u)); --left) {
       }
-      __syncwarp();
     } else {
       // ---------------------------------------------------------- values that some row does not see
       uint32_t vs = 0, vph = 0u;
@@ -628,7 +626,7 @@ __global__ void __launch_bounds__(kAcThreads, 1) k_attn_chunk(const __grid_const
         if (t + 1 < end && ok) have_s();
       }
       if (!ok) break;
-      // ---- this segment's result, 64 channels at a time: to the output, or (phase 0) to the item's parts in the workspace,
+      // ---- this segment's result, 32 channels at a time: to the output, or (phase 0) to the item's parts in the workspace,
       // which the warpgroup that arrives last joins in their order (phase 1).
       // Parts: [D / 4][256 rows][4], then [256][2].
       if (g.ta < end) {
@@ -642,20 +640,18 @@ __global__ void __launch_bounds__(kAcThreads, 1) k_attn_chunk(const __grid_const
 #pragma unroll 1
       for (int phase = 0; phase < 2; ++phase) {
 #pragma unroll 1
-        for (int c0 = 0; c0 < D; c0 += 64) {
-          float o[64], sum = l;
+        for (int c0 = 0; c0 < D; c0 += 32) {
+          float o[32], sum = l;
 #pragma unroll
-          for (int e = 0; e < 64; ++e) o[e] = 0.f;
+          for (int e = 0; e < 32; ++e) o[e] = 0.f;
           if (phase == 0) {
             if (g.ta < end) {
-              uint32_t v[2][32];
-              tmem_ld_x32(to + c0, v[0]);
-              tmem_ld_x32(to + c0 + 32, v[1]);
+              uint32_t v[32];
+              tmem_ld_x32(to + c0, v);
               tmem_wait_ld();
-              reg_fence(v[0]);
-              reg_fence(v[1]);
+              reg_fence(v);
 #pragma unroll
-              for (int e = 0; e < 64; ++e) o[e] = __uint_as_float(v[e >> 5][e & 31]);
+              for (int e = 0; e < 32; ++e) o[e] = __uint_as_float(v[e]);
             }
           } else {
             sum = 0.f;
@@ -667,7 +663,7 @@ __global__ void __launch_bounds__(kAcThreads, 1) k_attn_chunk(const __grid_const
               const float fp = ml.x == mm ? 1.f : ex2((ml.x - base) * c);
               sum = fmaf(ml.y, fp, sum);
 #pragma unroll
-              for (int e = 0; e < 64; e += 4) {
+              for (int e = 0; e < 32; e += 4) {
                 const float4 v = __ldcg(reinterpret_cast<const float4*>(sp + (size_t)((c0 + e) * kPartRows + 4 * ri)));
                 o[e] = fmaf(v.x, fp, o[e]);
                 o[e + 1] = fmaf(v.y, fp, o[e + 1]);
@@ -678,39 +674,36 @@ __global__ void __launch_bounds__(kAcThreads, 1) k_attn_chunk(const __grid_const
           }
           if (slot && phase == 0) {
 #pragma unroll
-            for (int e = 0; e < 64; e += 4)
+            for (int e = 0; e < 32; e += 4)
               *reinterpret_cast<float4*>(slot + (size_t)((c0 + e) * kPartRows + 4 * ri)) = make_float4(o[e], o[e + 1], o[e + 2], o[e + 3]);
             continue;
           }
           // A lane has a whole row: four lanes exchange 16-byte pieces until each has one piece of four rows, and write
           // 64 bytes of a row together.
           const float inv = row.vis > 0 ? 1.f / sum : 0.f;
+          uint32_t w[4][4];   // [piece, then row][word]
 #pragma unroll
-          for (int e = 0; e < 64; e += 32) {
-            uint32_t w[4][4];   // [piece, then row][word]
+          for (int i = 0; i < 4; ++i)
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
+            for (int k = 0; k < 4; ++k) w[i][k] = pack_bf16(o[8 * i + 2 * k] * inv, o[8 * i + 2 * k + 1] * inv);
 #pragma unroll
-              for (int k = 0; k < 4; ++k) w[i][k] = pack_bf16(o[e + 8 * i + 2 * k] * inv, o[e + 8 * i + 2 * k + 1] * inv);
+          for (int d = 1; d <= 2; d <<= 1)
 #pragma unroll
-            for (int d = 1; d <= 2; d <<= 1)
+            for (int i = 0; i < 4; ++i) {
+              if (i & d) continue;
 #pragma unroll
-              for (int i = 0; i < 4; ++i) {
-                if (i & d) continue;
-#pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                  const bool up = (lane & d) != 0;
-                  const uint32_t got = __shfl_xor_sync(0xffffffffu, up ? w[i][k] : w[i + d][k], d);
-                  w[i][k] = up ? got : w[i][k];
-                  w[i + d][k] = up ? w[i + d][k] : got;
-                }
+              for (int k = 0; k < 4; ++k) {
+                const bool up = (lane & d) != 0;
+                const uint32_t got = __shfl_xor_sync(0xffffffffu, up ? w[i][k] : w[i + d][k], d);
+                w[i][k] = up ? got : w[i][k];
+                w[i + d][k] = up ? w[i + d][k] : got;
               }
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-              const int64_t dst = __shfl_sync(0xffffffffu, mine, (lane & ~3) + r);
-              if (dst >= 0)
-                *reinterpret_cast<uint4*>(P.out + dst + c0 + e + 8 * (lane & 3)) = make_uint4(w[r][0], w[r][1], w[r][2], w[r][3]);
             }
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            const int64_t dst = __shfl_sync(0xffffffffu, mine, (lane & ~3) + r);
+            if (dst >= 0)
+              *reinterpret_cast<uint4*>(P.out + dst + c0 + 8 * (lane & 3)) = make_uint4(w[r][0], w[r][1], w[r][2], w[r][3]);
           }
         }
         if (phase == 0 && bad_s[at]) {
@@ -762,12 +755,7 @@ __global__ void __launch_bounds__(kAcThreads, 1) k_attn_chunk(const __grid_const
   }
   tc_fence_before();
   __syncthreads();
-  if (abort_s) {
-    // a role gave up: give copies in flight time to land
-    const uint64_t t0 = globaltimer_ns();
-    while (globaltimer_ns() - t0 < 2000000ull) {
-    }
-  }
+  end_of_waits(abort_flag, P.err);
   if (warp == 2) {
     tc_fence_after();
     tmem_dealloc(tmem, 512);

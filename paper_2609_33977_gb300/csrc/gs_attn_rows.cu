@@ -142,7 +142,7 @@ __global__ void __launch_bounds__(RowsCfg<D, WR>::kThreads, 1) k_attn_rows(const
   volatile int* abort_flag = &abort_s;
   const int chunk_shift = min(P.page_shift, 7), chunk = 1 << chunk_shift;   // rows of a TMA box
   const auto wait_warp = [&](uint64_t* bar, uint32_t parity) {
-    return mbar_wait_warp(bar, parity, abort_flag, P.err);
+    return mbar_wait_warp(bar, parity, abort_flag);
   };
 
   if (warp == C::kWarps) {
@@ -501,12 +501,7 @@ __global__ void __launch_bounds__(RowsCfg<D, WR>::kThreads, 1) k_attn_rows(const
     }
   }
   __syncthreads();
-  if (abort_s) {
-    // a role gave up: give copies in flight time to land
-    const uint64_t t0 = globaltimer_ns();
-    while (globaltimer_ns() - t0 < 2000000ull) {
-    }
-  }
+  end_of_waits(abort_flag, P.err);
 }
 
 template <int D, int WR>
