@@ -3,10 +3,10 @@
 //
 // HBM-bound: x, base and out move once (2 r FLOP per element of x and out), A and B
 // once per adapter, all of it in one launch for up to 8 layers.  A tile of M tokens
-// of one request belongs to a cluster of eight CTAs: CTA c contracts an eighth of
-// the inputs, the partial A x [M][r] are summed over the cluster through
-// distributed shared memory in a fixed order, and CTA c then forms an eighth of
-// the outputs.  M is 16 where requests are short (a decode step has one token
+// of one request belongs to a cluster of CL CTAs: CTA c contracts its part of the
+// inputs, the partial A x [M][r] are summed over the cluster through distributed
+// shared memory in a fixed order, and CTA c then forms its part of the outputs.
+// CL is 8 where tiles are few, less where they fill the SMs without.  M is 16 where requests are short (a decode step has one token
 // each) and 64 (32 above rank 64) where they are long, so that A and B come from
 // L2 once per M tokens.
 //
@@ -14,7 +14,8 @@
 // order, so a lane takes 8 consecutive elements of its row as one 16-byte load and
 // feeds them to two MMAs; no operand goes through shared memory.  A x enters the
 // second product as hi + lo bf16 (two MMAs), so that its only rounding to 16 bits
-// is the output's.
+// is the output's.  Loads are unconditional, at clamped addresses: one that depends on
+// a branch waits for the one before it.
 #include "gs_block.cuh"
 
 #include <cooperative_groups.h>
@@ -24,7 +25,6 @@ namespace {
 namespace cg = cooperative_groups;
 
 constexpr int kAdThreads = 256, kAdWarps = kAdThreads / 32;
-constexpr int kAdCluster = 8;
 
 struct AdLayer {
   const uint16_t* x;      // [T][in]
@@ -71,9 +71,8 @@ __device__ __forceinline__ void expand(const AdLayer& L, const uint4* v, const u
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
         const int r = 16 * m + 8 * h + g;
-        base[m][h] = vec && r < nt && col < L.out_n
-                         ? *reinterpret_cast<const uint4*>(L.base + (t0 + r) * L.out_n + col)
-                         : make_uint4(0u, 0u, 0u, 0u);
+        if (vec)   // rows and columns past the last: values that nobody uses
+          base[m][h] = *reinterpret_cast<const uint4*>(L.base + (t0 + min(r, nt - 1)) * L.out_n + min(col, L.out_n - 8));
       }
     float acc[MT][4][4];
 #pragma unroll
@@ -87,22 +86,20 @@ __device__ __forceinline__ void expand(const AdLayer& L, const uint4* v, const u
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         const int o = 32 * blk + 8 * (g >> 1) + 2 * j + (g & 1);   // this lane's row of B in MMA j
-        const uint16_t* src = B + (int64_t)o * rank + s * 4 * E + q * E;
+        const uint16_t* src = B + (int64_t)min(o, L.out_n - 1) * rank + s * 4 * E + q * E;
         w[j][0] = w[j][1] = w[j][2] = w[j][3] = 0u;
-        if (o < L.out_n) {
-          if constexpr (E == 8) {
-            const uint4 c = __ldg(reinterpret_cast<const uint4*>(src));
-            w[j][0] = c.x;
-            w[j][1] = c.y;
-            w[j][2] = c.z;
-            w[j][3] = c.w;
-          } else if constexpr (E == 4) {
-            const uint2 c = __ldg(reinterpret_cast<const uint2*>(src));
-            w[j][0] = c.x;
-            w[j][1] = c.y;
-          } else {
-            w[j][0] = __ldg(reinterpret_cast<const uint32_t*>(src));
-          }
+        if constexpr (E == 8) {
+          const uint4 c = __ldg(reinterpret_cast<const uint4*>(src));
+          w[j][0] = c.x;
+          w[j][1] = c.y;
+          w[j][2] = c.z;
+          w[j][3] = c.w;
+        } else if constexpr (E == 4) {
+          const uint2 c = __ldg(reinterpret_cast<const uint2*>(src));
+          w[j][0] = c.x;
+          w[j][1] = c.y;
+        } else {
+          w[j][0] = __ldg(reinterpret_cast<const uint32_t*>(src));
         }
       }
       constexpr int kMmas = E == 8 ? 2 : 1;
@@ -144,14 +141,19 @@ __device__ __forceinline__ void expand(const AdLayer& L, const uint4* v, const u
   }
 }
 
-// NT: n-tiles of 8 ranks held (rank <= 8 NT); MT: m-tiles of 16 tokens
-template <int NT, int MT>
-__global__ void __launch_bounds__(kAdThreads, 1) __cluster_dims__(kAdCluster, 1, 1) k_adapters(const __grid_constant__ AdParams P) {
+// CTAs of an SM: two where the partial sums (4 NT MT registers) leave room for it
+constexpr int ad_per_sm(int NT, int MT) { return NT * MT <= 8 ? 2 : 1; }
+
+__device__ __forceinline__ void prefetch_l2(const void* p) { asm volatile("prefetch.global.L2 [%0];" ::"l"(p)); }
+
+// NT: n-tiles of 8 ranks held (rank <= 8 NT); MT: m-tiles of 16 tokens; CL: CTAs of a cluster
+template <int NT, int MT, int CL>
+__global__ void __launch_bounds__(kAdThreads, ad_per_sm(NT, MT)) __cluster_dims__(CL, 1, 1) k_adapters(const __grid_constant__ AdParams P) {
   extern __shared__ __align__(16) uint8_t ad_smem[];
   constexpr int M = 16 * MT;
   cg::cluster_group cluster = cg::this_cluster();
   const int c = (int)cluster.block_rank();
-  const int u = (int)(blockIdx.x / kAdCluster);
+  const int u = (int)(blockIdx.x / CL);
   const AdLayer& L = P.layer[blockIdx.y];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, q = lane & 3;
 
@@ -169,7 +171,7 @@ __global__ void __launch_bounds__(kAdThreads, 1) __cluster_dims__(kAdCluster, 1,
   const int nt = (int)min((int64_t)M, end - t0);
   const int id = __ldg(P.ids + r);
   const int nb = (L.out_n + 31) / 32;
-  const int b0 = c * nb / kAdCluster, b1 = (c + 1) * nb / kAdCluster;
+  const int b0 = c * nb / CL, b1 = (c + 1) * nb / CL;
   if (id < 0 || id >= L.n_adapters) {   // no adapter
     if (L.out != L.base) {
       const int64_t c0 = 32 * (int64_t)b0, n = min((int64_t)32 * b1, (int64_t)L.out_n) - c0;
@@ -192,6 +194,16 @@ __global__ void __launch_bounds__(kAdThreads, 1) __cluster_dims__(kAdCluster, 1,
   const uint16_t* A = L.A + (int64_t)id * rank * L.in;
   const uint16_t* B = L.B + (int64_t)id * rank * L.out_n;
 
+  // What the second product reads comes to L2 under the first: this CTA's rows of B, and its columns of the base
+  {
+    const int c0 = 32 * b0, n_col = min(32 * b1, L.out_n) - c0;
+    const char* bp = reinterpret_cast<const char*>(B + (int64_t)c0 * rank);
+    for (int i = threadIdx.x; i * 64 < n_col * rank; i += kAdThreads) prefetch_l2(bp + (int64_t)i * 128);
+    const int lines = (n_col + 63) / 64;
+    for (int i = threadIdx.x; i < lines * nt; i += kAdThreads)
+      prefetch_l2(L.base + (t0 + i / lines) * L.out_n + c0 + min(64 * (i % lines), n_col - 1));
+  }
+
   // ---- A x over this CTA's inputs: blocks of 32, taken by the warps in turn
   float acc[MT][NT][4];
 #pragma unroll
@@ -201,23 +213,25 @@ __global__ void __launch_bounds__(kAdThreads, 1) __cluster_dims__(kAdCluster, 1,
 #pragma unroll
       for (int e = 0; e < 4; ++e) acc[m][j][e] = 0.f;
   const int nk = (L.in + 31) / 32;
-  const int k1 = (c + 1) * nk / kAdCluster;
+  const int k1 = (c + 1) * nk / CL;
   const uint4 zero = make_uint4(0u, 0u, 0u, 0u);
 #pragma unroll 2
-  for (int kb = c * nk / kAdCluster + warp; kb < k1; kb += kAdWarps) {
-    const int k = 32 * kb + 8 * q;
-    const bool in = k < L.in;
+  for (int kb = c * nk / CL + warp; kb < k1; kb += kAdWarps) {
+    const int k = min(32 * kb + 8 * q, L.in - 8);
     uint4 xa[MT][2], wa[NT];
 #pragma unroll
     for (int m = 0; m < MT; ++m)
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const int row = 16 * m + 8 * h + g;
-        xa[m][h] = in && row < nt ? __ldg(reinterpret_cast<const uint4*>(L.x + (t0 + row) * L.in + k)) : zero;
-      }
+      for (int h = 0; h < 2; ++h)
+        xa[m][h] = __ldg(reinterpret_cast<const uint4*>(L.x + (t0 + min(16 * m + 8 * h + g, nt - 1)) * L.in + k));
 #pragma unroll
-    for (int j = 0; j < NT; ++j)
-      wa[j] = in && j < nrt ? __ldg(reinterpret_cast<const uint4*>(A + (int64_t)(8 * j + g) * L.in + k)) : zero;
+    for (int j = 0; j < NT; ++j) wa[j] = __ldg(reinterpret_cast<const uint4*>(A + (int64_t)min(8 * j + g, rank - 1) * L.in + k));
+    if (32 * kb + 32 > L.in && 32 * kb + 8 * q >= L.in) {   // the last block's lanes past the inputs
+#pragma unroll
+      for (int m = 0; m < MT; ++m) xa[m][0] = xa[m][1] = zero;
+#pragma unroll
+      for (int j = 0; j < NT; ++j) wa[j] = zero;
+    }
 #pragma unroll
     for (int m = 0; m < MT; ++m)
 #pragma unroll
@@ -253,14 +267,14 @@ __global__ void __launch_bounds__(kAdThreads, 1) __cluster_dims__(kAdCluster, 1,
   const float scale = __ldg(L.scale + id);
   {
     // CTA c sums an eighth of the elements and gives them to every CTA
-    const int per = n / kAdCluster;   // n is a multiple of 128
+    const int per = n / CL;   // n is a multiple of 128
     for (int i = c * per + (int)threadIdx.x; i < (c + 1) * per; i += kAdThreads) {
       float s = 0.f;
 #pragma unroll
-      for (int w = 0; w < kAdCluster; ++w) s += cluster.map_shared_rank(mine, w)[i];
+      for (int w = 0; w < CL; ++w) s += cluster.map_shared_rank(mine, w)[i];
       s *= scale;
 #pragma unroll
-      for (int w = 0; w < kAdCluster; ++w) cluster.map_shared_rank(sum, w)[i] = s;
+      for (int w = 0; w < CL; ++w) cluster.map_shared_rank(sum, w)[i] = s;
     }
   }
   cluster.sync();
@@ -294,7 +308,7 @@ __global__ void __launch_bounds__(kAdThreads, 1) __cluster_dims__(kAdCluster, 1,
   else expand<MT, 2>(L, frag, B, t0, nt, rank, b0, b1, warp, lane);
 }
 
-template <int NT, int MT>
+template <int NT, int MT, int CL>
 gs_status ad_launch(const AdParams& P, int n, int rank, cudaStream_t s) {
   constexpr int M = 16 * MT;
   // partial sums of the warps, this CTA's and the cluster's; the fragments (4 bytes an
@@ -302,13 +316,22 @@ gs_status ad_launch(const AdParams& P, int n, int rank, cudaStream_t s) {
   const size_t smem = (size_t)(kAdWarps + 2) * M * rank * 4;
   constexpr size_t kMost = (size_t)(kAdWarps + 2) * M * (8 * NT) * 4;
   static const cudaError_t attr =
-      cudaFuncSetAttribute(k_adapters<NT, MT>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kMost);
+      cudaFuncSetAttribute(k_adapters<NT, MT, CL>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kMost);
   if (attr != cudaSuccess) return GS_ERR_CUDA;
   const int64_t units = P.T / M + P.n_seqs;
-  if (units * kAdCluster > INT32_MAX) return GS_ERR_UNSUPPORTED;
-  k_adapters<NT, MT><<<dim3((unsigned)(units * kAdCluster), (unsigned)n), kAdThreads, smem, s>>>(P);
+  if (units * CL > INT32_MAX) return GS_ERR_UNSUPPORTED;
+  k_adapters<NT, MT, CL><<<dim3((unsigned)(units * CL), (unsigned)n), kAdThreads, smem, s>>>(P);
   note_launch();
   return cudaGetLastError() == cudaSuccess ? GS_OK : GS_ERR_CUDA;
+}
+
+// The largest cluster with which all tiles are resident at once: more CTAs a tile shorten
+// it as long as they do not queue.
+template <int NT, int MT>
+gs_status ad_cluster(const AdParams& P, int n, int rank, cudaStream_t s) {
+  const int64_t tiles = (P.T / (16 * MT) + P.n_seqs) * n, room = (int64_t)sm_count() * ad_per_sm(NT, MT);
+  if (tiles * 8 <= room) return ad_launch<NT, MT, 8>(P, n, rank, s);
+  return tiles * 4 <= room ? ad_launch<NT, MT, 4>(P, n, rank, s) : ad_launch<NT, MT, 2>(P, n, rank, s);
 }
 
 }  // namespace
@@ -336,10 +359,10 @@ gs_status launch_adapters(const gs_adapter_layer* layers, int n, const int32_t* 
     rank = rank > L.rank ? rank : L.rank;
   }
   const bool longer = T >= (int64_t)32 * n_seqs;
-  if (rank <= 16) return longer ? ad_launch<2, 4>(P, n, rank, s) : ad_launch<2, 1>(P, n, rank, s);
-  if (rank <= 32) return longer ? ad_launch<4, 4>(P, n, rank, s) : ad_launch<4, 1>(P, n, rank, s);
-  if (rank <= 64) return longer ? ad_launch<8, 4>(P, n, rank, s) : ad_launch<8, 1>(P, n, rank, s);
-  return longer ? ad_launch<16, 2>(P, n, rank, s) : ad_launch<16, 1>(P, n, rank, s);
+  if (rank <= 16) return longer ? ad_cluster<2, 2>(P, n, rank, s) : ad_cluster<2, 1>(P, n, rank, s);
+  if (rank <= 32) return longer ? ad_cluster<4, 2>(P, n, rank, s) : ad_cluster<4, 1>(P, n, rank, s);
+  if (rank <= 64) return longer ? ad_cluster<8, 4>(P, n, rank, s) : ad_cluster<8, 1>(P, n, rank, s);
+  return longer ? ad_cluster<16, 2>(P, n, rank, s) : ad_cluster<16, 1>(P, n, rank, s);
 }
 
 }  // namespace gs
