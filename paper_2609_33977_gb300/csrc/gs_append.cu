@@ -4,15 +4,18 @@
 // c and s the angle table's rows of the token's position.
 //
 // Bound by HBM at long chunks (every element of q, k, v read and written once),
-// by latency at one token.  A block takes one token (or a part of its heads): the
-// whole block looks its sequence up once, and a thread turns 8 channel pairs of a
-// head, two 16-byte loads and stores.
+// by latency at few tokens: the look-up of a token's sequence, its length, its page
+// are loads that wait for one another.  A block takes one token (or a part of its
+// heads), a thread 8 channel pairs of a head: two 16-byte loads and stores.  Up to 32
+// sequences are looked up by every warp for itself, one load each and a ballot;
+// more by the whole block.  (Two or four tokens a block: 7 and 40 % slower at 3000
+// tokens, since a thread's loads then queue behind each other's look-ups.)
 #include "gs_block.cuh"
 
 namespace gs {
 namespace {
 
-constexpr int kAppThreads = 256;
+constexpr int kAppThreads = 512;   // at most
 
 struct AppendParams {
   const uint16_t* q;
@@ -33,24 +36,32 @@ struct AppendParams {
 __global__ void __launch_bounds__(kAppThreads) k_cache_append(const AppendParams P) {
   const int64_t t = blockIdx.x / (unsigned)P.parts;
   const int per = P.head_dim / 16;   // threads of a head
-  const int item = (int)(blockIdx.x % (unsigned)P.parts) * kAppThreads + (int)threadIdx.x;
+  const int item = (int)(blockIdx.x % (unsigned)P.parts) * (int)blockDim.x + (int)threadIdx.x;
   int head = item / per;
   const int i = item % per;
   const bool on = head < P.q_heads + 2 * P.kv_heads;
   const int kind = head < P.q_heads ? 0 : head < P.q_heads + P.kv_heads ? 1 : 2;   // q, k, v
   head -= kind == 0 ? 0 : kind == 1 ? P.q_heads : P.q_heads + P.kv_heads;
   const int64_t D = P.head_dim;
-  uint4 a = make_uint4(0u, 0u, 0u, 0u), b = a;
-  if (on) {   // before the look-up: neither needs the other
-    const uint16_t* src = (kind == 0 ? P.q + t * P.q_stride : kind == 1 ? P.k + t * P.k_stride : P.v + t * P.v_stride) + head * D;
-    a = __ldcs(reinterpret_cast<const uint4*>(src) + i);
-    b = __ldcs(reinterpret_cast<const uint4*>(src + D / 2) + i);
-  }
-  const int seq = block_count_le(P.offsets, P.n_seqs, (int)t);
+  // before the look-up: neither needs the other.  Threads past the last head read the first one's.
+  const uint16_t* src = (kind == 0 ? P.q + t * P.q_stride : kind == 1 ? P.k + t * P.k_stride : P.v + t * P.v_stride) +
+                        (on ? head * D : 0);
+  uint4 a = __ldcs(reinterpret_cast<const uint4*>(src) + i), b = __ldcs(reinterpret_cast<const uint4*>(src + D / 2) + i);
+  int seq;
   int64_t pos = -1;
-  if (seq < P.n_seqs) {
-    const int64_t first = __ldg(P.offsets + seq), end = __ldg(P.offsets + seq + 1);
-    if (t >= first) pos = (int64_t)__ldg(P.kv_lens + seq) - (end - first) + (t - first);
+  if (P.n_seqs <= 32) {
+    const int s = min((int)(threadIdx.x & 31), P.n_seqs - 1);
+    const int first = __ldg(P.offsets + s), end = __ldg(P.offsets + s + 1), kv = __ldg(P.kv_lens + s);
+    seq = __popc(__ballot_sync(0xffffffffu, (int)(threadIdx.x & 31) < P.n_seqs && end <= t));
+    const int64_t mine = t >= first ? (int64_t)kv - ((int64_t)end - first) + (t - first) : -1;
+    const int64_t got = __shfl_sync(0xffffffffu, mine, seq & 31);
+    if (seq < P.n_seqs) pos = got;
+  } else {
+    seq = block_count_le(P.offsets, P.n_seqs, (int)t);
+    if (seq < P.n_seqs) {
+      const int64_t first = __ldg(P.offsets + seq), end = __ldg(P.offsets + seq + 1);
+      if (t >= first) pos = (int64_t)__ldg(P.kv_lens + seq) - (end - first) + (t - first);
+    }
   }
   if (!on) return;
   const bool turn = pos >= 0 && pos < P.n_pos;
@@ -114,9 +125,10 @@ gs_status launch_cache_append(const gs_paged_cache& c, const gs_seq_batch& b, co
   P.head_dim = c.head_dim;
   const int items = (q_heads + 2 * c.kv_heads) * (c.head_dim / 16);
   P.parts = (items + kAppThreads - 1) / kAppThreads;
+  const unsigned threads = (unsigned)((items + P.parts - 1) / P.parts + 31) / 32 * 32;
   const int64_t blocks = b.tokens * P.parts;
   if (blocks > INT32_MAX) return GS_ERR_UNSUPPORTED;
-  k_cache_append<<<(unsigned)blocks, kAppThreads, 0, s>>>(P);
+  k_cache_append<<<(unsigned)blocks, threads, 0, s>>>(P);
   note_launch();
   return cudaGetLastError() == cudaSuccess ? GS_OK : GS_ERR_CUDA;
 }
