@@ -231,7 +231,7 @@ __device__ __forceinline__ Shares divide_work(const AttnParams& P, int cta, Work
   static_assert(kW >= 2 && kW <= 32 && THREADS % 32 == 0, "block");
   const bool one_pass = P.n_seqs <= THREADS;   // a sequence a thread: looked at once
   SeqInfo mine = {0, 0, 0, 0, 0};
-  int per_head = 0, tiles = 0, items = 0;
+  int per_head = 0, base = 0, items = 0;
   Shares sh(0, 0, 1, 1);
   if (threadIdx.x < 2) w.slot[threadIdx.x].r = P.n_seqs;
   // first the sums, then the sequences that hold this CTA's boundaries
@@ -245,33 +245,29 @@ __device__ __forceinline__ Shares divide_work(const AttnParams& P, int cta, Work
         const bool on = r < P.n_seqs;
         if (on) mine = seq_info(P, r);
         per_head = head_units<Traits>(P, mine, on);
-        tiles = on ? Traits::row_tiles(mine, P) : 0;
-      }
-      const int u = per_head * P.kv_heads;
-      int incl = u;
+        const int n = __reduce_add_sync(0xffffffffu, on ? Traits::row_tiles(mine, P) : 0);
+        int incl = per_head * P.kv_heads;
 #pragma unroll
-      for (int d = 1; d < 32; d <<= 1) {
-        const int o = __shfl_up_sync(0xffffffffu, incl, d);
-        if (lane >= d) incl += o;
-      }
-      const int n = __reduce_add_sync(0xffffffffu, tiles);
-      if (lane == 31) {
-        w.sums[0][warp] = incl;
-        w.sums[1][warp] = n;
-      }
-      __syncthreads();
-      int base = carry + incl - u;
-#pragma unroll 1
-      for (int i = 0; i < kW; ++i) {
-        if (i < warp) base += w.sums[0][i];
-        carry += w.sums[0][i];
-        if (pass == 0) items += w.sums[1][i] * P.kv_heads;
+        for (int d = 1; d < 32; d <<= 1) {
+          const int o = __shfl_up_sync(0xffffffffu, incl, d);
+          if (lane >= d) incl += o;
+        }
+        if (lane == 31) {
+          w.sums[0][warp] = incl;
+          w.sums[1][warp] = n;
+        }
+        __syncthreads();
+        const int sum = lane < kW ? w.sums[0][lane] : 0;
+        base = carry + __reduce_add_sync(0xffffffffu, lane < warp ? sum : 0) + incl - per_head * P.kv_heads;
+        carry += __reduce_add_sync(0xffffffffu, sum);
+        if (pass == 0) items += __reduce_add_sync(0xffffffffu, lane < kW ? w.sums[1][lane] : 0) * P.kv_heads;
+        if (!one_pass) __syncthreads();   // the sums are written again
       }
       if (pass == 1) {
 #pragma unroll 1
         for (int e = 0; e < 2; ++e) {
           const int off = sh.cut(min(cta + e, sh.ctas)) - base;
-          if (off >= 0 && off < u) {
+          if (off >= 0 && off < per_head * P.kv_heads) {
             w.slot[e].r = r;
             w.slot[e].base = base;
             w.slot[e].per_head = per_head;
@@ -279,10 +275,10 @@ __device__ __forceinline__ Shares divide_work(const AttnParams& P, int cta, Work
           }
         }
       }
-      __syncthreads();
     }
     if (pass == 0) sh = Shares(carry, items, (int)gridDim.x, Traits::kLeast);
   }
+  __syncthreads();
   if (warp < 2) {   // a warp a boundary
     WorkSlot& sl = w.slot[warp];
     const int cut = sh.cut(min(cta + warp, sh.ctas));

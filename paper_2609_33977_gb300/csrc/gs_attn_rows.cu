@@ -6,7 +6,9 @@
 // of units in flight per SM; a segment's queries come with its first unit), eight
 // compute with m16n8k16: WR row tiles of 16 x WK shares of the unit's keys, each warp
 // with its own running maximum, sum and output, joined over the WK warps once per
-// segment, in the segment's last stage.  Unused MMA rows cost nothing that matters.
+// segment, in the segment's last stage.  With one row tile, a warp's keys are read by
+// no other warp, so it leaves its part in their place without waiting, and goes on
+// unless it has a row to join.  Unused MMA rows cost nothing that matters.
 #include "gs_attn.cuh"
 
 #include <mutex>
@@ -114,11 +116,11 @@ __global__ void __launch_bounds__(RowsCfg<D, WR>::kThreads, 1) k_attn_rows(const
   __shared__ __align__(8) uint64_t full_bar[C::kStages];
   __shared__ __align__(8) uint64_t empty_bar[C::kStages];
   __shared__ __align__(8) uint64_t qempty_bar[C::kQSlots];
-  __shared__ __align__(8) uint64_t join_bar;
+  __shared__ __align__(8) uint64_t join_bar, meet_bar;
   __shared__ Segment segs[C::kStages];   // of the unit in a stage, where it is the segment's first; r < 0: the end
   __shared__ WorkShared work;
-  __shared__ float2 join_ml[C::kWarps * 16];   // [WK][rows]: maximum and sum
-  __shared__ int abort_s, last_s, bad_s[2];
+  __shared__ float2 join_ml[2][C::kWarps * 16];   // [WK][rows]: maximum and sum
+  __shared__ int abort_s, last_s, bad_s[4];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(ar_smem_raw) + 1023) & ~uintptr_t(1023));
   uint8_t* qsm = smem + C::kStages * C::kStageBytes;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -130,8 +132,9 @@ __global__ void __launch_bounds__(RowsCfg<D, WR>::kThreads, 1) k_attn_rows(const
     }
     for (int s = 0; s < C::kQSlots; ++s) mbar_init(&qempty_bar[s], C::kWarps);
     mbar_init(&join_bar, C::kWarps);
+    mbar_init(&meet_bar, C::kWarps);
     abort_s = 0;
-    bad_s[0] = bad_s[1] = 0;
+    for (int i = 0; i < 4; ++i) bad_s[i] = 0;
     fence_mbar_init();
   }
   if (threadIdx.x == C::kWarps * 32) {
@@ -215,13 +218,13 @@ __global__ void __launch_bounds__(RowsCfg<D, WR>::kThreads, 1) k_attn_rows(const
     constexpr int kKeys = kTile / WK;              // this warp's keys of a unit: 16, 32 or 64
     constexpr int kSub = kKeys < 32 ? kKeys : 32;  // keys between two steps of the running maximum
     constexpr int kNt = kSub / 8;
-    uint32_t jph = 0;
+    uint32_t jph = 0, mph = 0;
     // the compute warps' barrier, bounded like every wait: false when some role gave up
     const auto meet = [&]() {
       __syncwarp();
-      if (lane == 0) mbar_arrive(&join_bar);
-      const bool met = wait_warp(&join_bar, jph);
-      jph ^= 1u;
+      if (lane == 0) mbar_arrive(&meet_bar);
+      const bool met = wait_warp(&meet_bar, mph);
+      mph ^= 1u;
       return met;
     };
     uint32_t st = 0, ph = 0u, turn = 0, qs = 0;
@@ -250,18 +253,17 @@ __global__ void __launch_bounds__(RowsCfg<D, WR>::kThreads, 1) k_attn_rows(const
       const int row0 = 16 * wr + gq;
       uint32_t qf[D / 16][4];
       int seen[2];
-      const uint32_t flip = P.negate ? 0x80008000u : 0u;
+      const uint32_t qa = smem_u32(qsm + qs * C::kQBytes + (16 * wr + (lane & 15)) * C::kQRow + (lane >> 4) * 16);
 #pragma unroll
-      for (int hf = 0; hf < 2; ++hf) {
-        const int row = row0 + 8 * hf;
-        seen[hf] = row < g.s.rows ? g.s.seen(row_token(P, row)) : 0;
-        const uint32_t* src = reinterpret_cast<const uint32_t*>(qsm + qs * C::kQBytes + row * C::kQRow) + qd;
+      for (int ks = 0; ks < D / 16; ++ks) ldsm4(qf[ks], qa + 32 * ks);
+      if (P.negate) {
 #pragma unroll
-        for (int ks = 0; ks < D / 16; ++ks) {
-          qf[ks][hf] = src[8 * ks] ^ flip;
-          qf[ks][hf + 2] = src[8 * ks + 4] ^ flip;
-        }
+        for (int ks = 0; ks < D / 16; ++ks)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) qf[ks][e] ^= 0x80008000u;
       }
+#pragma unroll
+      for (int hf = 0; hf < 2; ++hf) seen[hf] = row0 + 8 * hf < g.s.rows ? g.s.seen(row_token(P, row0 + 8 * hf)) : 0;
       __syncwarp();
       if (lane == 0) mbar_arrive(&qempty_bar[qs]);
       if (++qs == C::kQSlots) qs = 0;
@@ -388,30 +390,49 @@ __global__ void __launch_bounds__(RowsCfg<D, WR>::kThreads, 1) k_attn_rows(const
         }
       }
       if (!ok) break;
-      // ---- join the WK warps of every row tile, in the stage that every warp has read
+      // ---- join the WK warps of every row tile, in the stage: [row][D] of warp w lies where its own keys and values
+      // were (one row tile), else in w's eighth
       ++turn;
-      if (!meet()) break;
-      float* join = reinterpret_cast<float*>(smem + st * C::kStageBytes);   // [WK][rows][D]
+      if (WR > 1 && !meet()) break;
+      const auto part_row = [&](int w, int row) -> float* {
+        uint8_t* stage = smem + st * C::kStageBytes;
+        if (WR > 1) return reinterpret_cast<float*>(stage) + (w * C::kRows + row) * D;
+        // 16 keys: kSlabs pieces of 2 KB in each operand, 2048 / (4 D) rows a piece
+        constexpr int kPer = 512 / D;
+        const int piece = row / kPer, key = 16 * w, op = piece / kSlabs, sl = piece % kSlabs;
+        return reinterpret_cast<float*>(stage + op * C::kOpBytes + ((key >> chunk_shift) * kSlabs + sl) * slab +
+                                        (key & (chunk - 1)) * 128) + (row % kPer) * D;
+      };
+      if (turn > 1u && WR == 1) {   // the join before is through: its barrier may be used again
+        if (!wait_warp(&join_bar, jph)) break;
+        jph ^= 1u;
+      }
       if (on) {
 #pragma unroll
         for (int hf = 0; hf < 2; ++hf) {
           const int row = row0 + 8 * hf;
           const float sum = quad_sum(l[hf]);
           if (row < g.s.rows) {
-            float* dst = join + (wk * C::kRows + row) * D + 2 * qd;
+            float* dst = part_row(wk, row) + 2 * qd;
 #pragma unroll
             for (int j = 0; j < D / 8; ++j) *reinterpret_cast<float2*>(dst + 8 * j) = make_float2(o[j][2 * hf], o[j][2 * hf + 1]);
-            if (qd == 0) join_ml[wk * C::kRows + row] = make_float2(m[hf], sum);
+            if (qd == 0) join_ml[turn & 1][wk * C::kRows + row] = make_float2(m[hf], sum);
           }
         }
-        if (bad) bad_s[turn & 1] = 1;
+        if (bad) bad_s[turn & 3] = 1;
       }
-      if (!meet()) break;
-      const bool fix = bad_s[turn & 1] != 0;
-      if (threadIdx.x == 0) bad_s[(turn + 1) & 1] = 0;
+      if constexpr (WR == 1) {
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&join_bar);
+        if (warp < g.s.rows && !wait_warp(&join_bar, jph)) break;   // the others look when they come to the next join
+      } else {
+        if (!meet()) break;
+      }
+      const bool fix = bad_s[turn & 3] != 0;
+      if (threadIdx.x == 0) bad_s[(turn + 2) & 3] = 0;
       float* slot = g.parts > 1 ? part_slot(P, g.first_cta, g.part, C::kRows, D) : nullptr;
       for (int row = warp; row < g.s.rows; row += C::kWarps) {   // a warp a row
-        const float2 ml = lane < WK ? join_ml[lane * C::kRows + row] : make_float2(-INFINITY, 0.f);
+        const float2 ml = lane < WK ? join_ml[turn & 1][lane * C::kRows + row] : make_float2(-INFINITY, 0.f);
         float mm = ml.x;
 #pragma unroll
         for (int d = WK / 2; d > 0; d >>= 1) mm = fmaxf(mm, __shfl_xor_sync(0xffffffffu, mm, d));
@@ -428,7 +449,7 @@ __global__ void __launch_bounds__(RowsCfg<D, WR>::kThreads, 1) k_attn_rows(const
         for (int w = 0; w < WK; ++w) {
           const float f = __shfl_sync(0xffffffffu, fw, w);
           float v[kC];
-          L::unpack(reinterpret_cast<const typename L::V*>(join + (w * C::kRows + row) * D)[lane], v);
+          L::unpack(reinterpret_cast<const typename L::V*>(part_row(w, row))[lane], v);
 #pragma unroll
           for (int c = 0; c < kC; ++c) a[c] = fmaf(v[c], f, a[c]);
         }
