@@ -7,12 +7,15 @@
 namespace gs {
 namespace {
 
-// Arrival counters (two a CTA), then the parts of split items.
+// Arrival counters (two a CTA for the chunk kernel, one for the few-row kernel), then the
+// parts of split items, each kernel's its own: the two launches of a step overlap.
 constexpr int64_t kCounterBytes = 4096;
 constexpr int kMaxCtas = 256;
-static_assert(kCounterBytes >= 2 * 4 * kMaxCtas, "two counters a CTA");
+static_assert(kCounterBytes >= 3 * 4 * kMaxCtas, "three counters a CTA");
 
 int attention_ctas() { return std::min(sm_count(), kMaxCtas); }
+
+size_t part_bytes(int rows, int head_dim) { return (size_t)attention_ctas() * 2 * (size_t)rows * (size_t)(head_dim + 2) * 4; }
 
 // The few-row kernel serves sequences of at most attn_rows_most() rows, the chunk kernel
 // the others.  Where all sequences are as long as the longest (known from the sizes
@@ -35,8 +38,9 @@ bool attention_units_fit(const gs_paged_cache& c, const gs_seq_batch& b, int32_t
 }
 
 size_t attention_workspace_bytes(const gs_paged_cache& c, const gs_seq_batch& b, int32_t q_heads) {
-  const int rows = kernels_of(b, q_heads / c.kv_heads).chunk ? attn_chunk_rows() : attn_rows_most();
-  return (size_t)kCounterBytes + (size_t)attention_ctas() * 2 * (size_t)rows * (size_t)(c.head_dim + 2) * 4;
+  const Kernels k = kernels_of(b, q_heads / c.kv_heads);
+  return (size_t)kCounterBytes + (k.chunk ? part_bytes(attn_chunk_rows(), c.head_dim) : 0) +
+         (k.few ? part_bytes(attn_rows_most(), c.head_dim) : 0);
 }
 
 gs_status launch_paged_attention(const gs_paged_cache& c, const gs_seq_batch& b, const void* q, int64_t q_stride,
@@ -48,8 +52,6 @@ gs_status launch_paged_attention(const gs_paged_cache& c, const gs_seq_batch& b,
   P.offsets = b.offsets_dev;
   P.kv_lens = b.kv_lens_dev;
   P.table = b.table_dev;
-  P.cnt = static_cast<int32_t*>(ws);
-  P.parts = reinterpret_cast<float*>(static_cast<uint8_t*>(ws) + kCounterBytes);
   P.err = device_error_flag();
   if (!P.err) return GS_ERR_CUDA;
   P.q_stride = q_stride;
@@ -69,30 +71,37 @@ gs_status launch_paged_attention(const gs_paged_cache& c, const gs_seq_batch& b,
   const uint64_t rows = (uint64_t)c.pages * c.kv_heads * c.page_size, D = (uint64_t)c.head_dim;
   const uint32_t slabs = (uint32_t)D / 64;
   const Kernels k = kernels_of(b, P.group);
-  if (k.few) {
-    const uint32_t box = (uint32_t)attn_rows_box(c.page_size);
-    if (!encode_tmap_slabs_bf16(&P.kmap, c.k_dev, D, rows, box, slabs) || !encode_tmap_slabs_bf16(&P.vmap, c.v_dev, D, rows, box, slabs))
+  P.two_launches = k.few && k.chunk;
+  int32_t* cnt = static_cast<int32_t*>(ws);
+  uint8_t* parts = static_cast<uint8_t*>(ws) + kCounterBytes;
+  if (k.chunk) {   // first: it is the longer one, and the other fills the SMs as they come free
+    const uint32_t box = (uint32_t)attn_chunk_box(c.page_size);
+    // keys of a page smaller than a unit arrive slab by slab
+    if (!encode_tmap_slabs_bf16(&P.kmap, c.k_dev, D, rows, box, (int)box == attn_chunk_tile() ? slabs : 1u) ||
+        !encode_tmap_slabs_bf16(&P.vmap, c.v_dev, D, rows, box, slabs))
       return GS_ERR_CUDA;
-    P.min_rows = 1;
-    P.max_rows = attn_rows_most();
-    P.zero_rest = !k.chunk;
-    const int most = (int)std::min((int64_t)b.max_new * P.group, (int64_t)attn_rows_most());
-    const gs_status st = launch_attn_rows(P, c.head_dim, most, attention_ctas(), s);
-    if (st != GS_OK || !k.chunk) return st;
+    P.half_tokens = attn_chunk_half_tokens(P.group);
+    const uint64_t dims[3] = {D, (uint64_t)q_heads, (uint64_t)b.tokens}, strides[2] = {D * 2, (uint64_t)q_stride * 2};
+    const uint32_t qbox[3] = {64, (uint32_t)P.group, (uint32_t)P.half_tokens};
+    if (!encode_tmap_nd_bf16(&P.qmap, q, 3, dims, strides, qbox, 128)) return GS_ERR_CUDA;
+    P.cnt = cnt;
+    P.parts = reinterpret_cast<float*>(parts);
+    P.min_rows = k.few ? attn_rows_most() + 1 : 1;
+    P.max_rows = INT32_MAX;
+    P.zero_rest = !k.few;
+    const gs_status st = launch_attn_chunk(P, c.head_dim, attention_ctas(), s);
+    if (st != GS_OK || !k.few) return st;
   }
-  const uint32_t box = (uint32_t)attn_chunk_box(c.page_size);
-  // keys of a page smaller than a unit arrive slab by slab
-  if (!encode_tmap_slabs_bf16(&P.kmap, c.k_dev, D, rows, box, (int)box == attn_chunk_tile() ? slabs : 1u) ||
-      !encode_tmap_slabs_bf16(&P.vmap, c.v_dev, D, rows, box, slabs))
+  const uint32_t box = (uint32_t)attn_rows_box(c.page_size);
+  if (!encode_tmap_slabs_bf16(&P.kmap, c.k_dev, D, rows, box, slabs) || !encode_tmap_slabs_bf16(&P.vmap, c.v_dev, D, rows, box, slabs))
     return GS_ERR_CUDA;
-  P.half_tokens = attn_chunk_half_tokens(P.group);
-  const uint64_t dims[3] = {D, (uint64_t)q_heads, (uint64_t)b.tokens}, strides[2] = {D * 2, (uint64_t)q_stride * 2};
-  const uint32_t qbox[3] = {64, (uint32_t)P.group, (uint32_t)P.half_tokens};
-  if (!encode_tmap_nd_bf16(&P.qmap, q, 3, dims, strides, qbox, 128)) return GS_ERR_CUDA;
-  P.min_rows = k.few ? attn_rows_most() + 1 : 1;
-  P.max_rows = INT32_MAX;
-  P.zero_rest = !k.few;
-  return launch_attn_chunk(P, c.head_dim, attention_ctas(), s);
+  P.cnt = cnt + 2 * kMaxCtas;
+  P.parts = reinterpret_cast<float*>(parts + (k.chunk ? part_bytes(attn_chunk_rows(), c.head_dim) : 0));
+  P.min_rows = 1;
+  P.max_rows = attn_rows_most();
+  P.zero_rest = !k.chunk;
+  const int most = (int)std::min((int64_t)b.max_new * P.group, (int64_t)attn_rows_most());
+  return launch_attn_rows(P, c.head_dim, most, attention_ctas(), s);
 }
 
 }  // namespace gs

@@ -34,6 +34,8 @@ struct AttnParams {
   int32_t half_tokens;      // chunk kernel: whole tokens in 128 rows
   int32_t min_rows, max_rows;   // sequences with that many rows (new tokens x query heads a key head) are this kernel's
   int32_t zero_rest;            // no other kernel runs: zeros for the tokens of sequences above max_rows, and of none
+  int32_t two_launches;         // chunk kernel: lets the few-row launch behind it begin on SMs that are through; that one: waits
+                                // for it at its end, so that whatever follows does too
   float scale_log2;             // |scale| log2(e)
   int32_t negate;               // scale < 0: the queries' signs are flipped
 };

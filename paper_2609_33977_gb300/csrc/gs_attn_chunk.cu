@@ -39,7 +39,7 @@ constexpr int kRegsOther = 56, kRegsSoftmax = 200;
 static_assert(8 * 32 * (kRegsOther + kRegsSoftmax) <= kAcThreads * 128, "register split");
 
 struct ChunkTraits {
-  static constexpr int kLeast = 8, kSnap = 3, kOver = 5;
+  static constexpr int kLeast = 8, kSnap = 3, kOver = 9;
   static constexpr bool kOneTile = false;
   // A half holds whole tokens (P.half_tokens: group x that of its 128 lanes are used), an item two halves.
   static __device__ __forceinline__ int row_tiles(const SeqInfo& s, const AttnParams& P) {
@@ -164,6 +164,7 @@ __global__ void __launch_bounds__(kAcThreads, 1) k_attn_chunk(const __grid_const
   uint8_t* ring_v = ring_k + kRing * C::kOpBytes;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int cta = (int)blockIdx.x;
+  if (P.two_launches) asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   if (threadIdx.x == 0) {
     for (int s = 0; s < kRing; ++s) {
       mbar_init(&kfull_bar[s], 1);

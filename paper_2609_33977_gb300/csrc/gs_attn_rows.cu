@@ -20,7 +20,7 @@ using namespace sm100;
 constexpr int kTile = 128;
 
 struct FewTraits {
-  static constexpr int kLeast = 2, kSnap = 1, kOver = 0;
+  static constexpr int kLeast = 2, kSnap = 1, kOver = 1;
   static constexpr bool kOneTile = true;
   static __device__ __forceinline__ int row_tiles(const SeqInfo& s, const AttnParams& P) {
     return s.rows >= P.min_rows && s.rows <= P.max_rows ? 1 : 0;
@@ -523,6 +523,7 @@ __global__ void __launch_bounds__(RowsCfg<D, WR>::kThreads, 1) k_attn_rows(const
   }
   __syncthreads();
   end_of_waits(abort_flag, P.err);
+  if (P.two_launches) asm volatile("griddepcontrol.wait;" ::: "memory");
 }
 
 template <int D, int WR>
@@ -530,9 +531,19 @@ gs_status rows_launch(const AttnParams& P, int ctas, cudaStream_t s) {
   using C = RowsCfg<D, WR>;
   static const cudaError_t attr = cudaFuncSetAttribute(k_attn_rows<D, WR>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::kSmem);
   if (attr != cudaSuccess) return GS_ERR_CUDA;
-  k_attn_rows<D, WR><<<(unsigned)ctas, C::kThreads, C::kSmem, s>>>(P);
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)ctas);
+  cfg.blockDim = dim3(C::kThreads);
+  cfg.dynamicSmemBytes = C::kSmem;
+  cfg.stream = s;
+  cudaLaunchAttribute overlap;
+  overlap.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  overlap.val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = &overlap;
+  cfg.numAttrs = P.two_launches ? 1 : 0;
+  const cudaError_t e = cudaLaunchKernelEx(&cfg, k_attn_rows<D, WR>, P);
   note_launch();
-  return cudaGetLastError() == cudaSuccess ? GS_OK : GS_ERR_CUDA;
+  return e == cudaSuccess ? GS_OK : GS_ERR_CUDA;
 }
 
 }  // namespace
