@@ -394,20 +394,25 @@ def _empty(shape, dtype: torch.dtype, device, stream: Optional[torch.cuda.Stream
         return torch.empty(shape, dtype=dtype, device=device)
 
 
+def _require_like(t: torch.Tensor, shape, name: str) -> int:
+    """The address of a contiguous bf16 CUDA tensor of that shape."""
+    if t.dtype != torch.bfloat16 or not t.is_cuda or not t.is_contiguous():
+        _require_cuda(t, torch.bfloat16, name)
+    if t.shape != shape:
+        raise ValueError(f"{name} must be {tuple(shape)}, got {tuple(t.shape)}")
+    return t.data_ptr()
+
+
 def _norm(x, weight, residual, eps, h, y, y8, scales, group, stream):
-    _require_cuda(x, torch.bfloat16, "x")
-    _require_cuda(weight, torch.bfloat16, "weight")
-    T, n = x.shape
-    if weight.shape != (n,):
-        raise ValueError("x must be [T, n] and weight [n]")
-    for t, name in ((residual, "residual"), (h, "h"), (y, "y")):
-        if t is not None:
-            _require_cuda(t, torch.bfloat16, name)
-            if t.shape != (T, n):
-                raise ValueError(f"{name} must have x's shape")
-    ptr = [None if t is None else t.data_ptr() for t in (residual, h, y, y8, scales)]
-    _check(lib.gs_add_rms_norm(x.data_ptr(), ptr[0], weight.data_ptr(), T, n, eps, ptr[1], ptr[2], ptr[3], ptr[4], group,
-                               _stream_ptr(stream)), "gs_add_rms_norm")
+    if x.dim() != 2:
+        raise ValueError("x must be [T, n]")
+    shape = x.shape
+    T, n = shape
+    _check(lib.gs_add_rms_norm(
+        _require_like(x, shape, "x"), None if residual is None else _require_like(residual, shape, "residual"),
+        _require_like(weight, (n,), "weight"), T, n, eps, None if h is None else _require_like(h, shape, "h"),
+        None if y is None else _require_like(y, shape, "y"), None if y8 is None else y8.data_ptr(),
+        None if scales is None else scales.data_ptr(), group, _stream_ptr(stream)), "gs_add_rms_norm")
 
 
 def add_rms_norm(x: torch.Tensor, weight: torch.Tensor, residual: Optional[torch.Tensor] = None, eps: float = 1e-5,
@@ -417,9 +422,9 @@ def add_rms_norm(x: torch.Tensor, weight: torch.Tensor, residual: Optional[torch
     Without a residual, h is None unless it was given (a copy of x then).  h may be the residual's or x's own
     tensor, y x's own."""
     if y is None:
-        y = _empty(x.shape, torch.bfloat16, x.device, stream)
+        y = torch.empty_like(x) if stream is None else _empty(x.shape, x.dtype, x.device, stream)
     if h is None and residual is not None:
-        h = _empty(x.shape, torch.bfloat16, x.device, stream)
+        h = torch.empty_like(x) if stream is None else _empty(x.shape, x.dtype, x.device, stream)
     _norm(x, weight, residual, eps, h, y, None, None, 0, stream)
     return y, h
 
@@ -428,6 +433,8 @@ def add_rms_norm_fp8(x: torch.Tensor, weight: torch.Tensor, residual: Optional[t
                      group: int = 0, h: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None):
     """add_rms_norm with y in 8 bits: (y8 e4m3 [T, n], scales float32 [T, groups], h), y = y8 * scales of the
     element's group of columns (0: one group a row; 128)."""
+    if x.dim() != 2:
+        raise ValueError("x must be [T, n]")
     y8 = _empty(x.shape, torch.float8_e4m3fn, x.device, stream)
     scales = _empty((x.shape[0], -(-x.shape[1] // group) if group > 0 else 1), torch.float32, x.device, stream)
     if h is None and residual is not None:
@@ -452,6 +459,8 @@ class Adapters:
         self.A, self.B, self.scale = A, B, scale
         self.n, self.rank, self.inp = A.shape
         self.out = B.shape[1]
+        self._c = _AdapterLayer(None, None, None, A.data_ptr(), B.data_ptr(), scale.data_ptr(), self.inp, self.out, self.n,
+                                self.rank)
 
 
 def adapters_batched_into(xs: Sequence[torch.Tensor], bases: Sequence[torch.Tensor], ads: Sequence[Adapters],
@@ -470,17 +479,11 @@ def adapters_batched_into(xs: Sequence[torch.Tensor], bases: Sequence[torch.Tens
     if offsets.dim() != 1 or ids.dim() != 1 or offsets.shape[0] != ids.shape[0] + 1:
         raise ValueError("offsets must be [n + 1] and ids [n]")
     T = xs[0].shape[0]
-    arr = (_AdapterLayer * n)()
+    arr = (_AdapterLayer * n)(*[ad._c for ad in ads])
     for l, x, base, ad, out in zip(arr, xs, bases, ads, outs):
-        _require_cuda(x, torch.bfloat16, "x")
-        _require_cuda(base, torch.bfloat16, "base")
-        if out is not base:
-            _require_cuda(out, torch.bfloat16, "out")
-        if x.shape != (T, ad.inp) or base.shape != (T, ad.out) or out.shape != (T, ad.out):
-            raise ValueError("every x must be [T, in_i], base and out [T, out_i] with one T")
-        l.x, l.base, l.out_ptr = x.data_ptr(), base.data_ptr(), out.data_ptr()
-        l.A, l.B, l.scale = ad.A.data_ptr(), ad.B.data_ptr(), ad.scale.data_ptr()
-        l.inp, l.out, l.n_adapters, l.rank = ad.inp, ad.out, ad.n, ad.rank
+        shape = (T, ad.out)
+        l.x, l.base = _require_like(x, (T, ad.inp), "x"), _require_like(base, shape, "base")
+        l.out_ptr = l.base if out is base else _require_like(out, shape, "out")
     _check(lib.gs_adapters_batched(n, arr, offsets.data_ptr(), ids.data_ptr(), ids.shape[0], T, _stream_ptr(stream)),
            "gs_adapters_batched")
 
@@ -589,13 +592,10 @@ def cache_append(cache: PagedCache, batch: Batch, q: torch.Tensor, k: torch.Tens
         raise ValueError("cos and sin must be [positions, head_dim / 2]")
     if q_out is None:
         q_out = _empty(q.shape, torch.bfloat16, q.device, stream)
-    else:
-        _require_cuda(q_out, torch.bfloat16, "q_out")
-        if q_out.shape != q.shape:
-            raise ValueError("q_out must have q's shape")
+    to = _require_like(q_out, q.shape, "q_out")
     batch._c.tokens = T
     _check(lib.gs_cache_append(cache._ref, batch._ref, q.data_ptr(), qs, q.shape[1], k.data_ptr(), ks, v.data_ptr(), vs,
-                               cos.data_ptr(), sin.data_ptr(), cos.shape[0], q_out.data_ptr(), _stream_ptr(stream)),
+                               cos.data_ptr(), sin.data_ptr(), cos.shape[0], to, _stream_ptr(stream)),
            "gs_cache_append")
     return q_out
 
@@ -608,15 +608,12 @@ def paged_attention(q: torch.Tensor, cache: PagedCache, batch: Batch, scale: Opt
     qs = _heads(q, D, "q")
     if out is None:
         out = _empty(q.shape, torch.bfloat16, q.device, stream)
-    else:
-        _require_cuda(out, torch.bfloat16, "out")
-        if out.shape != q.shape:
-            raise ValueError("out must have q's shape")
+    to = _require_like(out, q.shape, "out")
     batch._c.tokens = q.shape[0]
     sp = _stream_ptr(stream)
     ws = _attention_workspace(batch._workspace_bytes(cache, q.shape[1]), q.device, stream, sp)
     _check(lib.gs_paged_attention(cache._ref, batch._ref, q.data_ptr(), qs, q.shape[1],
-                                  D ** -0.5 if scale is None else scale, out.data_ptr(), ws.data_ptr(), ws.numel(), sp),
+                                  D ** -0.5 if scale is None else scale, to, ws.data_ptr(), ws.numel(), sp),
            "gs_paged_attention")
     return out
 
