@@ -509,8 +509,10 @@ gs_status gs_cache_append(const gs_paged_cache* cache, const gs_seq_batch* batch
  * workspace_dev  gs_paged_attention_workspace bytes, 16-byte aligned, zero before its
  *         first use; calls leave the part zero that has to be, so it serves one call
  *         after another on one stream without being cleared.
- * max_new chooses the kernels; a sequence with more new tokens than it says is served
- * all the same, or (if max_new is below what needs the chunk kernel) gets zeros.
+ * max_new chooses the kernels; a sequence with more new tokens than it says may get
+ * zeros.
+ * The first call of a process makes the library's error flag, if gs_pack has not: not
+ * inside a graph capture.
  * After GS_ERR_DEVICE_TIMEOUT the workspace has to be zeroed again.
  * Errors: INVALID_ARG, UNSUPPORTED (page_size, head_dim, more than 64 query heads a key
  * head, tokens * q_heads / kv_heads of 10^9 and more, or more than 2 * 10^9 tiles of

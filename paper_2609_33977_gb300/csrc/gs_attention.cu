@@ -98,10 +98,9 @@ gs_status launch_paged_attention(const gs_paged_cache& c, const gs_seq_batch& b,
   P.cnt = cnt + 2 * kMaxCtas;
   P.parts = reinterpret_cast<float*>(parts + (k.chunk ? part_bytes(attn_chunk_rows(), c.head_dim) : 0));
   P.min_rows = 1;
-  P.max_rows = attn_rows_most();
+  P.max_rows = attn_rows_held((int)std::min((int64_t)b.max_new * P.group, (int64_t)attn_rows_most()));
   P.zero_rest = !k.chunk;
-  const int most = (int)std::min((int64_t)b.max_new * P.group, (int64_t)attn_rows_most());
-  return launch_attn_rows(P, c.head_dim, most, attention_ctas(), s);
+  return launch_attn_rows(P, c.head_dim, attention_ctas(), s);
 }
 
 }  // namespace gs

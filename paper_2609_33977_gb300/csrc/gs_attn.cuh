@@ -40,11 +40,12 @@ struct AttnParams {
   int32_t negate;               // scale < 0: the queries' signs are flipped
 };
 
-// attn_rows.cu: sequences of at most attn_rows_most() rows; rows: a bound of theirs
+// attn_rows.cu: sequences of at most P.max_rows rows, one of the numbers that the kernel's forms hold
 int attn_rows_most();
+int attn_rows_held(int rows);       // the least of these numbers that is at least `rows`
 int attn_rows_box(int page_size);   // rows of a TMA box
 int attn_rows_tile();               // keys of a unit
-gs_status launch_attn_rows(const AttnParams& P, int head_dim, int rows, int ctas, cudaStream_t s);
+gs_status launch_attn_rows(const AttnParams& P, int head_dim, int ctas, cudaStream_t s);
 
 // attn_chunk.cu: any number of rows
 int attn_chunk_box(int page_size);
@@ -361,8 +362,8 @@ struct Walker {
     if (pos != first || stop != last) {
       // the boundaries inside the item that were not moved to its ends
       const int c_lo = sh.first_cut(first + Traits::kSnap + Traits::kOver + 1), c_hi = sh.first_cut(last - Traits::kSnap) - 1;
-      g.first_cta = c_lo - 1;
-      g.parts = c_hi - c_lo + 2;
+      g.first_cta = max(0, min(c_lo - 1, cta));
+      g.parts = max(1, min(c_hi - c_lo + 2, sh.ctas - g.first_cta));   // whatever the offsets, inside the workspace
       g.part = cta - g.first_cta;
     }
     pos = stop;

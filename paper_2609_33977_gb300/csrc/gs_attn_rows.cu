@@ -554,10 +554,13 @@ int attn_rows_box(int page_size) { return page_size < kTile ? page_size : kTile;
 
 int attn_rows_tile() { return kTile; }
 
-gs_status launch_attn_rows(const AttnParams& P, int head_dim, int rows, int ctas, cudaStream_t s) {
+int attn_rows_held(int rows) { return rows <= 16 ? 16 : rows <= 32 ? 32 : 64; }
+
+gs_status launch_attn_rows(const AttnParams& P, int head_dim, int ctas, cudaStream_t s) {
+  const int wr = P.max_rows / 16;
   if (head_dim == 128)
-    return rows <= 16 ? rows_launch<128, 1>(P, ctas, s) : rows <= 32 ? rows_launch<128, 2>(P, ctas, s) : rows_launch<128, 4>(P, ctas, s);
-  return rows <= 16 ? rows_launch<64, 1>(P, ctas, s) : rows <= 32 ? rows_launch<64, 2>(P, ctas, s) : rows_launch<64, 4>(P, ctas, s);
+    return wr == 1 ? rows_launch<128, 1>(P, ctas, s) : wr == 2 ? rows_launch<128, 2>(P, ctas, s) : rows_launch<128, 4>(P, ctas, s);
+  return wr == 1 ? rows_launch<64, 1>(P, ctas, s) : wr == 2 ? rows_launch<64, 2>(P, ctas, s) : rows_launch<64, 4>(P, ctas, s);
 }
 
 }  // namespace gs

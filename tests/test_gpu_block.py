@@ -328,6 +328,28 @@ def test_many_sequences(gs):
     _attend(gs, new, [n + (13 * i) % 90 for i, n in enumerate(new)], 4, 1, 64, 32)
 
 
+def test_many_chunks(gs):
+    """More sequences than threads of a block, each of more rows than the few-row kernel's."""
+    new = [17 + i % 9 for i in range(600)]
+    _attend(gs, new, [n + (29 * i) % 170 for i, n in enumerate(new)], 4, 1, 64, 32)
+
+
+@pytest.mark.parametrize("told", [1, 4, 5, 8, 16])
+def test_more_new_tokens_than_told(gs, told):
+    """A sequence of more new tokens than max_new is right or zero, and its neighbours are right."""
+    new, kv = [1, 20, 3, 9, 1], [30, 50, 70, 9, 200]
+    cache, table = ref.make_cache(gs, kv, 1, 128, 16, 130)
+    q = _rand((sum(new), 4, 128), 131)
+    out = gs.paged_attention(q, cache, gs.Batch(ref.offsets(new), ref.i32(kv), table, told))
+    want, bound = ref.attention(q, cache.k_pages, cache.v_pages, table, new, kv, 128 ** -0.5)
+    t = 0
+    for n in new:
+        rows = slice(t, t + n)
+        if n <= told or (out[rows] != 0).any():
+            ref.assert_close(out[rows], want[rows], bound[rows], f"{n} tokens, told {told}")
+        t += n
+
+
 def test_streams_and_graphs(gs):
     """A captured step follows new lengths, pages and tokens in the tensors it was captured with."""
     kv, hq, hkv, d, page = [100, 33, 260], 8, 2, 128, 16
