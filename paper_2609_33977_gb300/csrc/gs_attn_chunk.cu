@@ -634,7 +634,8 @@ __global__ void __launch_bounds__(kAcThreads, 1) k_attn_chunk(const __grid_const
         if (!wait_warp(&o_bar[h][(n - 1u) & 1u], ((n - 1u) >> 1) & 1u)) break;
         tc_fence_after();
       }
-      const int64_t mine = row.on ? ((int64_t)(g.s.tok0 + row.tok) * P.q_heads + g.h * P.group + row.hd) * D : -1;
+      // the row in the output (its elements fit memory, so rows fit 32 bits)
+      const uint32_t mine = row.on ? (uint32_t)(g.s.tok0 + row.tok) * (uint32_t)P.q_heads + (uint32_t)(g.h * P.group + row.hd) : ~0u;
       const int ri = h * kHalf + 32 * quarter + lane;
       float* slot = g.parts > 1 ? part_slot(P, g.first_cta, g.part, kPartRows, D) : nullptr;
       float mm = 0.f;
@@ -702,9 +703,9 @@ __global__ void __launch_bounds__(kAcThreads, 1) k_attn_chunk(const __grid_const
             }
 #pragma unroll
           for (int r = 0; r < 4; ++r) {
-            const int64_t dst = __shfl_sync(0xffffffffu, mine, (lane & ~3) + r);
-            if (dst >= 0)
-              *reinterpret_cast<uint4*>(P.out + dst + c0 + 8 * (lane & 3)) = make_uint4(w[r][0], w[r][1], w[r][2], w[r][3]);
+            const uint32_t dst = __shfl_sync(0xffffffffu, mine, (lane & ~3) + r);
+            if (dst != ~0u)
+              *reinterpret_cast<uint4*>(P.out + (int64_t)dst * D + c0 + 8 * (lane & 3)) = make_uint4(w[r][0], w[r][1], w[r][2], w[r][3]);
           }
         }
         if (phase == 0 && bad_s[at]) {
@@ -723,7 +724,7 @@ __global__ void __launch_bounds__(kAcThreads, 1) k_attn_chunk(const __grid_const
               if (slot) {
                 slot[(size_t)((e & ~3) * kPartRows + 4 * ri + (e & 3))] += x;
               } else {
-                volatile uint16_t* to16 = P.out + mine + e;
+                volatile uint16_t* to16 = P.out + (int64_t)mine * D + e;
                 *to16 = (uint16_t)pack_bf16(bf16_lo(*to16) + x, 0.f);
               }
             }
