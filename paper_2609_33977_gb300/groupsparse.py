@@ -554,8 +554,8 @@ class Batch:
         self._ref = ctypes.addressof(self._c)
         self._need = {}
 
-    def _workspace_bytes(self, cache: PagedCache, q_heads: int) -> int:
-        key = (q_heads, cache.kv_heads, cache.head_dim, cache.page_size, self._c.tokens)
+    def _workspace_bytes(self, cache: PagedCache, q_heads: int, tokens: int) -> int:
+        key = (q_heads, cache.kv_heads, cache.head_dim, tokens)
         need = self._need.get(key)
         if need is None:
             c = ctypes.c_size_t()
@@ -565,15 +565,20 @@ class Batch:
         return need
 
 
-def _heads(t: torch.Tensor, D: int, name: str) -> int:
-    """The distance of two tokens of [T, heads, D], whose heads lie side by side (a slice of a joint projection may)."""
+def _heads(t: torch.Tensor, D: int, name: str):
+    """(tokens, heads, distance of two tokens) of [T, heads, D], whose heads lie side by side (a slice of a joint
+    projection may be one)."""
     if not t.is_cuda:
         raise ValueError(f"{name} must be a CUDA tensor")
     if t.dtype != torch.bfloat16:
         raise ValueError(f"{name} must be torch.bfloat16, got {t.dtype}")
-    if t.dim() != 3 or t.shape[2] != D or t.stride(2) != 1 or (t.stride(1) != D and t.shape[1] != 1):
+    if t.dim() != 3:
+        raise ValueError(f"{name} must be [T, heads, {D}]")
+    T, heads, d = t.shape
+    token, head, one = t.stride()
+    if d != D or one != 1 or (head != D and heads != 1):
         raise ValueError(f"{name} must be [T, heads, {D}] with dense heads")
-    return t.stride(0) if t.shape[0] != 1 else t.shape[1] * D
+    return T, heads, token if T != 1 else heads * D
 
 
 def cache_append(cache: PagedCache, batch: Batch, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cos: torch.Tensor,
@@ -581,21 +586,25 @@ def cache_append(cache: PagedCache, batch: Batch, q: torch.Tensor, k: torch.Tens
                  stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
     """Turns q [T, q_heads, D] and k [T, kv_heads, D] by their positions' angles (cos, sin: float32 [positions, D / 2];
     channels i and i + D / 2 are a pair), writes k and v into the cache's pages and returns the turned q (q_out)."""
-    D = cache.head_dim
-    qs, ks, vs = _heads(q, D, "q"), _heads(k, D, "k"), _heads(v, D, "v")
-    T = q.shape[0]
-    if k.shape[0] != T or v.shape[0] != T or k.shape[1] != cache.kv_heads or v.shape[1] != cache.kv_heads:
+    D, kv = cache.head_dim, cache.kv_heads
+    T, heads, qs = _heads(q, D, "q")
+    Tk, hk, ks = _heads(k, D, "k")
+    Tv, hv, vs = _heads(v, D, "v")
+    if Tk != T or Tv != T or hk != kv or hv != kv:
         raise ValueError("k and v must be [T, kv_heads, D] with q's T")
-    _require_cuda(cos, torch.float32, "cos")
-    _require_cuda(sin, torch.float32, "sin")
-    if cos.dim() != 2 or cos.shape[1] != D // 2 or sin.shape != cos.shape:
+    if cos.dtype != torch.float32 or not cos.is_cuda or not cos.is_contiguous():
+        _require_cuda(cos, torch.float32, "cos")
+    if sin.dtype != torch.float32 or not sin.is_cuda or not sin.is_contiguous():
+        _require_cuda(sin, torch.float32, "sin")
+    shape = cos.shape
+    if len(shape) != 2 or shape[1] * 2 != D or sin.shape != shape:
         raise ValueError("cos and sin must be [positions, head_dim / 2]")
     if q_out is None:
         q_out = _empty(q.shape, torch.bfloat16, q.device, stream)
     to = _require_like(q_out, q.shape, "q_out")
     batch._c.tokens = T
-    _check(lib.gs_cache_append(cache._ref, batch._ref, q.data_ptr(), qs, q.shape[1], k.data_ptr(), ks, v.data_ptr(), vs,
-                               cos.data_ptr(), sin.data_ptr(), cos.shape[0], to, _stream_ptr(stream)),
+    _check(lib.gs_cache_append(cache._ref, batch._ref, q.data_ptr(), qs, heads, k.data_ptr(), ks, v.data_ptr(), vs,
+                               cos.data_ptr(), sin.data_ptr(), shape[0], to, _stream_ptr(stream)),
            "gs_cache_append")
     return q_out
 
@@ -605,16 +614,15 @@ def paged_attention(q: torch.Tensor, cache: PagedCache, batch: Batch, scale: Opt
     """Causal attention of a step's queries q [T, q_heads, D] over the cache (the step's own keys are in it already:
     cache_append), bf16 [T, q_heads, D].  scale: 1 / sqrt(D) if not given.  A token without visible keys gets zeros."""
     D = cache.head_dim
-    qs = _heads(q, D, "q")
+    T, heads, qs = _heads(q, D, "q")
     if out is None:
         out = _empty(q.shape, torch.bfloat16, q.device, stream)
     to = _require_like(out, q.shape, "out")
-    batch._c.tokens = q.shape[0]
+    batch._c.tokens = T
     sp = _stream_ptr(stream)
-    ws = _attention_workspace(batch._workspace_bytes(cache, q.shape[1]), q.device, stream, sp)
-    _check(lib.gs_paged_attention(cache._ref, batch._ref, q.data_ptr(), qs, q.shape[1],
-                                  D ** -0.5 if scale is None else scale, to, ws.data_ptr(), ws.numel(), sp),
-           "gs_paged_attention")
+    ws = _attention_workspace(batch._workspace_bytes(cache, heads, T), q.device, stream, sp)
+    _check(lib.gs_paged_attention(cache._ref, batch._ref, q.data_ptr(), qs, heads, D ** -0.5 if scale is None else scale, to,
+                                  ws.data_ptr(), ws.numel(), sp), "gs_paged_attention")
     return out
 
 
