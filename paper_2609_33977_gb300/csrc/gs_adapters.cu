@@ -63,46 +63,51 @@ __device__ __forceinline__ void expand(const AdLayer& L, const uint4* v, const u
   const int g = lane >> 2, q = lane & 3;
   const int steps = rank / (4 * E);
   const bool vec = (L.out_n & 7) == 0;
-  for (int blk = b0 + warp; blk < b1; blk += kAdWarps) {
-    const int col = 32 * blk + 8 * q;
-    uint4 base[MT][2];
+  // With one row of tiles two blocks are under way together: a load may not pass the stores before it (the base may be
+  // the output), and at few tokens the loads' wait is all there is.
+  constexpr int kB = MT == 1 ? 2 : 1;
+  constexpr int kMmas = E == 8 ? 2 : 1;
+  for (int blk = b0 + warp; blk < b1; blk += kB * kAdWarps) {
+    uint4 base[kB][MT][2];
+    float acc[kB][MT][4][4];
 #pragma unroll
-    for (int m = 0; m < MT; ++m)
+    for (int b = 0; b < kB; ++b) {
+      const int col = 32 * (blk + b * kAdWarps) + 8 * q;
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const int r = 16 * m + 8 * h + g;
-        if (vec)   // rows and columns past the last: values that nobody uses
-          base[m][h] = *reinterpret_cast<const uint4*>(L.base + (t0 + min(r, nt - 1)) * L.out_n + min(col, L.out_n - 8));
+      for (int m = 0; m < MT; ++m) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+          if (vec)   // rows and columns past the last: values that nobody uses
+            base[b][m][h] = *reinterpret_cast<const uint4*>(L.base + (t0 + min(16 * m + 8 * h + g, nt - 1)) * L.out_n + min(col, L.out_n - 8));
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) acc[b][m][j][e] = 0.f;
       }
-    float acc[MT][4][4];
-#pragma unroll
-    for (int m = 0; m < MT; ++m)
-#pragma unroll
-      for (int j = 0; j < 4; ++j)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) acc[m][j][e] = 0.f;
+    }
     for (int s = 0; s < steps; ++s) {
-      uint32_t w[4][4];
+      uint32_t w[kB][4][4];
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const int o = 32 * blk + 8 * (g >> 1) + 2 * j + (g & 1);   // this lane's row of B in MMA j
-        const uint16_t* src = B + (int64_t)min(o, L.out_n - 1) * rank + s * 4 * E + q * E;
-        w[j][0] = w[j][1] = w[j][2] = w[j][3] = 0u;
-        if constexpr (E == 8) {
-          const uint4 c = __ldg(reinterpret_cast<const uint4*>(src));
-          w[j][0] = c.x;
-          w[j][1] = c.y;
-          w[j][2] = c.z;
-          w[j][3] = c.w;
-        } else if constexpr (E == 4) {
-          const uint2 c = __ldg(reinterpret_cast<const uint2*>(src));
-          w[j][0] = c.x;
-          w[j][1] = c.y;
-        } else {
-          w[j][0] = __ldg(reinterpret_cast<const uint32_t*>(src));
+      for (int b = 0; b < kB; ++b)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const int o = 32 * (blk + b * kAdWarps) + 8 * (g >> 1) + 2 * j + (g & 1);   // this lane's row of B in MMA j
+          const uint16_t* src = B + (int64_t)min(o, L.out_n - 1) * rank + s * 4 * E + q * E;
+          w[b][j][0] = w[b][j][1] = w[b][j][2] = w[b][j][3] = 0u;
+          if constexpr (E == 8) {
+            const uint4 c = __ldg(reinterpret_cast<const uint4*>(src));
+            w[b][j][0] = c.x;
+            w[b][j][1] = c.y;
+            w[b][j][2] = c.z;
+            w[b][j][3] = c.w;
+          } else if constexpr (E == 4) {
+            const uint2 c = __ldg(reinterpret_cast<const uint2*>(src));
+            w[b][j][0] = c.x;
+            w[b][j][1] = c.y;
+          } else {
+            w[b][j][0] = __ldg(reinterpret_cast<const uint32_t*>(src));
+          }
         }
-      }
-      constexpr int kMmas = E == 8 ? 2 : 1;
 #pragma unroll
       for (int m = 0; m < MT; ++m)
 #pragma unroll
@@ -111,33 +116,40 @@ __device__ __forceinline__ void expand(const AdLayer& L, const uint4* v, const u
           for (int part = 0; part < 2; ++part) {
             const uint4 f = v[(((m * steps + s) * kMmas + p) * 2 + part) * 32 + lane];
 #pragma unroll
-            for (int j = 0; j < 4; ++j) mma16816(acc[m][j], f.x, f.y, f.z, f.w, w[j][2 * p], w[j][2 * p + 1]);
+            for (int b = 0; b < kB; ++b)
+#pragma unroll
+              for (int j = 0; j < 4; ++j) mma16816(acc[b][m][j], f.x, f.y, f.z, f.w, w[b][j][2 * p], w[b][j][2 * p + 1]);
           }
     }
 #pragma unroll
-    for (int m = 0; m < MT; ++m)
+    for (int b = 0; b < kB; ++b) {
+      const int col = 32 * (blk + b * kAdWarps) + 8 * q;
+      if (blk + b * kAdWarps >= b1) break;   // not this CTA's
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const int r = 16 * m + 8 * h + g;
-        if (r >= nt || col >= L.out_n) continue;
-        uint16_t* dst = L.out + (t0 + r) * L.out_n + col;
-        if (vec) {
-          const uint32_t bw[4] = {base[m][h].x, base[m][h].y, base[m][h].z, base[m][h].w};
-          uint32_t o[4];
+      for (int m = 0; m < MT; ++m)
 #pragma unroll
-          for (int j = 0; j < 4; ++j)
-            o[j] = pack_bf16(bf16_lo(bw[j]) + acc[m][j][2 * h], bf16_hi(bw[j]) + acc[m][j][2 * h + 1]);
-          *reinterpret_cast<uint4*>(dst) = make_uint4(o[0], o[1], o[2], o[3]);
-        } else {
-          const uint16_t* src = L.base + (t0 + r) * L.out_n + col;
+        for (int h = 0; h < 2; ++h) {
+          const int r = 16 * m + 8 * h + g;
+          if (r >= nt || col >= L.out_n) continue;
+          uint16_t* dst = L.out + (t0 + r) * L.out_n + col;
+          if (vec) {
+            const uint32_t bw[4] = {base[b][m][h].x, base[b][m][h].y, base[b][m][h].z, base[b][m][h].w};
+            uint32_t o[4];
 #pragma unroll
-          for (int j = 0; j < 4; ++j)
+            for (int j = 0; j < 4; ++j)
+              o[j] = pack_bf16(bf16_lo(bw[j]) + acc[b][m][j][2 * h], bf16_hi(bw[j]) + acc[b][m][j][2 * h + 1]);
+            *reinterpret_cast<uint4*>(dst) = make_uint4(o[0], o[1], o[2], o[3]);
+          } else {
+            const uint16_t* src = L.base + (t0 + r) * L.out_n + col;
 #pragma unroll
-            for (int e = 0; e < 2; ++e)
-              if (col + 2 * j + e < L.out_n)
-                dst[2 * j + e] = (uint16_t)pack_bf16(bf16_lo(src[2 * j + e]) + acc[m][j][2 * h + e], 0.f);
+            for (int j = 0; j < 4; ++j)
+#pragma unroll
+              for (int e = 0; e < 2; ++e)
+                if (col + 2 * j + e < L.out_n)
+                  dst[2 * j + e] = (uint16_t)pack_bf16(bf16_lo(src[2 * j + e]) + acc[b][m][j][2 * h + e], 0.f);
+          }
         }
-      }
+    }
   }
 }
 
