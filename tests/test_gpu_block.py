@@ -55,6 +55,22 @@ def test_norm_8_bits(gs, T, n, group):
     ref.assert_close(y8.float(), yr / each, (yr / each).abs() * (1.02 * 2.0 ** -4 + rel) + 1.02 * 2.0 ** -10, "y8")
 
 
+@pytest.mark.parametrize("T,n", [(160, 4096), (160, 4104), (153, 8200), (3, 32768), (2, 32776), (200, 1000)])
+def test_norm_many_rows_and_long_ones(gs, T, n):
+    x, r, w = _rand((T, n), 41), _rand((T, n), 42, 2.0), _rand((n,), 43)
+    y, h = gs.add_rms_norm(x, w, r, 1e-5)
+    hr, yr = ref.norm(x, r, w, 1e-5)
+    ref.assert_close(y, yr, yr.abs() * (ref.BF + n * 2.0 ** -24) + 1e-30, "y")
+    ref.assert_close(h, hr, hr.abs() * ref.BF, "h")
+    y8, sc, h = gs.add_rms_norm_fp8(x, w, r, 1e-5, 128)
+    want = torch.stack([yr[:, i: i + 128].abs().amax(1) for i in range(0, n, 128)], 1) / 448
+    rel = n * 2.0 ** -24 + 2.0 ** -20
+    ref.assert_close(sc, want, want * rel, "scales")
+    at = yr / want.repeat_interleave(128, 1)[:, :n]
+    ref.assert_close(y8.float(), at, at.abs() * (1.02 * 2.0 ** -4 + rel) + 1.02 * 2.0 ** -10, "y8")
+    ref.assert_close(h, hr, hr.abs() * ref.BF, "h")
+
+
 def test_norm_in_place_and_nonfinite(gs):
     for n in (512, 515):
         x, r, w = _rand((3, n), 7), _rand((3, n), 8), _rand((n,), 9)
