@@ -5,17 +5,21 @@
 //
 // Bound by HBM at long chunks (every element of q, k, v read and written once),
 // by latency at few tokens: the look-up of a token's sequence, its length, its page
-// are loads that wait for one another.  A block takes one token (or a part of its
-// heads), a thread 8 channel pairs of a head: two 16-byte loads and stores.  Up to 32
-// sequences are looked up by every warp for itself, one load each and a ballot;
-// more by the whole block.  (Two or four tokens a block: 7 and 40 % slower at 3000
-// tokens, since a thread's loads then queue behind each other's look-ups.)
+// are loads that wait for one another.  A block takes a part of one token's heads, a
+// thread 8 channel pairs of a head: two 16-byte loads and stores.  (Blocks of 512
+// threads 2.6 us, of 128 2.4, for 16 tokens of 32 + 2 x 32 heads.  Two or four tokens a
+// block: 7 and 40 % slower at 3000 tokens, since a thread's loads then queue behind each
+// other's look-ups.)  Up to 32 sequences are looked up by every warp for itself, one load
+// each and a ballot; more by the whole block (us at these 16 tokens and at 3000 of
+// 28 + 2 x 4 heads: 2.5 and 11.3 by a warp, 2.7 and 11.5 by the block).
+//
+// 3000 tokens of 28 + 2 x 4 heads of 128: 11 us, 5.1 TB/s.
 #include "gs_block.cuh"
 
 namespace gs {
 namespace {
 
-constexpr int kAppThreads = 512;   // at most
+constexpr int kAppThreads = 128;   // at most
 
 struct AppendParams {
   const uint16_t* q;
