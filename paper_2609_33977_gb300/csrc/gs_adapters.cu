@@ -6,9 +6,9 @@
 // of one request belongs to a cluster of CL CTAs: CTA c contracts its part of the
 // inputs, the partial A x [M][r] are summed over the cluster through distributed
 // shared memory in a fixed order, and CTA c then forms its part of the outputs.
-// CL is 8 where tiles are few, less where they fill the SMs without.  M is 16 where requests are short (a decode step has one token
-// each) and 64 (32 above rank 64) where they are long, so that A and B come from
-// L2 once per M tokens.
+// CL is the largest of 8, 4, 2 with which all tiles are resident (ad_cluster).  M is 16
+// where requests are short (a decode step has one token each) and 32 where they are
+// long, so that A and B come from L2 half as often (launch_adapters).
 //
 // Products are m16n8k16 with float32 sums.  A contraction may take its index in any
 // order, so a lane takes 8 consecutive elements of its row as one 16-byte load and
@@ -63,9 +63,10 @@ __device__ __forceinline__ void expand(const AdLayer& L, const uint4* v, const u
   const int g = lane >> 2, q = lane & 3;
   const int steps = rank / (4 * E);
   const bool vec = (L.out_n & 7) == 0;
-  // With one row of tiles two blocks are under way together: a load may not pass the stores before it (the base may be
-  // the output), and at few tokens the loads' wait is all there is.
-  constexpr int kB = MT == 1 ? 2 : 1;
+  // With one row of tiles and a short contraction two blocks are under way together: a load may not pass the stores
+  // before it (the base may be the output), and the loads' wait is all there is.  Us at one / two: q, k, v of 16 tokens,
+  // rank 16  7.7 / 7.4;  4096x11008, rank 32, 8 x 48 tokens  9.8 / 10.1;  rank 64, 16 tokens  14.0 / 15.0.
+  constexpr int kB = MT == 1 && E <= 4 ? 2 : 1;
   constexpr int kMmas = E == 8 ? 2 : 1;
   for (int blk = b0 + warp; blk < b1; blk += kB * kAdWarps) {
     uint4 base[kB][MT][2];
@@ -156,8 +157,6 @@ __device__ __forceinline__ void expand(const AdLayer& L, const uint4* v, const u
 // CTAs of an SM: two where the partial sums (4 NT MT registers) leave room for it
 constexpr int ad_per_sm(int NT, int MT) { return NT * MT <= 8 ? 2 : 1; }
 
-__device__ __forceinline__ void prefetch_l2(const void* p) { asm volatile("prefetch.global.L2 [%0];" ::"l"(p)); }
-
 // NT: n-tiles of 8 ranks held (rank <= 8 NT); MT: m-tiles of 16 tokens; CL: CTAs of a cluster
 template <int NT, int MT, int CL>
 __global__ void __launch_bounds__(kAdThreads, ad_per_sm(NT, MT)) __cluster_dims__(CL, 1, 1) k_adapters(const __grid_constant__ AdParams P) {
@@ -205,16 +204,6 @@ __global__ void __launch_bounds__(kAdThreads, ad_per_sm(NT, MT)) __cluster_dims_
   const int rank = L.rank, nrt = rank / 8;
   const uint16_t* A = L.A + (int64_t)id * rank * L.in;
   const uint16_t* B = L.B + (int64_t)id * rank * L.out_n;
-
-  // What the second product reads comes to L2 under the first: this CTA's rows of B, and its columns of the base
-  {
-    const int c0 = 32 * b0, n_col = min(32 * b1, L.out_n) - c0;
-    const char* bp = reinterpret_cast<const char*>(B + (int64_t)c0 * rank);
-    for (int i = threadIdx.x; i * 64 < n_col * rank; i += kAdThreads) prefetch_l2(bp + (int64_t)i * 128);
-    const int lines = (n_col + 63) / 64;
-    for (int i = threadIdx.x; i < lines * nt; i += kAdThreads)
-      prefetch_l2(L.base + (t0 + i / lines) * L.out_n + c0 + min(64 * (i % lines), n_col - 1));
-  }
 
   // ---- A x over this CTA's inputs: blocks of 32, taken by the warps in turn
   float acc[MT][NT][4];
@@ -338,7 +327,8 @@ gs_status ad_launch(const AdParams& P, int n, int rank, cudaStream_t s) {
 }
 
 // The largest cluster with which all tiles are resident at once: more CTAs a tile shorten
-// it as long as they do not queue.
+// it as long as they do not queue (us at 8 / 4 / 2: 51 tiles of rank 16  10.7 / 7.8 / 9.7,
+// 70 tiles of rank 32  34 / 29 / 44, 17 tiles of rank 64  15 / 23 / 41).
 template <int NT, int MT>
 gs_status ad_cluster(const AdParams& P, int n, int rank, cudaStream_t s) {
   const int64_t tiles = (P.T / (16 * MT) + P.n_seqs) * n, room = (int64_t)sm_count() * ad_per_sm(NT, MT);
@@ -370,10 +360,15 @@ gs_status launch_adapters(const gs_adapter_layer* layers, int n, const int32_t* 
     L.rank = layers[i].rank;
     rank = rank > L.rank ? rank : L.rank;
   }
-  const bool longer = T >= (int64_t)32 * n_seqs;
+  // 32 tokens a tile where the mean request has at least 64 (us at 16 / 32 a tile; 4096x11008 but where said otherwise):
+  //   rank 16 and 32    6 requests of 2048 tokens  30.4 / 21.5 and 35.4 / 27.3,  12 x 64 (4096x4096, rank 16)  9.0 / 8.5
+  //   below, rank 32    16 x 48 tokens  21.7 / 24.9,  8 x 32  9.2 / 10.1,  16 x 1 (q, k, v; rank 16)  7.4 / 8.9
+  //   rank 128          2048 tokens  99 / 74;  rank 64: 43.6 / 46.2, its sums leave no second CTA an SM: always 16
+  // (64 a tile: 34 at rank 16, 53 at 32, 79 at 64.)
+  const bool longer = T >= (int64_t)64 * n_seqs;
   if (rank <= 16) return longer ? ad_cluster<2, 2>(P, n, rank, s) : ad_cluster<2, 1>(P, n, rank, s);
   if (rank <= 32) return longer ? ad_cluster<4, 2>(P, n, rank, s) : ad_cluster<4, 1>(P, n, rank, s);
-  if (rank <= 64) return longer ? ad_cluster<8, 4>(P, n, rank, s) : ad_cluster<8, 1>(P, n, rank, s);
+  if (rank <= 64) return ad_cluster<8, 1>(P, n, rank, s);
   return longer ? ad_cluster<16, 2>(P, n, rank, s) : ad_cluster<16, 1>(P, n, rank, s);
 }
 
