@@ -658,7 +658,7 @@ __global__ void __launch_bounds__(kAcThreads, 1) k_attn_chunk(const __grid_const
           } else {
             sum = 0.f;
             const float base = mm == -INFINITY ? 0.f : mm;
-#pragma unroll 1
+#pragma unroll 2
             for (int p = 0; p < g.parts; ++p) {
               const float* sp = part_slot(P, g.first_cta, p, kPartRows, D);
               const float2 ml = __ldcg(reinterpret_cast<const float2*>(sp + D * kPartRows + 2 * ri));

@@ -11,13 +11,12 @@
 // unless it has a row to join.  Unused MMA rows cost nothing that matters.
 #include "gs_attn.cuh"
 
-#include <mutex>
-
 namespace gs {
 namespace {
 using namespace sm100;
 
 constexpr int kTile = 128;
+constexpr int kJoin = 8;   // rows of parts that a warp has under way when it joins them
 
 struct FewTraits {
   static constexpr int kLeast = 2, kSnap = 1, kOver = 1;
@@ -500,18 +499,41 @@ __global__ void __launch_bounds__(RowsCfg<D, WR>::kThreads, 1) k_attn_rows(const
             float mm = -INFINITY, ll = 0.f, a[kC];
 #pragma unroll
             for (int c = 0; c < kC; ++c) a[c] = 0.f;
-#pragma unroll 2
-            for (int p = 0; p < g.parts; ++p) {
-              const float* sp = part_slot(P, g.first_cta, p, C::kRows, D);
-              const float2 ml = __ldcg(reinterpret_cast<const float2*>(sp + (size_t)C::kRows * D + 2 * row));
-              float v[kC];
-              L::unpack(__ldcg(reinterpret_cast<const typename L::V*>(sp + (size_t)row * D) + lane), v);
-              const float mn = fmaxf(mm, ml.x), b = mn == -INFINITY ? 0.f : mn;
-              const float f0 = ex2(mm - b), f1 = ex2(ml.x - b);
-              ll = ll * f0 + ml.y * f1;
+#pragma unroll 1
+            for (int p0 = 0; p0 < g.parts; p0 += 32) {   // a lane a part's maximum and sum, then kJoin parts' rows at once
+              const int np = min(32, g.parts - p0);
+              const float* mls = part_slot(P, g.first_cta, p0 + min(lane, np - 1), C::kRows, D) + (size_t)C::kRows * D + 2 * row;
+              float2 ml = __ldcg(reinterpret_cast<const float2*>(mls));
+              if (lane >= np) ml = make_float2(-INFINITY, 0.f);
+              float mn = fmaxf(mm, ml.x);
 #pragma unroll
-              for (int c = 0; c < kC; ++c) a[c] = a[c] * f0 + v[c] * f1;
+              for (int d = 16; d > 0; d >>= 1) mn = fmaxf(mn, __shfl_xor_sync(0xffffffffu, mn, d));
+              const float b = mn == -INFINITY ? 0.f : mn, before = ex2(mm - b), fp = ex2(ml.x - b);
+              float add = ml.y * fp;
+#pragma unroll
+              for (int d = 16; d > 0; d >>= 1) add += __shfl_xor_sync(0xffffffffu, add, d);
+              ll = ll * before + add;
+#pragma unroll
+              for (int c = 0; c < kC; ++c) a[c] *= before;
               mm = mn;
+#pragma unroll 1
+              for (int p1 = 0; p1 < np; p1 += kJoin) {
+                typename L::V v[kJoin];
+#pragma unroll
+                for (int i = 0; i < kJoin; ++i)
+                  v[i] = __ldcg(reinterpret_cast<const typename L::V*>(
+                                    part_slot(P, g.first_cta, p0 + min(p1 + i, np - 1), C::kRows, D) + (size_t)row * D) + lane);
+#pragma unroll
+                for (int i = 0; i < kJoin; ++i) {
+                  const float f = __shfl_sync(0xffffffffu, fp, (p1 + i) & 31);
+                  float x[kC];
+                  L::unpack(v[i], x);
+                  if (p1 + i < np) {
+#pragma unroll
+                    for (int c = 0; c < kC; ++c) a[c] = fmaf(x[c], f, a[c]);
+                  }
+                }
+              }
             }
             const int tok = row_token(P, row), hd = row - tok * P.group;
             L::store_bf16(P.out + ((int64_t)(g.s.tok0 + tok) * P.q_heads + g.h * P.group + hd) * D + kC * lane, a,
