@@ -7,11 +7,11 @@
 namespace gs {
 namespace {
 
-// Arrival counters (two a CTA for the chunk kernel, one for the few-row kernel), then the
-// parts of split items, each kernel's its own: the two launches of a step overlap.
-constexpr int64_t kCounterBytes = 4096;
+// Arrival counters (two levels; two halves in the chunk kernel), then the parts of split
+// items, each kernel's its own: the two launches of a step overlap.
 constexpr int kMaxCtas = 256;
-static_assert(kCounterBytes >= 3 * 4 * kMaxCtas, "three counters a CTA");
+constexpr int64_t kCounterBytes = 8192;
+static_assert(kCounterBytes >= 6 * 4 * kMaxCtas, "six counters a CTA");
 
 int attention_ctas() { return std::min(sm_count(), kMaxCtas); }
 
@@ -95,7 +95,7 @@ gs_status launch_paged_attention(const gs_paged_cache& c, const gs_seq_batch& b,
   const uint32_t box = (uint32_t)attn_rows_box(c.page_size);
   if (!encode_tmap_slabs_bf16(&P.kmap, c.k_dev, D, rows, box, slabs) || !encode_tmap_slabs_bf16(&P.vmap, c.v_dev, D, rows, box, slabs))
     return GS_ERR_CUDA;
-  P.cnt = cnt + 2 * kMaxCtas;
+  P.cnt = cnt + 4 * kMaxCtas;
   P.parts = reinterpret_cast<float*>(parts + (k.chunk ? part_bytes(attn_chunk_rows(), c.head_dim) : 0));
   P.min_rows = 1;
   P.max_rows = attn_rows_held((int)std::min((int64_t)b.max_new * P.group, (int64_t)attn_rows_most()));

@@ -6,7 +6,8 @@
 // a step of any mix of lengths ends everywhere at the same time.  An item (a
 // sequence, a key head, a tile of rows) that lies across CTAs is split: each part
 // leaves (m, l, o) in the workspace, and the CTA that arrives last joins them in
-// order.  Lengths are read from device memory, by every CTA for itself.
+// order, in two levels where there are many (join_step).  Lengths are read from device
+// memory, by every CTA for itself.
 #pragma once
 
 #include "gs_block.cuh"
@@ -25,7 +26,8 @@ struct AttnParams {
   const int32_t* offsets;
   const int32_t* kv_lens;
   const int32_t* table;
-  int32_t* cnt;             // [CTAs] arrivals at the item that begins in the CTA and is split (zero between calls)
+  int32_t* cnt;             // [2][CTAs] arrivals (a half of the item each in the chunk kernel) at the group of parts, and at the
+                            // split item, that begin in the CTA; zero between calls
   float* parts;             // [CTAs][2][rows of a tile][head_dim + 2]
   int* err;
   int64_t q_stride, tokens, pages;
@@ -391,6 +393,30 @@ __device__ __forceinline__ void zero_rows(const AttnParams& P, int head_dim, int
 // began before it, and at most one of an item that goes on after it.
 __device__ __forceinline__ float* part_slot(const AttnParams& P, int first_cta, int part, int rows, int head_dim) {
   return P.parts + ((int64_t)(first_cta + part) * 2 + (part == 0 ? 1 : 0)) * rows * (head_dim + 2);
+}
+
+// The two levels in which a split item's parts are joined: groups of neighbouring parts, each
+// into its first one's place, then the groups into the output.  One CTA joining all P parts
+// reads them one behind the other; groups of sqrt(P) are joined by as many CTAs at once.
+// Up to `flat` parts are one group.  A group of two or more crosses the end of its first
+// CTA's share, and so does an item of two or more: no other has its counter there.
+struct JoinStep {
+  int first, n, stride;   // parts first, first + stride, ...
+  bool last;              // the output follows
+};
+__device__ __forceinline__ JoinStep join_step(const Segment& g, int level, int flat) {
+  int size = g.parts;
+  if (size > flat)
+#pragma unroll 1
+    for (size = 2; size * size < g.parts; ++size) {
+    }
+  JoinStep j;
+  const int groups = (g.parts + size - 1) / size;
+  j.first = level == 0 ? g.part - g.part % size : 0;
+  j.n = level == 0 ? min(size, g.parts - j.first) : groups;
+  j.stride = level == 0 ? 1 : size;
+  j.last = level == 1 || groups == 1;
+  return j;
 }
 
 }  // namespace gs

@@ -34,6 +34,7 @@ constexpr int kPartRows = 2 * kHalf;           // rows of a part in the workspac
 constexpr int kAcThreads = 512;                // warps: keys, values, S x 2, P V x 2, two value checkers; two softmax warpgroups
 constexpr int kRing = 5;                       // slots of keys, and as many of values
 constexpr int kSegs = 4;
+constexpr int kFlat = 6;                       // parts joined in one level
 constexpr int kCheckers = 2;
 constexpr int kRegsOther = 56, kRegsSoftmax = 200;
 static_assert(8 * 32 * (kRegsOther + kRegsSoftmax) <= kAcThreads * 128, "register split");
@@ -628,7 +629,7 @@ __global__ void __launch_bounds__(kAcThreads, 1) k_attn_chunk(const __grid_const
       }
       if (!ok) break;
       // ---- this segment's result, 32 channels at a time: to the output, or (phase 0) to the item's parts in the workspace,
-      // which the warpgroup that arrives last joins in their order (phase 1).
+      // which the warpgroups that arrive last join in their order (phases 1 and 2, join_step's levels).
       // Parts: [D / 4][256 rows][4], then [256][2].
       if (g.ta < end) {
         if (!wait_warp(&o_bar[h][(n - 1u) & 1u], ((n - 1u) >> 1) & 1u)) break;
@@ -637,13 +638,32 @@ __global__ void __launch_bounds__(kAcThreads, 1) k_attn_chunk(const __grid_const
       // the row in the output (its elements fit memory, so rows fit 32 bits)
       const uint32_t mine = row.on ? (uint32_t)(g.s.tok0 + row.tok) * (uint32_t)P.q_heads + (uint32_t)(g.h * P.group + row.hd) : ~0u;
       const int ri = h * kHalf + 32 * quarter + lane;
-      float* slot = g.parts > 1 ? part_slot(P, g.first_cta, g.part, kPartRows, D) : nullptr;
-      float mm = 0.f;
+      JoinStep j = {g.part, 1, 1, g.parts == 1};
+      float mm = m, sum = l;
 #pragma unroll 1
-      for (int phase = 0; phase < 2; ++phase) {
+      for (int phase = 0; phase < 3; ++phase) {
+        if (phase > 0) {
+          j = join_step(g, phase - 1, kFlat);
+          if (j.n == 1) continue;   // a group of its own: the next level
+          __threadfence();
+          if (!(ok = meet())) break;
+          if (quarter == 0 && lane == 0) {
+            int32_t* cnt = P.cnt + 2 * ((phase - 1) * (int)gridDim.x + g.first_cta + j.first) + h;
+            last_s[h] = atomicAdd(cnt, 1) == j.n - 1;
+            if (last_s[h]) *cnt = 0;
+            __threadfence();
+          }
+          if (!(ok = meet())) break;
+          if (!last_s[h]) break;
+          mm = -INFINITY;
+#pragma unroll 1
+          for (int p = 0; p < j.n; ++p)
+            mm = fmaxf(mm, __ldcg(part_slot(P, g.first_cta, j.first + p * j.stride, kPartRows, D) + D * kPartRows + 2 * ri));
+        }
+        float* slot = j.last ? nullptr : part_slot(P, g.first_cta, j.first, kPartRows, D);
 #pragma unroll 1
         for (int c0 = 0; c0 < D; c0 += 32) {
-          float o[32], sum = l;
+          float o[32];
 #pragma unroll
           for (int e = 0; e < 32; ++e) o[e] = 0.f;
           if (phase == 0) {
@@ -659,8 +679,8 @@ __global__ void __launch_bounds__(kAcThreads, 1) k_attn_chunk(const __grid_const
             sum = 0.f;
             const float base = mm == -INFINITY ? 0.f : mm;
 #pragma unroll 2
-            for (int p = 0; p < g.parts; ++p) {
-              const float* sp = part_slot(P, g.first_cta, p, kPartRows, D);
+            for (int p = 0; p < j.n; ++p) {
+              const float* sp = part_slot(P, g.first_cta, j.first + p * j.stride, kPartRows, D);
               const float2 ml = __ldcg(reinterpret_cast<const float2*>(sp + D * kPartRows + 2 * ri));
               const float fp = ml.x == mm ? 1.f : ex2((ml.x - base) * c);
               sum = fmaf(ml.y, fp, sum);
@@ -674,7 +694,7 @@ __global__ void __launch_bounds__(kAcThreads, 1) k_attn_chunk(const __grid_const
               }
             }
           }
-          if (slot && phase == 0) {
+          if (slot) {
 #pragma unroll
             for (int e = 0; e < 32; e += 4)
               *reinterpret_cast<float4*>(slot + (size_t)((c0 + e) * kPartRows + 4 * ri)) = make_float4(o[e], o[e + 1], o[e + 2], o[e + 3]);
@@ -730,22 +750,8 @@ __global__ void __launch_bounds__(kAcThreads, 1) k_attn_chunk(const __grid_const
             }
           }
         }
-        if (!slot || phase == 1) break;
-        *reinterpret_cast<float2*>(slot + (size_t)(D * kPartRows + 2 * ri)) = make_float2(m, l);
-        __threadfence();
-        if (!(ok = meet())) break;
-        if (quarter == 0 && lane == 0) {
-          const int got = atomicAdd(P.cnt + 2 * g.first_cta + h, 1);
-          last_s[h] = got == g.parts - 1;
-          if (last_s[h]) P.cnt[2 * g.first_cta + h] = 0;
-          __threadfence();
-        }
-        if (!(ok = meet())) break;
-        if (!last_s[h]) break;
-        mm = -INFINITY;
-#pragma unroll 1
-        for (int p = 0; p < g.parts; ++p)
-          mm = fmaxf(mm, __ldcg(part_slot(P, g.first_cta, p, kPartRows, D) + D * kPartRows + 2 * ri));
+        if (!slot) break;
+        *reinterpret_cast<float2*>(slot + (size_t)(D * kPartRows + 2 * ri)) = make_float2(mm, sum);
       }
       if (!ok) break;
       __syncwarp();

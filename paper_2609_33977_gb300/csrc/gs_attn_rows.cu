@@ -17,6 +17,8 @@ using namespace sm100;
 
 constexpr int kTile = 128;
 constexpr int kJoin = 8;   // rows of parts that a warp has under way when it joins them
+constexpr int kFlat = 16;  // parts joined in one level
+static_assert(kFlat <= 32, "a lane a part");
 
 struct FewTraits {
   static constexpr int kLeast = 2, kSnap = 1, kOver = 1;
@@ -485,61 +487,64 @@ __global__ void __launch_bounds__(RowsCfg<D, WR>::kThreads, 1) k_attn_rows(const
       }
       if (slot) {
         // ---- the last of the item's CTAs joins its parts, in order
-        __threadfence();
-        if (!meet()) break;
-        if (threadIdx.x == 0) {
-          const int got = atomicAdd(P.cnt + g.first_cta, 1);
-          last_s = got == g.parts - 1;
-          if (last_s) P.cnt[g.first_cta] = 0;
-          __threadfence();
-        }
-        if (!meet()) break;
-        if (last_s) {
-          for (int row = warp; row < g.s.rows; row += C::kWarps) {
-            float mm = -INFINITY, ll = 0.f, a[kC];
-#pragma unroll
-            for (int c = 0; c < kC; ++c) a[c] = 0.f;
 #pragma unroll 1
-            for (int p0 = 0; p0 < g.parts; p0 += 32) {   // a lane a part's maximum and sum, then kJoin parts' rows at once
-              const int np = min(32, g.parts - p0);
-              const float* mls = part_slot(P, g.first_cta, p0 + min(lane, np - 1), C::kRows, D) + (size_t)C::kRows * D + 2 * row;
-              float2 ml = __ldcg(reinterpret_cast<const float2*>(mls));
-              if (lane >= np) ml = make_float2(-INFINITY, 0.f);
-              float mn = fmaxf(mm, ml.x);
+        for (int level = 0; level < 2; ++level) {
+          const JoinStep j = join_step(g, level, kFlat);
+          if (j.n > 1) {
+            __threadfence();
+            if (!(ok = meet())) break;
+            if (threadIdx.x == 0) {
+              int32_t* cnt = P.cnt + level * (int)gridDim.x + g.first_cta + j.first;
+              last_s = atomicAdd(cnt, 1) == j.n - 1;
+              if (last_s) *cnt = 0;
+              __threadfence();
+            }
+            if (!(ok = meet())) break;
+            if (!last_s) break;
+            for (int row = warp; row < g.s.rows; row += C::kWarps) {   // a warp a row, a lane a part's maximum and sum
+              const auto part_at = [&](int i) { return part_slot(P, g.first_cta, j.first + i * j.stride, C::kRows, D); };
+              float2 ml = __ldcg(reinterpret_cast<const float2*>(part_at(min(lane, j.n - 1)) + (size_t)C::kRows * D + 2 * row));
+              if (lane >= j.n) ml = make_float2(-INFINITY, 0.f);
+              float mm = ml.x;
 #pragma unroll
-              for (int d = 16; d > 0; d >>= 1) mn = fmaxf(mn, __shfl_xor_sync(0xffffffffu, mn, d));
-              const float b = mn == -INFINITY ? 0.f : mn, before = ex2(mm - b), fp = ex2(ml.x - b);
-              float add = ml.y * fp;
+              for (int d = 16; d > 0; d >>= 1) mm = fmaxf(mm, __shfl_xor_sync(0xffffffffu, mm, d));
+              const float fp = ex2(ml.x - (mm == -INFINITY ? 0.f : mm));
+              float ll = ml.y * fp, a[kC];
 #pragma unroll
-              for (int d = 16; d > 0; d >>= 1) add += __shfl_xor_sync(0xffffffffu, add, d);
-              ll = ll * before + add;
+              for (int d = 16; d > 0; d >>= 1) ll += __shfl_xor_sync(0xffffffffu, ll, d);
 #pragma unroll
-              for (int c = 0; c < kC; ++c) a[c] *= before;
-              mm = mn;
+              for (int c = 0; c < kC; ++c) a[c] = 0.f;
 #pragma unroll 1
-              for (int p1 = 0; p1 < np; p1 += kJoin) {
+              for (int p0 = 0; p0 < j.n; p0 += kJoin) {
                 typename L::V v[kJoin];
 #pragma unroll
                 for (int i = 0; i < kJoin; ++i)
-                  v[i] = __ldcg(reinterpret_cast<const typename L::V*>(
-                                    part_slot(P, g.first_cta, p0 + min(p1 + i, np - 1), C::kRows, D) + (size_t)row * D) + lane);
+                  v[i] = __ldcg(reinterpret_cast<const typename L::V*>(part_at(min(p0 + i, j.n - 1)) + (size_t)row * D) + lane);
 #pragma unroll
                 for (int i = 0; i < kJoin; ++i) {
-                  const float f = __shfl_sync(0xffffffffu, fp, (p1 + i) & 31);
+                  const float f = __shfl_sync(0xffffffffu, fp, (p0 + i) & 31);
                   float x[kC];
                   L::unpack(v[i], x);
-                  if (p1 + i < np) {
+                  if (p0 + i < j.n) {
 #pragma unroll
                     for (int c = 0; c < kC; ++c) a[c] = fmaf(x[c], f, a[c]);
                   }
                 }
               }
+              if (!j.last) {   // in the place of the group's first part
+                float* to = part_at(0);
+                reinterpret_cast<typename L::V*>(to + (size_t)row * D)[lane] = L::pack(a);
+                if (lane == 0) *reinterpret_cast<float2*>(to + (size_t)C::kRows * D + 2 * row) = make_float2(mm, ll);
+              } else {
+                const int tok = row_token(P, row), hd = row - tok * P.group;
+                L::store_bf16(P.out + ((int64_t)(g.s.tok0 + tok) * P.q_heads + g.h * P.group + hd) * D + kC * lane, a,
+                              g.s.seen(tok) > 0 ? 1.f / ll : 0.f);
+              }
             }
-            const int tok = row_token(P, row), hd = row - tok * P.group;
-            L::store_bf16(P.out + ((int64_t)(g.s.tok0 + tok) * P.q_heads + g.h * P.group + hd) * D + kC * lane, a,
-                          g.s.seen(tok) > 0 ? 1.f / ll : 0.f);
           }
+          if (j.last) break;
         }
+        if (!ok) break;
       }
     }
   }
