@@ -15,7 +15,7 @@ static_assert(kCounterBytes >= 6 * 4 * kMaxCtas, "six counters a CTA");
 
 int attention_ctas() { return std::min(sm_count(), kMaxCtas); }
 
-size_t part_bytes(int rows, int head_dim) { return (size_t)attention_ctas() * 2 * (size_t)rows * (size_t)(head_dim + 2) * 4; }
+size_t parts_bytes(int size) { return (size_t)attention_ctas() * 2 * (size_t)size * 4; }
 
 // The few-row kernel serves sequences of at most attn_rows_most() rows, the chunk kernel
 // the others.  Where all sequences are as long as the longest (known from the sizes
@@ -33,14 +33,15 @@ Kernels kernels_of(const gs_seq_batch& b, int32_t group) {
 
 bool attention_units_fit(const gs_paged_cache& c, const gs_seq_batch& b, int32_t q_heads) {
   const double rows = (double)b.tokens * (q_heads / c.kv_heads), cap = (double)b.table_width * c.page_size;
-  const double units = (rows / (attn_chunk_rows() / 2) + b.n + 1.0) * c.kv_heads * (cap / std::min(attn_rows_tile(), attn_chunk_tile()) + 1.0);
+  const double items = (rows / attn_chunk_rows() + b.n + 1.0) * c.kv_heads;
+  const double units = items * (cap / std::min(attn_rows_tile(), attn_chunk_tile()) + 1.0 + attn_most_over());
   return rows < 1e9 && units < 2e9;
 }
 
 size_t attention_workspace_bytes(const gs_paged_cache& c, const gs_seq_batch& b, int32_t q_heads) {
   const Kernels k = kernels_of(b, q_heads / c.kv_heads);
-  return (size_t)kCounterBytes + (k.chunk ? part_bytes(attn_chunk_rows(), c.head_dim) : 0) +
-         (k.few ? part_bytes(attn_rows_most(), c.head_dim) : 0);
+  return (size_t)kCounterBytes + (k.chunk ? parts_bytes(attn_chunk_part(c.head_dim)) : 0) +
+         (k.few ? parts_bytes(attn_rows_part(c.head_dim)) : 0);
 }
 
 gs_status launch_paged_attention(const gs_paged_cache& c, const gs_seq_batch& b, const void* q, int64_t q_stride,
@@ -96,7 +97,7 @@ gs_status launch_paged_attention(const gs_paged_cache& c, const gs_seq_batch& b,
   if (!encode_tmap_slabs_bf16(&P.kmap, c.k_dev, D, rows, box, slabs) || !encode_tmap_slabs_bf16(&P.vmap, c.v_dev, D, rows, box, slabs))
     return GS_ERR_CUDA;
   P.cnt = cnt + 4 * kMaxCtas;
-  P.parts = reinterpret_cast<float*>(parts + (k.chunk ? part_bytes(attn_chunk_rows(), c.head_dim) : 0));
+  P.parts = reinterpret_cast<float*>(parts + (k.chunk ? parts_bytes(attn_chunk_part(c.head_dim)) : 0));
   P.min_rows = 1;
   P.max_rows = attn_rows_held((int)std::min((int64_t)b.max_new * P.group, (int64_t)attn_rows_most()));
   P.zero_rest = !k.chunk;

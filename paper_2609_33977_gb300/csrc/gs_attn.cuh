@@ -28,7 +28,7 @@ struct AttnParams {
   const int32_t* table;
   int32_t* cnt;             // [2][CTAs] arrivals (a half of the item each in the chunk kernel) at the group of parts, and at the
                             // split item, that begin in the CTA; zero between calls
-  float* parts;             // [CTAs][2][rows of a tile][head_dim + 2]
+  float* parts;             // [CTAs][2] parts
   int* err;
   int64_t q_stride, tokens, pages;
   int32_t n_seqs, width, page_shift, q_heads, kv_heads, group;
@@ -44,6 +44,7 @@ struct AttnParams {
 
 // attn_rows.cu: sequences of at most P.max_rows rows, one of the numbers that the kernel's forms hold
 int attn_rows_most();
+int attn_rows_part(int head_dim);   // floats of a part in the workspace, at most
 int attn_rows_held(int rows);       // the least of these numbers that is at least `rows`
 int attn_rows_box(int page_size);   // rows of a TMA box
 int attn_rows_tile();               // keys of a unit
@@ -53,7 +54,9 @@ gs_status launch_attn_rows(const AttnParams& P, int head_dim, int ctas, cudaStre
 int attn_chunk_box(int page_size);
 int attn_chunk_tile();
 int attn_chunk_half_tokens(int group);   // tokens of half an item
-int attn_chunk_rows();                   // rows of a part in the workspace
+int attn_chunk_rows();                   // an item has more rows than this, but for a sequence's last
+int attn_chunk_part(int head_dim);       // floats of a part in the workspace
+int attn_most_over();                    // what an item costs beside its units, in units, at most
 gs_status launch_attn_chunk(const AttnParams& P, int head_dim, int ctas, cudaStream_t s);
 
 struct SeqInfo {
@@ -391,8 +394,8 @@ __device__ __forceinline__ void zero_rows(const AttnParams& P, int head_dim, int
 
 // Where part `part` of a split item lies: a CTA holds at most one part of an item that
 // began before it, and at most one of an item that goes on after it.
-__device__ __forceinline__ float* part_slot(const AttnParams& P, int first_cta, int part, int rows, int head_dim) {
-  return P.parts + ((int64_t)(first_cta + part) * 2 + (part == 0 ? 1 : 0)) * rows * (head_dim + 2);
+__device__ __forceinline__ float* part_slot(const AttnParams& P, int first_cta, int part, int size) {
+  return P.parts + ((int64_t)(first_cta + part) * 2 + (part == 0 ? 1 : 0)) * size;
 }
 
 // The two levels in which a split item's parts are joined: groups of neighbouring parts, each

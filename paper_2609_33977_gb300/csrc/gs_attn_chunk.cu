@@ -31,16 +31,18 @@ using namespace sm100;
 constexpr int kCT = 64;                        // keys of a unit
 constexpr int kHalf = 128;                     // lanes of a half
 constexpr int kPartRows = 2 * kHalf;           // rows of a part in the workspace
+constexpr int kPartPad = 2;                    // floats of a row of it beside the output's
 constexpr int kAcThreads = 512;                // warps: keys, values, S x 2, P V x 2, two value checkers; two softmax warpgroups
 constexpr int kRing = 5;                       // slots of keys, and as many of values
 constexpr int kSegs = 4;
 constexpr int kFlat = 6;                       // parts joined in one level
+constexpr int kJoin = 3;                       // of them under way at once
 constexpr int kCheckers = 2;
 constexpr int kRegsOther = 56, kRegsSoftmax = 200;
 static_assert(8 * 32 * (kRegsOther + kRegsSoftmax) <= kAcThreads * 128, "register split");
 
 struct ChunkTraits {
-  static constexpr int kLeast = 8, kSnap = 3, kOver = 9;
+  static constexpr int kLeast = 8, kSnap = 3, kOver = 8;
   static constexpr bool kOneTile = false;
   // A half holds whole tokens (P.half_tokens: group x that of its 128 lanes are used), an item two halves.
   static __device__ __forceinline__ int row_tiles(const SeqInfo& s, const AttnParams& P) {
@@ -132,6 +134,18 @@ __device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
   uint64_t d;
   asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
   return d;
+}
+
+// from L2, in program order: loads that are written together are under way together
+__device__ __forceinline__ float4 load_part(const float* p) {
+  float4 v;
+  asm volatile("ld.global.cg.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "l"(p));
+  return v;
+}
+__device__ __forceinline__ float2 load_ml(const float* p) {
+  float2 v;
+  asm volatile("ld.global.cg.v2.f32 {%0, %1}, [%2];" : "=f"(v.x), "=f"(v.y) : "l"(p));
+  return v;
 }
 
 // two bf16: 0 x + c
@@ -638,6 +652,10 @@ __global__ void __launch_bounds__(kAcThreads, 1) k_attn_chunk(const __grid_const
       // the row in the output (its elements fit memory, so rows fit 32 bits)
       const uint32_t mine = row.on ? (uint32_t)(g.s.tok0 + row.tok) * (uint32_t)P.q_heads + (uint32_t)(g.h * P.group + row.hd) : ~0u;
       const int ri = h * kHalf + 32 * quarter + lane;
+      // Rows that exist, in whole 128-byte lines: a sector that is written in part costs whoever reads it a fill from HBM
+      // (9 tokens of 28/4 heads at 30000 keys 50 us, 43 so).
+      const bool some = __shfl_sync(0xffffffffu, row.on, lane & ~7);
+      const int ri_read = some ? ri : ri - lane;
       JoinStep j = {g.part, 1, 1, g.parts == 1};
       float mm = m, sum = l;
 #pragma unroll 1
@@ -657,10 +675,15 @@ __global__ void __launch_bounds__(kAcThreads, 1) k_attn_chunk(const __grid_const
           if (!last_s[h]) break;
           mm = -INFINITY;
 #pragma unroll 1
-          for (int p = 0; p < j.n; ++p)
-            mm = fmaxf(mm, __ldcg(part_slot(P, g.first_cta, j.first + p * j.stride, kPartRows, D) + D * kPartRows + 2 * ri));
+          for (int p0 = 0; p0 < j.n; p0 += 4) {
+            float2 ml[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+              ml[i] = load_ml(part_slot(P, g.first_cta, j.first + min(p0 + i, j.n - 1) * j.stride, kPartRows * (D + kPartPad)) + D * kPartRows + 2 * ri_read);
+            mm = fmaxf(max3(mm, ml[0].x, ml[1].x), fmaxf(ml[2].x, ml[3].x));
+          }
         }
-        float* slot = j.last ? nullptr : part_slot(P, g.first_cta, j.first, kPartRows, D);
+        float* slot = j.last ? nullptr : part_slot(P, g.first_cta, j.first, kPartRows * (D + kPartPad));
 #pragma unroll 1
         for (int c0 = 0; c0 < D; c0 += 32) {
           float o[32];
@@ -676,25 +699,38 @@ __global__ void __launch_bounds__(kAcThreads, 1) k_attn_chunk(const __grid_const
               for (int e = 0; e < 32; ++e) o[e] = __uint_as_float(v[e]);
             }
           } else {
+            // kJoin parts' pieces under way at once, at clamped addresses
             sum = 0.f;
             const float base = mm == -INFINITY ? 0.f : mm;
-#pragma unroll 2
-            for (int p = 0; p < j.n; ++p) {
-              const float* sp = part_slot(P, g.first_cta, j.first + p * j.stride, kPartRows, D);
-              const float2 ml = __ldcg(reinterpret_cast<const float2*>(sp + D * kPartRows + 2 * ri));
-              const float fp = ml.x == mm ? 1.f : ex2((ml.x - base) * c);
-              sum = fmaf(ml.y, fp, sum);
+            if (!__any_sync(0xffffffffu, some)) break;
+#pragma unroll 1
+            for (int p0 = 0; p0 < j.n; p0 += kJoin) {
+              float2 ml[kJoin];
+              float4 v[kJoin][8];
 #pragma unroll
-              for (int e = 0; e < 32; e += 4) {
-                const float4 v = __ldcg(reinterpret_cast<const float4*>(sp + (size_t)((c0 + e) * kPartRows + 4 * ri)));
-                o[e] = fmaf(v.x, fp, o[e]);
-                o[e + 1] = fmaf(v.y, fp, o[e + 1]);
-                o[e + 2] = fmaf(v.z, fp, o[e + 2]);
-                o[e + 3] = fmaf(v.w, fp, o[e + 3]);
+              for (int i = 0; i < kJoin; ++i) {
+                const float* sp = part_slot(P, g.first_cta, j.first + min(p0 + i, j.n - 1) * j.stride, kPartRows * (D + kPartPad));
+                ml[i] = load_ml(sp + D * kPartRows + 2 * ri_read);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v[i][e] = load_part(sp + (size_t)((c0 + 4 * e) * kPartRows + 4 * ri_read));
+              }
+#pragma unroll
+              for (int i = 0; i < kJoin; ++i) {
+                if (p0 + i >= j.n) break;
+                const float fp = ml[i].x == mm ? 1.f : ex2((ml[i].x - base) * c);
+                sum = fmaf(ml[i].y, fp, sum);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                  o[4 * e] = fmaf(v[i][e].x, fp, o[4 * e]);
+                  o[4 * e + 1] = fmaf(v[i][e].y, fp, o[4 * e + 1]);
+                  o[4 * e + 2] = fmaf(v[i][e].z, fp, o[4 * e + 2]);
+                  o[4 * e + 3] = fmaf(v[i][e].w, fp, o[4 * e + 3]);
+                }
               }
             }
           }
           if (slot) {
+            if (!some) continue;
 #pragma unroll
             for (int e = 0; e < 32; e += 4)
               *reinterpret_cast<float4*>(slot + (size_t)((c0 + e) * kPartRows + 4 * ri)) = make_float4(o[e], o[e + 1], o[e + 2], o[e + 3]);
@@ -786,7 +822,11 @@ int attn_chunk_box(int page_size) { return page_size < kCT ? page_size : kCT; }
 
 int attn_chunk_tile() { return kCT; }
 
-int attn_chunk_rows() { return kPartRows; }
+int attn_chunk_rows() { return kHalf; }   // two halves, each of more than half its lanes
+
+int attn_most_over() { return ChunkTraits::kOver; }
+
+int attn_chunk_part(int head_dim) { return kPartRows * (head_dim + kPartPad); }
 
 int attn_chunk_half_tokens(int group) { return kHalf / group; }
 

@@ -16,6 +16,8 @@ namespace {
 using namespace sm100;
 
 constexpr int kTile = 128;
+constexpr int kMost = 32;      // rows
+constexpr int kPartPad = 8;    // floats of a row of a part beside the output's
 constexpr int kJoin = 8;   // rows of parts that a warp has under way when it joins them
 constexpr int kFlat = 16;  // parts joined in one level
 static_assert(kFlat <= 32, "a lane a part");
@@ -75,11 +77,12 @@ struct RowsCfg {
   static constexpr int kWK = kWarps / WR;
   static constexpr int kThreads = (kWarps + 1) * 32; // + the fetching warp
   static constexpr int kRows = 16 * WR;
+  static constexpr int kPart = kRows * (D + kPartPad);   // floats of a part
   static constexpr int kOpBytes = kTile * D * 2;
   static constexpr int kStageBytes = 2 * kOpBytes;   // also what a join needs: kWarps x 16 x D floats
   static constexpr int kQRow = D * 2 + 16;           // bytes of a row of queries: rows start in different banks
   static constexpr int kQBytes = kRows * kQRow;
-  static constexpr int kQSlots = WR == 4 ? 1 : 2;    // segments whose queries are here ahead
+  static constexpr int kQSlots = 2;                  // segments whose queries are here ahead
   static constexpr int kStages = 192 * 1024 / kStageBytes;
   static constexpr int kSmem = kStages * kStageBytes + kQSlots * kQBytes + 1024;
   static_assert(kWarps * 16 * D * 4 <= kStageBytes, "join");
@@ -216,7 +219,7 @@ __global__ void __launch_bounds__(RowsCfg<D, WR>::kThreads, 1) k_attn_rows(const
   } else {
     // ------------------------------------------------------------ compute
     const int wr = warp / WK, wk = warp % WK, gq = lane >> 2, qd = lane & 3;
-    constexpr int kKeys = kTile / WK;              // this warp's keys of a unit: 16, 32 or 64
+    constexpr int kKeys = kTile / WK;              // this warp's keys of a unit: 16 or 32
     constexpr int kSub = kKeys < 32 ? kKeys : 32;  // keys between two steps of the running maximum
     constexpr int kNt = kSub / 8;
     uint32_t jph = 0, mph = 0;
@@ -227,6 +230,12 @@ __global__ void __launch_bounds__(RowsCfg<D, WR>::kThreads, 1) k_attn_rows(const
       const bool met = wait_warp(&meet_bar, mph);
       mph ^= 1u;
       return met;
+    };
+    // A part: [rows][D], then [rows][8] with maximum and sum, the rest zeros: a 32-byte sector that is written in part
+    // costs whoever reads it a fill from HBM.
+    const auto store_part = [&](float* slot, int row, const float (&a)[kC], float mm, float ll) {
+      reinterpret_cast<typename L::V*>(slot + row * D)[lane] = L::pack(a);
+      if (lane < 2) reinterpret_cast<float4*>(slot + C::kRows * D + kPartPad * row)[lane] = lane == 0 ? make_float4(mm, ll, 0.f, 0.f) : make_float4(0.f, 0.f, 0.f, 0.f);
     };
     uint32_t st = 0, ph = 0u, turn = 0, qs = 0;
     bool ok = true;
@@ -431,7 +440,7 @@ __global__ void __launch_bounds__(RowsCfg<D, WR>::kThreads, 1) k_attn_rows(const
       }
       const bool fix = bad_s[turn & 3] != 0;
       if (threadIdx.x == 0) bad_s[(turn + 2) & 3] = 0;
-      float* slot = g.parts > 1 ? part_slot(P, g.first_cta, g.part, C::kRows, D) : nullptr;
+      float* slot = g.parts > 1 ? part_slot(P, g.first_cta, g.part, C::kPart) : nullptr;
       for (int row = warp; row < g.s.rows; row += C::kWarps) {   // a warp a row
         const float2 ml = lane < WK ? join_ml[turn & 1][lane * C::kRows + row] : make_float2(-INFINITY, 0.f);
         float mm = ml.x;
@@ -471,8 +480,7 @@ __global__ void __launch_bounds__(RowsCfg<D, WR>::kThreads, 1) k_attn_rows(const
           }
         }
         if (slot) {
-          reinterpret_cast<typename L::V*>(slot + (size_t)row * D)[lane] = L::pack(a);
-          if (lane == 0) *reinterpret_cast<float2*>(slot + (size_t)C::kRows * D + 2 * row) = make_float2(mm, ll);
+          store_part(slot, row, a, mm, ll);
         } else {
           L::store_bf16(P.out + ((int64_t)(g.s.tok0 + tok) * P.q_heads + g.h * P.group + hd) * D + kC * lane, a,
                         vis > 0 ? 1.f / ll : 0.f);
@@ -502,8 +510,8 @@ __global__ void __launch_bounds__(RowsCfg<D, WR>::kThreads, 1) k_attn_rows(const
             if (!(ok = meet())) break;
             if (!last_s) break;
             for (int row = warp; row < g.s.rows; row += C::kWarps) {   // a warp a row, a lane a part's maximum and sum
-              const auto part_at = [&](int i) { return part_slot(P, g.first_cta, j.first + i * j.stride, C::kRows, D); };
-              float2 ml = __ldcg(reinterpret_cast<const float2*>(part_at(min(lane, j.n - 1)) + (size_t)C::kRows * D + 2 * row));
+              const auto part_at = [&](int i) { return part_slot(P, g.first_cta, j.first + i * j.stride, C::kPart); };
+              float2 ml = __ldcg(reinterpret_cast<const float2*>(part_at(min(lane, j.n - 1)) + C::kRows * D + kPartPad * row));
               if (lane >= j.n) ml = make_float2(-INFINITY, 0.f);
               float mm = ml.x;
 #pragma unroll
@@ -519,7 +527,7 @@ __global__ void __launch_bounds__(RowsCfg<D, WR>::kThreads, 1) k_attn_rows(const
                 typename L::V v[kJoin];
 #pragma unroll
                 for (int i = 0; i < kJoin; ++i)
-                  v[i] = __ldcg(reinterpret_cast<const typename L::V*>(part_at(min(p0 + i, j.n - 1)) + (size_t)row * D) + lane);
+                  v[i] = __ldcg(reinterpret_cast<const typename L::V*>(part_at(min(p0 + i, j.n - 1)) + row * D) + lane);
 #pragma unroll
                 for (int i = 0; i < kJoin; ++i) {
                   const float f = __shfl_sync(0xffffffffu, fp, (p0 + i) & 31);
@@ -532,9 +540,7 @@ __global__ void __launch_bounds__(RowsCfg<D, WR>::kThreads, 1) k_attn_rows(const
                 }
               }
               if (!j.last) {   // in the place of the group's first part
-                float* to = part_at(0);
-                reinterpret_cast<typename L::V*>(to + (size_t)row * D)[lane] = L::pack(a);
-                if (lane == 0) *reinterpret_cast<float2*>(to + (size_t)C::kRows * D + 2 * row) = make_float2(mm, ll);
+                store_part(part_at(0), row, a, mm, ll);
               } else {
                 const int tok = row_token(P, row), hd = row - tok * P.group;
                 L::store_bf16(P.out + ((int64_t)(g.s.tok0 + tok) * P.q_heads + g.h * P.group + hd) * D + kC * lane, a,
@@ -575,19 +581,20 @@ gs_status rows_launch(const AttnParams& P, int ctas, cudaStream_t s) {
 
 }  // namespace
 
-int attn_rows_most() { return 64; }
+int attn_rows_most() { return kMost; }
+
+int attn_rows_part(int head_dim) { return kMost * (head_dim + kPartPad); }
 
 int attn_rows_box(int page_size) { return page_size < kTile ? page_size : kTile; }
 
 int attn_rows_tile() { return kTile; }
 
-int attn_rows_held(int rows) { return rows <= 16 ? 16 : rows <= 32 ? 32 : 64; }
+int attn_rows_held(int rows) { return rows <= 16 ? 16 : 32; }
 
 gs_status launch_attn_rows(const AttnParams& P, int head_dim, int ctas, cudaStream_t s) {
-  const int wr = P.max_rows / 16;
-  if (head_dim == 128)
-    return wr == 1 ? rows_launch<128, 1>(P, ctas, s) : wr == 2 ? rows_launch<128, 2>(P, ctas, s) : rows_launch<128, 4>(P, ctas, s);
-  return wr == 1 ? rows_launch<64, 1>(P, ctas, s) : wr == 2 ? rows_launch<64, 2>(P, ctas, s) : rows_launch<64, 4>(P, ctas, s);
+  const bool one = P.max_rows == 16;
+  if (head_dim == 128) return one ? rows_launch<128, 1>(P, ctas, s) : rows_launch<128, 2>(P, ctas, s);
+  return one ? rows_launch<64, 1>(P, ctas, s) : rows_launch<64, 2>(P, ctas, s);
 }
 
 }  // namespace gs
