@@ -404,15 +404,24 @@ def _require_like(t: torch.Tensor, shape, name: str) -> int:
 
 
 def _norm(x, weight, residual, eps, h, y, y8, scales, group, stream):
+    """The outputs are addresses."""
     if x.dim() != 2:
         raise ValueError("x must be [T, n]")
     shape = x.shape
     T, n = shape
     _check(lib.gs_add_rms_norm(
         _require_like(x, shape, "x"), None if residual is None else _require_like(residual, shape, "residual"),
-        _require_like(weight, (n,), "weight"), T, n, eps, None if h is None else _require_like(h, shape, "h"),
-        None if y is None else _require_like(y, shape, "y"), None if y8 is None else y8.data_ptr(),
-        None if scales is None else scales.data_ptr(), group, _stream_ptr(stream)), "gs_add_rms_norm")
+        _require_like(weight, (n,), "weight"), T, n, eps, h, y, y8, scales, group, _stream_ptr(stream)), "gs_add_rms_norm")
+
+
+def _norm_sum(x, residual, h, stream):
+    """h and its address."""
+    if h is not None:
+        return h, _require_like(h, x.shape, "h")
+    if residual is None:
+        return None, None
+    h = torch.empty_like(x) if stream is None else _empty(x.shape, x.dtype, x.device, stream)
+    return h, h.data_ptr()
 
 
 def add_rms_norm(x: torch.Tensor, weight: torch.Tensor, residual: Optional[torch.Tensor] = None, eps: float = 1e-5,
@@ -421,11 +430,13 @@ def add_rms_norm(x: torch.Tensor, weight: torch.Tensor, residual: Optional[torch
     """h = x + residual, y = h / sqrt(mean(h^2) + eps) * weight over the rows of x [T, n]: (y, h), both bf16.
     Without a residual, h is None unless it was given (a copy of x then).  h may be the residual's or x's own
     tensor, y x's own."""
-    if y is None:
+    if y is None:   # x is checked before anything uses a tensor like it
         y = torch.empty_like(x) if stream is None else _empty(x.shape, x.dtype, x.device, stream)
-    if h is None and residual is not None:
-        h = torch.empty_like(x) if stream is None else _empty(x.shape, x.dtype, x.device, stream)
-    _norm(x, weight, residual, eps, h, y, None, None, 0, stream)
+        to_y = y.data_ptr()
+    else:
+        to_y = _require_like(y, x.shape, "y")
+    h, to_h = _norm_sum(x, residual, h, stream)
+    _norm(x, weight, residual, eps, to_h, to_y, None, None, 0, stream)
     return y, h
 
 
@@ -435,11 +446,11 @@ def add_rms_norm_fp8(x: torch.Tensor, weight: torch.Tensor, residual: Optional[t
     element's group of columns (0: one group a row; 128)."""
     if x.dim() != 2:
         raise ValueError("x must be [T, n]")
-    y8 = _empty(x.shape, torch.float8_e4m3fn, x.device, stream)
-    scales = _empty((x.shape[0], -(-x.shape[1] // group) if group > 0 else 1), torch.float32, x.device, stream)
-    if h is None and residual is not None:
-        h = _empty(x.shape, torch.bfloat16, x.device, stream)
-    _norm(x, weight, residual, eps, h, None, y8, scales, group, stream)
+    shape, device = x.shape, x.device
+    y8 = _empty(shape, torch.float8_e4m3fn, device, stream)
+    scales = _empty((shape[0], -(-shape[1] // group) if group > 0 else 1), torch.float32, device, stream)
+    h, to_h = _norm_sum(x, residual, h, stream)
+    _norm(x, weight, residual, eps, to_h, None, y8.data_ptr(), scales.data_ptr(), group, stream)
     return y8, scales, h
 
 
