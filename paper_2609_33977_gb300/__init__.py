@@ -1,7 +1,8 @@
 """GB300-native group-sparse linear layer y = x (W (.) M)^T (GroupMask, Sec. 2.1, Eq. 1).
 
 Submodules:
-  groupsparse  ctypes binding of libgroupsparse.so (pack / linear / unpack); loads the CUDA library
+  groupsparse  ctypes binding of libgroupsparse.so (pack / linear / unpack, and a served block's norm, adapters,
+               cache and attention); loads the CUDA library
   workload     seeded synthetic inputs (weights, group masks, activations)
   build        nvcc build of libgroupsparse.so for sm_103a
 
