@@ -50,7 +50,7 @@ static_assert(8 * 32 * (kRegsOther + kRegsSoftmax) <= kAcThreads * 128, "registe
 // kSnap 1 / 3 / 6: prompts 224 / 221 / 222, the mixed step 82 / 82 / 84.  kLeast 6 / 8 / 12: 30 tokens at 8192 keys
 // (28/4 heads) 39 / 34 / 36, 64 tokens 35 / 37 / 38.
 struct ChunkTraits {
-  static constexpr int kLeast = 8, kSnap = 3, kOver = 8;
+  static constexpr int kLeast = 8, kSnap = 3, kOver = 5;
   static constexpr bool kOneTile = false;
   // A half holds whole tokens (P.half_tokens: group x that of its 128 lanes are used), an item two halves.
   static __device__ __forceinline__ int row_tiles(const SeqInfo& s, const AttnParams& P) {
@@ -455,36 +455,37 @@ __global__ void __launch_bounds__(kAcThreads, 1) k_attn_chunk(const __grid_const
           }
           const int key0 = t * kCT;
           if (key0 + kCT > all_see) {
-            constexpr int kPieces = D / 8, kStep = 32 / kPieces, kDeep = 16 / kStep;   // keys of a step of the warp; steps at once
-            const int end = min(kCT, max(0, len - key0)), piece = lane % kPieces;
+            // 16 keys at a time, of one box (a page has 16 at least): a key's row is kSlabs pieces of 128 bytes, whose swizzle
+            // does not matter here.  A lane has 16 bytes of one key in kStep.
+            constexpr int kPieces = D / 8, kStep = 32 / kPieces, kDeep = 16 / kStep;
+            const int from = max(0, all_see - key0), end = min(kCT, max(0, len - key0)), piece = lane % kPieces;
             bool bad = false;
-            // a key's row is kSlabs pieces of 128 bytes; their swizzle does not matter here
-            const auto piece_at = [&](int k) {
-              return ring_v + vs * C::kOpBytes + (((k >> box_shift) * C::kSlabs + (piece >> 3)) << box_shift) * 128 +
-                     (k & (box - 1)) * 128 + (piece & 7) * 16;
-            };
-            for (int k0 = max(0, all_see - key0) + mine * (kDeep * kStep); k0 < kCT; k0 += kCheckers * kDeep * kStep) {
+#pragma unroll 1
+            for (int k0 = (from & ~15) + 16 * mine; k0 < kCT; k0 += 16 * kCheckers) {
+              uint8_t* base = ring_v + vs * C::kOpBytes + (((k0 >> box_shift) * C::kSlabs + (piece >> 3)) << box_shift) * 128 +
+                              ((k0 & (box - 1)) + lane / kPieces) * 128 + (piece & 7) * 16;
               uint4 x[kDeep];
-              uint32_t any = 0u;   // bf16 pairs: the sum of 0 x, NaN where some x is an infinity or NaN
+              uint32_t any[4] = {0u, 0u, 0u, 0u};   // bf16 pairs: sums of 0 x, NaN where some x is an infinity or NaN
+#pragma unroll
+              for (int i = 0; i < kDeep; ++i) x[i] = *reinterpret_cast<const uint4*>(base + i * (kStep * 128));
 #pragma unroll
               for (int i = 0; i < kDeep; ++i) {
-                x[i] = *reinterpret_cast<const uint4*>(piece_at(min(k0 + i * kStep + lane / kPieces, kCT - 1)));
+                any[0] = times_zero(x[i].x, any[0]);
+                any[1] = times_zero(x[i].y, any[1]);
+                any[2] = times_zero(x[i].z, any[2]);
+                any[3] = times_zero(x[i].w, any[3]);
               }
-#pragma unroll
-              for (int i = 0; i < kDeep; ++i)
-                any = times_zero(x[i].w, times_zero(x[i].z, times_zero(x[i].y, times_zero(x[i].x, any))));
-              if (nonfinite2(any) == 0u && k0 + kDeep * kStep <= end) continue;   // the rule: nothing to do
+              // +-0 sums: an exponent of ones stays one in the "or" of all four
+              if (nonfinite2(any[0] | any[1] | any[2] | any[3]) == 0u && k0 + 16 <= end) continue;   // the rule: nothing to do
 #pragma unroll 1
               for (int i = 0; i < kDeep; ++i) {
                 const int k = k0 + i * kStep + lane / kPieces;
-                if (k >= kCT) break;
-#pragma unroll 1
-                for (int j = 0; j < 4; ++j) {
-                  uint32_t* w = reinterpret_cast<uint32_t*>(piece_at(k)) + j;
-                  const uint32_t x = k < end ? *w : 0u, n = nonfinite2(x);
-                  bad |= n != 0u;
-                  *w = x & ~n;
-                }
+                if (k < from) continue;   // every row sees it
+                uint4* at16 = reinterpret_cast<uint4*>(base + i * (kStep * 128));
+                uint4 v = k < end ? *at16 : make_uint4(0u, 0u, 0u, 0u);
+                const uint32_t n[4] = {nonfinite2(v.x), nonfinite2(v.y), nonfinite2(v.z), nonfinite2(v.w)};
+                bad |= (n[0] | n[1] | n[2] | n[3]) != 0u;
+                *at16 = make_uint4(v.x & ~n[0], v.y & ~n[1], v.z & ~n[2], v.w & ~n[3]);
               }
             }
             if (bad) bad_s[at] = 1;
