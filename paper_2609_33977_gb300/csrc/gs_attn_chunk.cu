@@ -156,6 +156,29 @@ __device__ __forceinline__ float2 load_ml(const float* p) {
   return v;
 }
 
+// within a unit in the last place (the output is rounded to 8 bits of fraction)
+__device__ __forceinline__ float reciprocal(float x) {
+  float y;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+
+// 64 bytes at an address that is a multiple of 16: whole 32-byte sectors where it is one of 32
+__device__ __forceinline__ void store_sectors(uint16_t* p, const uint32_t (&w)[16]) {
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    if ((reinterpret_cast<uintptr_t>(p) & 16) == 0) {
+      asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p + 16 * i), "r"(w[8 * i]), "r"(w[8 * i + 1]),
+                   "r"(w[8 * i + 2]), "r"(w[8 * i + 3]), "r"(w[8 * i + 4]), "r"(w[8 * i + 5]), "r"(w[8 * i + 6]), "r"(w[8 * i + 7])
+                   : "memory");
+    } else {
+      uint4* q = reinterpret_cast<uint4*>(p + 16 * i);
+      q[0] = make_uint4(w[8 * i], w[8 * i + 1], w[8 * i + 2], w[8 * i + 3]);
+      q[1] = make_uint4(w[8 * i + 4], w[8 * i + 5], w[8 * i + 6], w[8 * i + 7]);
+    }
+  }
+}
+
 // two bf16: 0 x + c
 __device__ __forceinline__ uint32_t times_zero(uint32_t x, uint32_t c) {
   uint32_t d;
@@ -745,32 +768,13 @@ __global__ void __launch_bounds__(kAcThreads, 1) k_attn_chunk(const __grid_const
               *reinterpret_cast<float4*>(slot + (size_t)((c0 + e) * kPartRows + 4 * ri)) = make_float4(o[e], o[e + 1], o[e + 2], o[e + 3]);
             continue;
           }
-          // A lane has a whole row: four lanes exchange 16-byte pieces until each has one piece of four rows, and write
-          // 64 bytes of a row together.
-          const float inv = row.vis > 0 ? 1.f / sum : 0.f;
-          uint32_t w[4][4];   // [piece, then row][word]
+          // A lane has a whole row: 64 bytes of it, in two sectors.
+          if (row.on) {
+            const float inv = row.vis > 0 ? reciprocal(sum) : 0.f;
+            uint32_t w[16];
 #pragma unroll
-          for (int i = 0; i < 4; ++i)
-#pragma unroll
-            for (int k = 0; k < 4; ++k) w[i][k] = pack_bf16(o[8 * i + 2 * k] * inv, o[8 * i + 2 * k + 1] * inv);
-#pragma unroll
-          for (int d = 1; d <= 2; d <<= 1)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              if (i & d) continue;
-#pragma unroll
-              for (int k = 0; k < 4; ++k) {
-                const bool up = (lane & d) != 0;
-                const uint32_t got = __shfl_xor_sync(0xffffffffu, up ? w[i][k] : w[i + d][k], d);
-                w[i][k] = up ? got : w[i][k];
-                w[i + d][k] = up ? w[i + d][k] : got;
-              }
-            }
-#pragma unroll
-          for (int r = 0; r < 4; ++r) {
-            const uint32_t dst = __shfl_sync(0xffffffffu, mine, (lane & ~3) + r);
-            if (dst != ~0u)
-              *reinterpret_cast<uint4*>(P.out + (int64_t)dst * D + c0 + 8 * (lane & 3)) = make_uint4(w[r][0], w[r][1], w[r][2], w[r][3]);
+            for (int e = 0; e < 16; ++e) w[e] = pack_bf16(o[2 * e] * inv, o[2 * e + 1] * inv);
+            store_sectors(P.out + (int64_t)mine * D + c0, w);
           }
         }
         if (phase == 0 && bad_s[at]) {
