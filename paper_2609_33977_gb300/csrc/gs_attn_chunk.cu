@@ -21,10 +21,11 @@
 // end become zeros, and infinities and NaN are taken out (a weight of zero would not
 // silence them) and added at the end to the rows that see them.
 //
-// 8192 new tokens, 40 heads: 520 us, 1322 TFLOP/s of the pairs that are seen; 4096: 162 us,
-// 1060; prompts of 4096, 1023, 1777 and 300: 221 us, 980; 512 tokens at 8192 keys, 28/4
-// heads: 65 us, 890.  What short items lose is their ends: the first keys' way to the
-// exponentials, and the last output's way out of TMEM (some 9000 cycles an item in all).
+// 8192 new tokens, 40 heads: 506 us, 1360 TFLOP/s of the pairs that are seen; 4096: 153 us,
+// 1120; prompts of 4096, 1023, 1777 and 300: 204 us, 1060; 512 tokens at 8192 keys, 28/4
+// heads: 62 us, 930.  What short items lose is their ends: the first keys' way to the
+// exponentials, and the last output's way out of TMEM (some 6000 cycles an item in all,
+// a unit takes 1550).
 //
 // TMEM: per half S (64 columns) and two P (32 each) from column 0 / 128, O from 256 / 384.
 #include "gs_attn.cuh"
@@ -41,13 +42,14 @@ constexpr int kAcThreads = 512;                // warps: keys, values, S x 2, P 
 constexpr int kRing = 5;                       // slots of keys, and as many of values
 constexpr int kSegs = 4;
 constexpr int kFlat = 6;                       // parts joined in one level (16 tokens at 60000 keys, 28/4 heads: 52 us; always one level: 95)
-constexpr int kJoin = 3;                       // of them under way at once
+constexpr int kJoin = 3;                       // of them under way at once (2 and 4: the same within 2 %)
 constexpr int kCheckers = 2;
 constexpr int kRegsOther = 56, kRegsSoftmax = 200;
 static_assert(8 * 32 * (kRegsOther + kRegsSoftmax) <= kAcThreads * 128, "register split");
 
-// kOver 0 / 5 / 8 / 12: prompts as above 275 / 231 / 221 / 230 us; a mixed step of 681 tokens 132 / 82 / 80 / 84.
-// kSnap 1 / 3 / 6: prompts 224 / 221 / 222, the mixed step 82 / 82 / 84.  kLeast 6 / 8 / 12: 30 tokens at 8192 keys
+// kOver 4 / 5 / 6 / 8: prompts as above 201 / 204 / 206 / 209 us, 6 x 1024 tokens of 32 heads 84 / 82 / 83 / 87, a mixed
+// step of 681 tokens 78 / 78 / 77 / 80; 0 (with longer ends: 275 against 231 at 5, the mixed step 132 against 82).
+// kSnap 1 / 3 / 6 (then): prompts 224 / 221 / 222, the mixed step 82 / 82 / 84.  kLeast 6 / 8 / 12: 30 tokens at 8192 keys
 // (28/4 heads) 39 / 34 / 36, 64 tokens 35 / 37 / 38.
 struct ChunkTraits {
   static constexpr int kLeast = 8, kSnap = 3, kOver = 5;

@@ -327,6 +327,23 @@ def test_strided_queries_scales_and_large_scores(gs):
         _attend(gs, new, kv, 6, 2, 128, 32, 98, qscale=qscale, scale=scale)
 
 
+@pytest.mark.parametrize("hq,hkv,d,page", [(7, 1, 128, 64), (2, 2, 64, 16)])
+@pytest.mark.parametrize("new,kv", [([1], [20011]), ([4], [9000]), ([9, 2], [16000, 3]), ([40], [8191]), ([300], [5000])])
+def test_one_sequence_in_many_parts(gs, hq, hkv, d, page, new, kv):
+    _attend(gs, new, kv, hq, hkv, d, page, seed=120)
+
+
+@pytest.mark.parametrize("new,kv", [([3], [70]), ([90], [400]), ([200, 2], [4000, 9])])
+def test_output_off_a_sector(gs, new, kv):
+    cache, table = ref.make_cache(gs, kv, 2, 128, 32, 130)
+    q = _rand((sum(new), 4, 128), 131)
+    b = gs.Batch(ref.offsets(new), ref.i32(kv), table, max(new))
+    room = torch.full((q.numel() + 16,), 7.0, device="cuda", dtype=torch.bfloat16)
+    out = room[8: 8 + q.numel()].view(q.shape)        # 16 bytes past a 32-byte boundary
+    assert torch.equal(gs.paged_attention(q, cache, b, out=out), gs.paged_attention(q, cache, b))
+    assert (room[:8] == 7).all() and (room[-8:] == 7).all()
+
+
 def test_tokens_of_no_sequence_and_more_tokens_than_told(gs):
     cache, table = ref.make_cache(gs, [40], 1, 64, 16, 99)
     q = _rand((5, 2, 64), 100)
