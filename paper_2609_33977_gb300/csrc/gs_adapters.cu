@@ -168,6 +168,7 @@ __global__ void __launch_bounds__(kAdThreads, ad_per_sm(NT, MT)) __cluster_dims_
   extern __shared__ __align__(16) uint8_t ad_smem[];
   constexpr int M = 16 * MT;
   cg::cluster_group cluster = cg::this_cluster();
+  start_of_work();
   const int c = (int)cluster.block_rank();
   const int u = (int)(blockIdx.x / CL);
   const AdLayer& L = P.layer[blockIdx.y];
@@ -326,9 +327,7 @@ gs_status ad_launch(const AdParams& P, int n, int rank, cudaStream_t s) {
   if (attr != cudaSuccess) return GS_ERR_CUDA;
   const int64_t units = P.T / M + P.n_seqs;
   if (units * CL > INT32_MAX) return GS_ERR_UNSUPPORTED;
-  k_adapters<NT, MT, CL><<<dim3((unsigned)(units * CL), (unsigned)n), kAdThreads, smem, s>>>(P);
-  note_launch();
-  return cudaGetLastError() == cudaSuccess ? GS_OK : GS_ERR_CUDA;
+  return launch_behind(k_adapters<NT, MT, CL>, dim3((unsigned)(units * CL), (unsigned)n), kAdThreads, smem, s, P);
 }
 
 // The largest cluster with which all tiles are resident at once: more CTAs a tile shorten

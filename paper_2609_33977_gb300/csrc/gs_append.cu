@@ -38,6 +38,7 @@ struct AppendParams {
 };
 
 __global__ void __launch_bounds__(kAppThreads) k_cache_append(const AppendParams P) {
+  start_of_work();
   const int64_t t = blockIdx.x / (unsigned)P.parts;
   const int per = P.head_dim / 16;   // threads of a head
   const int item = (int)(blockIdx.x % (unsigned)P.parts) * (int)blockDim.x + (int)threadIdx.x;
@@ -132,9 +133,7 @@ gs_status launch_cache_append(const gs_paged_cache& c, const gs_seq_batch& b, co
   const unsigned threads = (unsigned)((items + P.parts - 1) / P.parts + 31) / 32 * 32;
   const int64_t blocks = b.tokens * P.parts;
   if (blocks > INT32_MAX) return GS_ERR_UNSUPPORTED;
-  k_cache_append<<<(unsigned)blocks, threads, 0, s>>>(P);
-  note_launch();
-  return cudaGetLastError() == cudaSuccess ? GS_OK : GS_ERR_CUDA;
+  return launch_behind(k_cache_append, dim3((unsigned)blocks), threads, 0, s, P);
 }
 
 }  // namespace gs

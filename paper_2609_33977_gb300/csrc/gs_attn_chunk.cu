@@ -212,7 +212,6 @@ __global__ void __launch_bounds__(kAcThreads, 1) k_attn_chunk(const __grid_const
   uint8_t* ring_v = ring_k + kRing * C::kOpBytes;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int cta = (int)blockIdx.x;
-  if (P.two_launches) asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   if (threadIdx.x == 0) {
     for (int s = 0; s < kRing; ++s) {
       mbar_init(&kfull_bar[s], 1);
@@ -247,6 +246,8 @@ __global__ void __launch_bounds__(kAcThreads, 1) k_attn_chunk(const __grid_const
     tmem_alloc(&tmem_base_s, 512);
     tmem_relinquish();
   }
+  start_of_work();
+  if (P.two_launches) asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   const Shares shares = divide_work<ChunkTraits, kAcThreads>(P, cta, work);
   tc_fence_before();
   __syncthreads();
@@ -826,9 +827,7 @@ gs_status chunk_launch(const AttnParams& P, int ctas, cudaStream_t s) {
   static const cudaError_t attr =
       cudaFuncSetAttribute(k_attn_chunk<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, ChunkCfg<D>::kSmem);
   if (attr != cudaSuccess) return GS_ERR_CUDA;
-  k_attn_chunk<D><<<(unsigned)ctas, kAcThreads, ChunkCfg<D>::kSmem, s>>>(P);
-  note_launch();
-  return cudaGetLastError() == cudaSuccess ? GS_OK : GS_ERR_CUDA;
+  return launch_behind(k_attn_chunk<D>, dim3((unsigned)ctas), kAcThreads, ChunkCfg<D>::kSmem, s, P);
 }
 
 }  // namespace

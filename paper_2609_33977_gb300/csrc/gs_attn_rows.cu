@@ -151,6 +151,7 @@ __global__ void __launch_bounds__(RowsCfg<D, WR>::kThreads, 1) k_attn_rows(const
     prefetch_tmap(&P.kmap);
     prefetch_tmap(&P.vmap);
   }
+  if (!P.two_launches) start_of_work();   // else the chunk launch has waited, and lets this one begin after that
   const Shares shares = divide_work<FewTraits, C::kThreads>(P, cta, work);
   volatile int* abort_flag = &abort_s;
   const int chunk_shift = min(P.page_shift, 7), chunk = 1 << chunk_shift;   // rows of a TMA box
@@ -562,7 +563,7 @@ __global__ void __launch_bounds__(RowsCfg<D, WR>::kThreads, 1) k_attn_rows(const
   }
   __syncthreads();
   end_of_waits(abort_flag, P.err);
-  if (P.two_launches) asm volatile("griddepcontrol.wait;" ::: "memory");
+  if (P.two_launches) start_of_work();   // the chunk launch's end: what follows waits for this one only
 }
 
 template <int D, int WR>
@@ -570,19 +571,7 @@ gs_status rows_launch(const AttnParams& P, int ctas, cudaStream_t s) {
   using C = RowsCfg<D, WR>;
   static const cudaError_t attr = cudaFuncSetAttribute(k_attn_rows<D, WR>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::kSmem);
   if (attr != cudaSuccess) return GS_ERR_CUDA;
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)ctas);
-  cfg.blockDim = dim3(C::kThreads);
-  cfg.dynamicSmemBytes = C::kSmem;
-  cfg.stream = s;
-  cudaLaunchAttribute overlap;
-  overlap.id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  overlap.val.programmaticStreamSerializationAllowed = 1;
-  cfg.attrs = &overlap;
-  cfg.numAttrs = P.two_launches ? 1 : 0;
-  const cudaError_t e = cudaLaunchKernelEx(&cfg, k_attn_rows<D, WR>, P);
-  note_launch();
-  return e == cudaSuccess ? GS_OK : GS_ERR_CUDA;
+  return launch_behind(k_attn_rows<D, WR>, dim3((unsigned)ctas), C::kThreads, C::kSmem, s, P);
 }
 
 }  // namespace

@@ -35,6 +35,27 @@ inline int sm_count() {
   return n;
 }
 
+// These kernels are short and follow one another: each may be set up while the launch before it
+// drains, and begins by waiting for that one's end (start_of_work, by every thread, before
+// anything is read or written).
+template <class P>
+gs_status launch_behind(void (*kernel)(P), dim3 grid, unsigned threads, size_t smem, cudaStream_t s, const P& params) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = grid;
+  cfg.blockDim = dim3(threads);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = s;
+  cudaLaunchAttribute overlap;
+  overlap.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  overlap.val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = &overlap;
+  cfg.numAttrs = 1;
+  const cudaError_t e = cudaLaunchKernelEx(&cfg, kernel, params);
+  note_launch();
+  return e == cudaSuccess ? GS_OK : GS_ERR_CUDA;
+}
+__device__ __forceinline__ void start_of_work() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+
 // Number of entries i in [1, n] of a non-decreasing list with at[i] <= v, by a whole
 // block (any barrier-synchronised block size).  n is at least 1.
 __device__ __forceinline__ int block_count_le(const int32_t* __restrict__ at, int n, int v) {

@@ -65,6 +65,7 @@ struct NormParams {
 template <int V>
 __global__ void __launch_bounds__(1024) k_norm(const NormParams P) {
   __shared__ float red[32];
+  start_of_work();
   const int nv = P.n >> 3;
   const int64_t row = blockIdx.x;
   const uint4* xr = reinterpret_cast<const uint4*>(P.x + row * P.n);
@@ -142,6 +143,7 @@ __global__ void __launch_bounds__(1024) k_norm(const NormParams P) {
 // Any row length: one element per thread and step, the row read again for each pass.
 __global__ void __launch_bounds__(256) k_norm_any(const NormParams P) {
   __shared__ float red[32];
+  start_of_work();
   const int64_t row = blockIdx.x;
   const uint16_t* x = P.x + row * P.n;
   const uint16_t* r = P.res ? P.res + row * P.n : nullptr;
@@ -200,13 +202,9 @@ gs_status launch_add_rms_norm(const void* x, const void* res, const void* w, int
   if (n % 8 == 0 && nv <= 4096) {
     const int v = nv <= 512 || (nv <= 2048 && T <= sm_count()) ? 2 : 4;
     const unsigned threads = (unsigned)(((nv + v - 1) / v + 31) / 32 * 32);
-    if (v == 2) k_norm<2><<<(unsigned)T, threads, 0, s>>>(P);
-    else k_norm<4><<<(unsigned)T, threads, 0, s>>>(P);
-  } else {
-    k_norm_any<<<(unsigned)T, 256, 0, s>>>(P);
+    return launch_behind(v == 2 ? k_norm<2> : k_norm<4>, dim3((unsigned)T), threads, 0, s, P);
   }
-  note_launch();
-  return cudaGetLastError() == cudaSuccess ? GS_OK : GS_ERR_CUDA;
+  return launch_behind(k_norm_any, dim3((unsigned)T), 256, 0, s, P);
 }
 
 }  // namespace gs
