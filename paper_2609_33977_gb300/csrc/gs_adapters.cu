@@ -17,7 +17,7 @@
 // is the output's.  Loads are unconditional, at clamped addresses: one that depends on
 // a branch waits for the one before it.
 //
-// q, k and v of 16 sequences with an adapter each (4096x4096, rank 16): 7.4 us; 9 MB, so the
+// q, k and v of 16 sequences with an adapter each (4096x4096, rank 16): 7.2 us; 9 MB, so the
 // way of a tile through two products and two cluster barriers, not the bytes.  2048 tokens
 // through 4096x11008, rank 32: 27 us, 3.0 TB/s: the loads of one block of inputs wait for
 // the products of the one before, and two CTAs an SM do not hide all of it.

