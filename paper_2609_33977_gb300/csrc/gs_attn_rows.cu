@@ -24,7 +24,9 @@ constexpr int kTile = 128;
 constexpr int kMost = 32;      // rows
 constexpr int kPartPad = 8;    // floats of a row of a part beside the output's
 constexpr int kJoin = 8;   // rows of parts that a warp has under way when it joins them
-constexpr int kFlat = 16;  // parts joined in one level
+// Parts joined in one level: the three long sequences above take 53 us, 55 with at most 8, 4 tokens of 28/4 heads at 60000
+// keys 42 (always one level: 46).  More go in groups of at most sqrt(256).
+constexpr int kFlat = 16;
 static_assert(kFlat <= 32, "a lane a part");
 
 // One unit an item beside its keys: the 16 sequences above take 70 us, 82 without.  kLeast 1, 2, 4: no difference.
