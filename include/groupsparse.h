@@ -30,6 +30,9 @@
 #ifndef GROUPSPARSE_H
 #define GROUPSPARSE_H
 
+/* gs_paged_attention's workspace begins with its counters, so many bytes */
+#define GS_ATTENTION_COUNTER_BYTES 8192
+
 #include <stddef.h>
 #include <stdint.h>
 
@@ -506,14 +509,18 @@ gs_status gs_cache_append(const gs_paged_cache* cache, const gs_seq_batch* batch
  * q_dev  bf16 [tokens][q_heads][head_dim], tokens q_stride elements apart (a multiple of 8).
  * out_dev  bf16 [tokens][q_heads][head_dim], dense, fully overwritten.
  * scale  finite.
- * workspace_dev  gs_paged_attention_workspace bytes, 16-byte aligned, zero before its
- *         first use; calls leave the part zero that has to be, so it serves one call
- *         after another on one stream without being cleared.
+ * workspace_dev  gs_paged_attention_workspace bytes, 16-byte aligned, the first
+ *         GS_ATTENTION_COUNTER_BYTES of them zero before its first use; calls leave them
+ *         zero, so it serves one call after another on one stream without being cleared.
+ *         Calls that may run at the same time need one each.  A graph goes on using the
+ *         one that it was captured with: replays must be ordered with each other and with
+ *         every other use of it, whatever streams they run on.
  * max_new chooses the kernels; a sequence with more new tokens than it says may get
  * zeros.
  * The first call of a process makes the library's error flag, if gs_pack has not: not
  * inside a graph capture.
- * After GS_ERR_DEVICE_TIMEOUT the workspace has to be zeroed again.
+ * After GS_ERR_DEVICE_TIMEOUT the counters have to be zeroed again, those of captured
+ * graphs too (or a graph zeroes them itself, before its first call).
  * Errors: INVALID_ARG, UNSUPPORTED (page_size, head_dim, more than 64 query heads a key
  * head, tokens * q_heads / kv_heads of 10^9 and more, or more than 2 * 10^9 tiles of
  * 128 keys x 256 rows in the page tables), CUDA.
@@ -543,6 +550,10 @@ gs_status gs_paged_attention(const gs_paged_cache* cache, const gs_seq_batch* ba
  */
 gs_status gs_debug_fail_alloc(int64_t nth);
 gs_status gs_debug_inject_wait(gs_algo family, uint64_t limit_ns);
+
+/* gs_capture_id - *id tells the graph capture that `stream` is in from every other one
+ * of the process (0: none).  Errors: INVALID_ARG (id), CUDA. */
+gs_status gs_capture_id(void* stream, uint64_t* id);
 
 /* Number of kernel launches the library issued since the process started (all
  * families; used to report launch counts). */

@@ -663,6 +663,21 @@ gs_status gs_debug_inject_wait(gs_algo family, uint64_t limit_ns) {
   return GS_OK;
 }
 
+gs_status gs_capture_id(void* stream, uint64_t* id) {
+  if (!id) return GS_ERR_INVALID_ARG;
+  *id = 0;
+  const cudaStream_t s = static_cast<cudaStream_t>(stream);
+  if (s == nullptr || s == cudaStreamLegacy) return GS_OK;   // cannot be captured
+  cudaStreamCaptureStatus st = cudaStreamCaptureStatusNone;
+  unsigned long long v = 0;
+  if (cudaStreamGetCaptureInfo(s, &st, &v) != cudaSuccess) {
+    cudaGetLastError();
+    return GS_ERR_CUDA;
+  }
+  if (st == cudaStreamCaptureStatusActive) *id = v;
+  return GS_OK;
+}
+
 int64_t gs_launch_count(void) { return g_launches.load(std::memory_order_relaxed); }
 
 }  // extern "C"

@@ -10,7 +10,7 @@ namespace {
 // Arrival counters (two levels; two halves in the chunk kernel), then the parts of split
 // items, each kernel's its own: the two launches of a step overlap.
 constexpr int kMaxCtas = 256;
-constexpr int64_t kCounterBytes = 8192;
+constexpr int64_t kCounterBytes = GS_ATTENTION_COUNTER_BYTES;
 static_assert(kCounterBytes >= 6 * 4 * kMaxCtas, "six counters a CTA");
 
 int attention_ctas() { return std::min(sm_count(), kMaxCtas); }

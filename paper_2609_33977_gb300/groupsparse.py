@@ -19,6 +19,7 @@ LIB_PATH = _PKG / "libgroupsparse.so"
 
 GS_OK, GS_ERR_INVALID_ARG, GS_ERR_UNSUPPORTED, GS_ERR_OOM, GS_ERR_CUDA, GS_ERR_DEVICE_TIMEOUT = range(6)
 ALGO_AUTO, ALGO_DECODE, ALGO_PREFILL, ALGO_PREFILL_DENSE = 0, 1, 2, 3
+ATTENTION_COUNTER_BYTES = 8192   # GS_ATTENTION_COUNTER_BYTES
 
 _c_i64p = ctypes.POINTER(ctypes.c_int64)
 _c_i32p = ctypes.POINTER(ctypes.c_int32)
@@ -74,6 +75,7 @@ def _load(path: Path = LIB_PATH) -> ctypes.CDLL:
     lib.gs_cache_append.argtypes = [vp, vp, vp, i64, i32, vp, i64, vp, i64, vp, vp, i64, vp, vp]
     lib.gs_paged_attention_workspace.argtypes = [vp, vp, i32, ctypes.POINTER(ctypes.c_size_t)]
     lib.gs_paged_attention.argtypes = [vp, vp, vp, i64, i32, ctypes.c_float, vp, vp, ctypes.c_size_t, vp]
+    lib.gs_capture_id.argtypes = [vp, ctypes.POINTER(ctypes.c_uint64)]
     lib.gs_debug_fail_alloc.argtypes = [i64]
     lib.gs_debug_inject_wait.argtypes = [ctypes.c_int, ctypes.c_uint64]
     for fn in (lib.gs_pack, lib.gs_linear, lib.gs_linear_ex, lib.gs_linear_batched, lib.gs_unpack,
@@ -81,7 +83,7 @@ def _load(path: Path = LIB_PATH) -> ctypes.CDLL:
                lib.gs_preserved_rates, lib.gs_debug_fail_alloc, lib.gs_debug_inject_wait, lib.gs_pack_groups,
                lib.gs_packed_group_shape, lib.gs_gumbel_select, lib.gs_masked_linear_backward_workspace,
                lib.gs_masked_linear_backward, lib.gs_add_rms_norm, lib.gs_adapters_batched, lib.gs_cache_append,
-               lib.gs_paged_attention_workspace, lib.gs_paged_attention):
+               lib.gs_paged_attention_workspace, lib.gs_paged_attention, lib.gs_capture_id):
         fn.restype = ctypes.c_int
     return lib
 
@@ -186,6 +188,7 @@ def trim() -> None:
     """Give the device buffers kept from released handles back to the device (waits for it), and the
     attention's workspaces to torch's allocator."""
     _attention_ws.clear()
+    _captured_ws.clear()
     lib.gs_trim()
 
 
@@ -527,10 +530,27 @@ class PagedCache:
         self._ref = ctypes.addressof(self._c)
 
 
-# The attention's workspace, one per (device, stream) for all layers; calls leave it ready for the next.  A graph
-# goes on using the one it was captured with: those stay (_attention_ws_in_graphs).
+# The attention's workspace, one per (device, stream) for all layers; calls leave its counters ready for the next.
+# A graph has its own, of its memory pool: it may be replayed on any stream, beside calls on the one it was captured
+# on and beside other graphs.  Each replay begins by zeroing the counters, so nothing is left of one that gave up.
 _attention_ws: dict = {}
-_attention_ws_in_graphs: dict = {}
+_captured_ws: dict = {}       # (device, stream): (capture, workspace), held while that capture may still use it
+_foreign_ws: list = []        # of captures with no memory pool of torch's: in use as long as their graphs live
+
+
+def _new_workspace(need: int, device) -> torch.Tensor:
+    ws = torch.empty((need,), dtype=torch.uint8, device=device)
+    ws[:ATTENTION_COUNTER_BYTES].zero_()
+    return ws
+
+
+def _graph_owned(t: torch.Tensor) -> bool:
+    """Whether t lies in a graph's memory pool, which keeps the memory for the graph after t is gone."""
+    if torch.cuda.get_allocator_backend() != "native":
+        return False
+    at = t.data_ptr()
+    return any(s["address"] <= at < s["address"] + s["total_size"] and tuple(s["segment_pool_id"]) != (0, 0)
+               for s in torch.cuda.memory_snapshot())
 
 
 def _attention_workspace(need: int, device, stream: Optional[torch.cuda.Stream], sp: int) -> torch.Tensor:
@@ -538,14 +558,19 @@ def _attention_workspace(need: int, device, stream: Optional[torch.cuda.Stream],
         with torch.cuda.stream(stream):
             return _attention_workspace(need, device, None, sp)
     key = (device.index, sp)
-    ws = _attention_ws.get(key)
-    fits = ws is not None and ws.numel() >= need
     if torch.cuda.is_current_stream_capturing():
-        if not fits:               # the graph's own memory, zeroed in every replay
-            return torch.zeros((need,), dtype=torch.uint8, device=device)
-        _attention_ws_in_graphs[ws.data_ptr()] = ws
-    elif not fits:
-        ws = _attention_ws[key] = torch.zeros((need,), dtype=torch.uint8, device=device)
+        capture = ctypes.c_uint64()
+        _check(lib.gs_capture_id(sp, ctypes.byref(capture)), "gs_capture_id")
+        of, ws = _captured_ws.get(key, (0, None))
+        if of != capture.value or ws.numel() < need:
+            ws = _new_workspace(need, device)
+            if not _graph_owned(ws):
+                _foreign_ws.append(ws)
+            _captured_ws[key] = (capture.value, ws)
+        return ws
+    ws = _attention_ws.get(key)
+    if ws is None or ws.numel() < need:
+        ws = _attention_ws[key] = _new_workspace(need, device)
     return ws
 
 
@@ -623,7 +648,8 @@ def cache_append(cache: PagedCache, batch: Batch, q: torch.Tensor, k: torch.Tens
 def paged_attention(q: torch.Tensor, cache: PagedCache, batch: Batch, scale: Optional[float] = None,
                     out: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
     """Causal attention of a step's queries q [T, q_heads, D] over the cache (the step's own keys are in it already:
-    cache_append), bf16 [T, q_heads, D].  scale: 1 / sqrt(D) if not given.  A token without visible keys gets zeros."""
+    cache_append), bf16 [T, q_heads, D].  scale: 1 / sqrt(D) if not given.  A token without visible keys gets zeros.
+    Its workspace is the stream's, or the graph's where the stream is being captured."""
     D = cache.head_dim
     T, heads, qs = _heads(q, D, "q")
     if out is None:
@@ -650,7 +676,7 @@ def debug_inject_wait(algo: int, limit_ns: int) -> None:
 def device_status(stream: Optional[torch.cuda.Stream] = None) -> int:
     status = int(lib.gs_device_status(_stream_ptr(stream)))
     if status == GS_ERR_DEVICE_TIMEOUT:
-        _attention_ws.clear()      # counters of a kernel that gave up are not zero
+        _attention_ws.clear()      # counters of a kernel that gave up are not zero (graphs zero theirs)
     return status
 
 
