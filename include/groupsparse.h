@@ -546,10 +546,16 @@ gs_status gs_paged_attention(const gs_paged_cache* cache, const gs_seq_batch* ba
  * a library word that nothing ever sets, for at most limit_ns (<= 1 s).  The
  * wait runs out, the kernel records GS_ERR_DEVICE_TIMEOUT and that CTA skips
  * its work; the other CTAs finish theirs.  One-shot; limit_ns = 0 disarms.
+ *
+ * gs_debug_inject_attention_wait(chunk, limit_ns) - the same for the next launch of
+ * gs_paged_attention's kernel for few rows (chunk = 0) or for many (1): the warp that
+ * its first CTA's copies come from waits and gives up in their place, and the CTA's
+ * other warps leave their own waits for it.
  * Errors: INVALID_ARG (negative count, unknown family, limit above 1 s).
  */
 gs_status gs_debug_fail_alloc(int64_t nth);
 gs_status gs_debug_inject_wait(gs_algo family, uint64_t limit_ns);
+gs_status gs_debug_inject_attention_wait(int32_t chunk, uint64_t limit_ns);
 
 /* gs_capture_id - *id tells the graph capture that `stream` is in from every other one
  * of the process (0: none).  Errors: INVALID_ARG (id), CUDA. */

@@ -21,7 +21,7 @@ std::atomic<int64_t> g_launches{0};
 std::atomic<uint64_t> g_timeout_epoch{0};
 // test hooks: countdown to a failing allocation (0 = off), injected wait limits
 std::atomic<int64_t> g_fail_alloc_in{0};
-std::atomic<uint64_t> g_inject_ns[4] = {{0}, {0}, {0}, {0}};
+std::atomic<uint64_t> g_inject_ns[kInjectFamilies] = {};
 
 // Token count at and above which gs_linear uses the tensor-core kernels: one
 // decode launch covers up to 16 tokens, while the tensor-core kernels' time is
@@ -216,7 +216,7 @@ gs_status lib_malloc(void** ptr, size_t bytes) {
 }
 
 uint64_t take_injected_wait(int family) {
-  if (family < GS_ALGO_DECODE || family > GS_ALGO_PREFILL_DENSE) return 0;
+  if (family < GS_ALGO_DECODE || family >= kInjectFamilies) return 0;
   return g_inject_ns[family].exchange(0);
 }
 
@@ -675,6 +675,12 @@ gs_status gs_capture_id(void* stream, uint64_t* id) {
     return GS_ERR_CUDA;
   }
   if (st == cudaStreamCaptureStatusActive) *id = v;
+  return GS_OK;
+}
+
+gs_status gs_debug_inject_attention_wait(int32_t chunk, uint64_t limit_ns) {
+  if ((chunk != 0 && chunk != 1) || limit_ns > 1000000000ull) return GS_ERR_INVALID_ARG;
+  g_inject_ns[chunk ? kInjectAttnChunk : kInjectAttnRows].store(limit_ns);
   return GS_OK;
 }
 

@@ -95,6 +95,7 @@ gs_status launch_paged_attention(const gs_paged_cache& c, const gs_seq_batch& b,
     P.min_rows = k.few ? attn_rows_most() + 1 : 1;
     P.max_rows = INT32_MAX;
     P.zero_rest = !k.few;
+    P.inject_ns = take_injected_wait(kInjectAttnChunk);
     const gs_status st = launch_attn_chunk(P, c.head_dim, attention_ctas(), s);
     if (st != GS_OK || !k.few) return st;
   }
@@ -106,6 +107,7 @@ gs_status launch_paged_attention(const gs_paged_cache& c, const gs_seq_batch& b,
   P.min_rows = 1;
   P.max_rows = attn_rows_held((int)std::min((int64_t)b.max_new * P.group, (int64_t)attn_rows_most()));
   P.zero_rest = !k.chunk;
+  P.inject_ns = take_injected_wait(kInjectAttnRows);
   return launch_attn_rows(P, c.head_dim, attention_ctas(), s);
 }
 

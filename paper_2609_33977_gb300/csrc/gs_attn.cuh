@@ -30,6 +30,7 @@ struct AttnParams {
                             // split item, that begin in the CTA; zero between calls
   float* parts;             // [CTAs][2] parts
   int* err;
+  uint64_t inject_ns;       // test hook: CTA 0 waits so long on a word that nothing sets, in place of its copies (0: off)
   int64_t q_stride, tokens, pages;
   int32_t n_seqs, width, page_shift, q_heads, kv_heads, group;
   uint32_t group_inv;       // floor((2^32 - 1) / group)
@@ -108,6 +109,21 @@ __device__ __forceinline__ bool mbar_wait_warp(uint64_t* bar, uint32_t parity, v
     if (__any_sync(0xffffffffu, *abort_flag != 0)) return false;
   }
   return true;
+}
+// Test hook, for the warp that a CTA's work begins with: waits on a word that nothing sets (the one after the error
+// flag) until the limit, then gives up like every wait that runs out.
+__device__ __forceinline__ bool injected_timeout(const AttnParams& P, int cta, volatile int* abort_flag) {
+  if (P.inject_ns == 0 || cta != 0) return false;
+  const volatile int* never = P.err + 1;
+  const uint64_t t0 = sm100::globaltimer_ns();
+  bool out = false;
+  while (!out && *never == 0) {
+    out = sm100::globaltimer_ns() - t0 > P.inject_ns;
+    __nanosleep(1000);
+  }
+  out = __any_sync(0xffffffffu, out);
+  if (out) *abort_flag = 1;
+  return out;
 }
 // At a kernel's end, after a block barrier: records that some wait ran out, and gives
 // copies in flight time to land.

@@ -284,7 +284,7 @@ __global__ void __launch_bounds__(kAcThreads, 1) k_attn_chunk(const __grid_const
       uint64_t* empty_bar = keys ? kempty_bar : vempty_bar;
       uint8_t* ring = keys ? ring_k : ring_v;
       uint32_t slot = 0, ph = 1u, qph0 = 1u, qph1 = 1u;
-      bool ok = true;
+      bool ok = !keys || !injected_timeout(P, cta, abort_flag);
       while (ok) {
         if (keys) {
           const bool more = walk.next(g);

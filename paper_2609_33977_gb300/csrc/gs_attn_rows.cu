@@ -167,7 +167,7 @@ __global__ void __launch_bounds__(RowsCfg<D, WR>::kThreads, 1) k_attn_rows(const
     Segment g;
     const int32_t no_row = (int32_t)((P.pages * P.kv_heads) << P.page_shift);   // past the last: reads as zeros
     uint32_t st = 0, ph = 1u, qs = 0, qph = 1u;
-    bool ok = true;
+    bool ok = !injected_timeout(P, cta, abort_flag);
     while (ok && walk.next(g)) {
       const int len = g.s.len();
       const int64_t trow = (int64_t)g.r * P.width;

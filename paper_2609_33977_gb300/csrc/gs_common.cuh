@@ -153,7 +153,8 @@ cudaError_t device_malloc(void** ptr, size_t bytes);
 // Test hook: limit of a wait on the never-set word to inject into the next
 // launch of a kernel family (GS_ALGO_DECODE / GS_ALGO_PREFILL /
 // GS_ALGO_PREFILL_DENSE); 0 = none.
-// Reading it disarms it.
+// Reading it disarms it.  The attention kernels' hooks follow the algorithms'.
+constexpr int kInjectAttnRows = 4, kInjectAttnChunk = 5, kInjectFamilies = 6;
 uint64_t take_injected_wait(int family);
 
 // The k-th tile of owner b, or -1 when it has no more (TileList: gs_plan.cuh).

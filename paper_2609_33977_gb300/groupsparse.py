@@ -78,12 +78,14 @@ def _load(path: Path = LIB_PATH) -> ctypes.CDLL:
     lib.gs_capture_id.argtypes = [vp, ctypes.POINTER(ctypes.c_uint64)]
     lib.gs_debug_fail_alloc.argtypes = [i64]
     lib.gs_debug_inject_wait.argtypes = [ctypes.c_int, ctypes.c_uint64]
+    lib.gs_debug_inject_attention_wait.argtypes = [i32, ctypes.c_uint64]
     for fn in (lib.gs_pack, lib.gs_linear, lib.gs_linear_ex, lib.gs_linear_batched, lib.gs_unpack,
                lib.gs_packed_info, lib.gs_packed_export, lib.gs_device_status, lib.gs_select_groups,
                lib.gs_preserved_rates, lib.gs_debug_fail_alloc, lib.gs_debug_inject_wait, lib.gs_pack_groups,
                lib.gs_packed_group_shape, lib.gs_gumbel_select, lib.gs_masked_linear_backward_workspace,
                lib.gs_masked_linear_backward, lib.gs_add_rms_norm, lib.gs_adapters_batched, lib.gs_cache_append,
-               lib.gs_paged_attention_workspace, lib.gs_paged_attention, lib.gs_capture_id):
+               lib.gs_paged_attention_workspace, lib.gs_paged_attention, lib.gs_capture_id,
+               lib.gs_debug_inject_attention_wait):
         fn.restype = ctypes.c_int
     return lib
 
@@ -671,6 +673,11 @@ def debug_fail_alloc(nth: int) -> None:
 def debug_inject_wait(algo: int, limit_ns: int) -> None:
     """Test hook: the next launch of that kernel family times out on a word nothing sets."""
     _check(lib.gs_debug_inject_wait(int(algo), int(limit_ns)), "gs_debug_inject_wait")
+
+
+def debug_inject_attention_wait(chunk: bool, limit_ns: int) -> None:
+    """Test hook: the next launch of the attention's kernel for few (or many) rows times out on a word nothing sets."""
+    _check(lib.gs_debug_inject_attention_wait(int(bool(chunk)), int(limit_ns)), "gs_debug_inject_attention_wait")
 
 
 def device_status(stream: Optional[torch.cuda.Stream] = None) -> int:

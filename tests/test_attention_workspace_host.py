@@ -32,3 +32,9 @@ def test_a_timeout_drops_the_streams_workspaces(gs, monkeypatch):
     assert gs.device_status() == gs.GS_OK and gs._attention_ws
     monkeypatch.setattr(gs.lib, "gs_device_status", lambda s: 5)
     assert gs.device_status() == gs.GS_ERR_DEVICE_TIMEOUT and not gs._attention_ws
+
+
+def test_the_attentions_wait_hook_checks_its_arguments(gs):
+    f = gs.lib.gs_debug_inject_attention_wait
+    assert f(2, 1000) == 1 and f(-1, 1000) == 1 and f(0, 1_000_000_001) == 1
+    assert f(0, 0) == 0 and f(1, 0) == 0
