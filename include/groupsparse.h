@@ -406,7 +406,7 @@ gs_status gs_masked_linear_backward(const void* x_dev, const void* W_dev, const 
  * h_dev         bf16 [T][n] or NULL: the residual stream for the next call.  May
  *               be residual_dev or x_dev itself.
  * y_dev         bf16 [T][n] or NULL.  May be x_dev itself.
- * y8_dev        e4m3 [T][n] or NULL: y / scale, rounded to nearest even, with
+ * y8_dev        e4m3 [T][n] or NULL: the float32 y / scale, rounded to nearest even, with
  * scales_dev    float32 [T][ceil(n / group)] (group 0: [T]) and
  *               scale = max(max|y| / 448, 2^-126) over the group's columns.
  * group         0 (one scale a row) or 128; read with y8_dev only.
