@@ -437,6 +437,10 @@ typedef struct gs_adapter_layer {
  * and a = ids[i].  float32 sums, one rounding, at the output.  A sequence whose id is
  * outside [0, n_adapters) has no adapter: out = base.
  *
+ * Infinities and NaN follow the formula: of x they stay with their token, of B with
+ * their output (base + s inf (A x)), of A with the tokens of that adapter.  A rank that
+ * was padded with zeros makes the NaN of 0 inf where x has an infinity.
+ *
  * offsets_dev  int32 [n_seqs + 1], non-decreasing, from 0 to T: the tokens of each
  *              sequence (empty ones allowed).  Tokens that no sequence holds are not
  *              written.

@@ -59,11 +59,31 @@ __device__ __forceinline__ void mma16816(float (&d)[4], uint32_t a0, uint32_t a1
 // MMAs) for ranks in whole 32s, 4 (one MMA) in whole 16s, else 2 (half an MMA).
 __host__ __device__ constexpr int rank_elems(int rank) { return rank % 32 == 0 ? 8 : rank % 16 == 0 ? 4 : 2; }
 
+// Columns [col, col + 8) of a lane's 2 mt rows, some of whose sums t [mt][4][4] an infinite element of B made infinite or
+// NaN: hi and lo are two terms of one product, which may cancel then, or lo is 0.  Such sums are formed again in float32.
+__device__ __noinline__ void store_odd(const AdLayer& L, const float* t, const float* sax, const uint16_t* B, int64_t t0,
+                                       int nt, int rank, int col, int mt) {
+  const int g = (int)(threadIdx.x & 31) >> 2;
+#pragma unroll 1
+  for (int i = 0; i < 16 * mt; ++i) {
+    const int r = 16 * (i >> 4) + 8 * ((i >> 1) & 1) + g, o = col + 2 * ((i >> 2) & 3) + (i & 1);
+    if (r >= nt || o >= L.out_n) continue;
+    float s = t[i];
+    if (!isfinite(s)) {
+      s = 0.f;
+#pragma unroll 1
+      for (int k = 0; k < rank; ++k) s = fmaf(sax[r * rank + k], bf16_lo(__ldg(B + (int64_t)o * rank + k)), s);
+    }
+    const int64_t at = (t0 + r) * L.out_n + o;
+    L.out[at] = (uint16_t)pack_bf16(bf16_lo(L.base[at]) + s, 0.f);
+  }
+}
+
 // out columns [32 blk, 32 blk + 32) of the tile: lane (g, q) of a warp ends with
 // columns 8 q .. 8 q + 7 of rows g and g + 8 of each 16 tokens.
-// v: [m][step][hi, lo][lane] fragments of s A x.
+// v: [m][step][hi, lo][lane] fragments of s A x, sax: its [rows][rank] in float32.
 template <int MT, int E>
-__device__ __forceinline__ void expand(const AdLayer& L, const uint4* v, const uint16_t* B, int64_t t0, int nt, int rank,
+__device__ __forceinline__ void expand(const AdLayer& L, const uint4* v, const float* sax, const uint16_t* B, int64_t t0, int nt, int rank,
                                        int b0, int b1, int warp, int lane) {
   const int g = lane >> 2, q = lane & 3;
   const int steps = rank / (4 * E);
@@ -131,6 +151,19 @@ __device__ __forceinline__ void expand(const AdLayer& L, const uint4* v, const u
     for (int b = 0; b < kB; ++b) {
       const int col = 32 * (blk + b * kAdWarps) + 8 * q;
       if (blk + b * kAdWarps >= b1) break;   // not this CTA's
+      // an infinite element of B shows in every row of its column: hi times it is infinite, or NaN where hi is 0
+      float odd[2] = {0.f, 0.f};
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) odd[e] = fmaf(acc[b][0][j][e], 0.f, odd[e]);
+      if (odd[0] + odd[1] != 0.f) {
+        float t[MT * 16];
+#pragma unroll
+        for (int i = 0; i < MT * 16; ++i) t[i] = acc[b][i >> 4][(i >> 2) & 3][i & 3];
+        store_odd(L, t, sax, B, t0, nt, rank, col, MT);
+        continue;
+      }
 #pragma unroll
       for (int m = 0; m < MT; ++m)
 #pragma unroll
@@ -156,6 +189,7 @@ __device__ __forceinline__ void expand(const AdLayer& L, const uint4* v, const u
           }
         }
     }
+    __syncwarp();   // lanes may come from store_odd
   }
 }
 
@@ -311,9 +345,9 @@ __global__ void __launch_bounds__(kAdThreads, ad_per_sm(NT, MT)) __cluster_dims_
     dst[32] = make_uint4(lo[0], lo[1], lo[2], lo[3]);
   }
   __syncthreads();
-  if (E == 8) expand<MT, 8>(L, frag, B, t0, nt, rank, b0, b1, warp, lane);
-  else if (E == 4) expand<MT, 4>(L, frag, B, t0, nt, rank, b0, b1, warp, lane);
-  else expand<MT, 2>(L, frag, B, t0, nt, rank, b0, b1, warp, lane);
+  if (E == 8) expand<MT, 8>(L, frag, sum, B, t0, nt, rank, b0, b1, warp, lane);
+  else if (E == 4) expand<MT, 4>(L, frag, sum, B, t0, nt, rank, b0, b1, warp, lane);
+  else expand<MT, 2>(L, frag, sum, B, t0, nt, rank, b0, b1, warp, lane);
 }
 
 template <int NT, int MT, int CL>

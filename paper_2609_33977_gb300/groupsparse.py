@@ -461,7 +461,8 @@ def add_rms_norm_fp8(x: torch.Tensor, weight: torch.Tensor, residual: Optional[t
 
 class Adapters:
     """The low-rank adapters of one projection: A [n, rank, in], B [n, out, rank] (bf16) and scale [n] (float32,
-    alpha / rank).  Ranks that are no multiple of 8 are padded with zeros, once, here."""
+    alpha / rank).  Ranks that are no multiple of 8 are padded with zeros, once, here (an infinity in x
+    then gives NaN)."""
 
     def __init__(self, A: torch.Tensor, B: torch.Tensor, scale: torch.Tensor):
         for t, dt, name in ((A, torch.bfloat16, "A"), (B, torch.bfloat16, "B"), (scale, torch.float32, "scale")):
