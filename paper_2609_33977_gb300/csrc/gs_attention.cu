@@ -40,7 +40,8 @@ bool attention_units_fit(const gs_paged_cache& c, const gs_seq_batch& b, int32_t
   const double rows = (double)b.tokens * (q_heads / c.kv_heads), cap = (double)b.table_width * c.page_size;
   const double items = (rows / attn_chunk_rows() + b.n + 1.0) * c.kv_heads;
   const double units = items * (cap / std::min(attn_rows_tile(), attn_chunk_tile()) + 1.0 + attn_most_over());
-  return rows < 1e9 && units < 2e9;
+  // the key behind a sequence's last tile is still a number of 32 bits
+  return rows < 1e9 && units < 2e9 && cap <= 2147483648.0 - 256.0;
 }
 
 size_t attention_workspace_bytes(const gs_paged_cache& c, const gs_seq_batch& b, int32_t q_heads) {

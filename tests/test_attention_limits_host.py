@@ -34,3 +34,13 @@ def test_work_in_32_bits(gs, tokens, n, heads, kv_heads, page):
 def test_rows_below_a_thousand_million(gs):
     assert _status(gs, 10 ** 9 - 1, 1, 1, 1, 1) == 0
     assert _status(gs, 10 ** 9, 1, 1, 1, 1) == UNSUPPORTED
+
+
+@pytest.mark.parametrize("page", [16, 32, 64, 128, 256])
+@pytest.mark.parametrize("max_new", [1, 8])
+def test_keys_end_a_tile_short_of_32_bits(gs, page, max_new):
+    """The key that follows a sequence's last tile has a number of 32 bits too."""
+    most = (2 ** 31 - 256) // page
+    assert _status(gs, max_new, 1, most, 1, 1, page, max_new) == 0
+    if (most + 1) * page < 2 ** 31:
+        assert _status(gs, max_new, 1, most + 1, 1, 1, page, max_new) == UNSUPPORTED
