@@ -396,7 +396,8 @@ gs_status gs_masked_linear_backward(const void* x_dev, const void* W_dev, const 
 
 /*
  * gs_add_rms_norm - h = x + residual, y = h * rsqrt(mean(h^2) + eps) * w per row.
- * y is formed from the float32 h and rounded once.
+ * y is formed from the float32 h and rounded once; a row of finite h has finite norms,
+ * also where its squares leave float32's range.
  *
  * x_dev         bf16 [T][n].
  * residual_dev  bf16 [T][n], or NULL (h = x).

@@ -12,6 +12,8 @@
 // part that L2 still holds counts as read); one row of 4096 takes 1.8 us, a launch.
 #include "gs_block.cuh"
 
+#include <cfloat>
+
 namespace gs {
 namespace {
 
@@ -37,6 +39,16 @@ __device__ __forceinline__ float block_reduce(float v, float* red) {
   __syncthreads();
   v = lane < n ? red[lane] : 0.f;
   return kMax ? warp_max(v) : warp_sum(v);
+}
+
+// A mean square (eps in it) that float32 squares do not give: out of their range, or of magnitudes that they lose.
+__device__ __forceinline__ bool off_range(float ms) { return !(ms >= 0x1p-100f && ms <= FLT_MAX); }
+// Such a row is scaled first, by the power of two that brings the larger of its largest magnitude and eps' root near 1
+// (1: an infinite or empty row).  Rows of 1e20, say, whose squares are infinite, would be zeros otherwise.
+__device__ __forceinline__ float row_scale(float amax, float eps) {
+  const float top = fmaxf(amax, sqrtf(eps));
+  if (!(top > 0.f) || isinf(top)) return 1.f;
+  return __uint_as_float((uint32_t)max(1, 254 - (int)(__float_as_uint(top) >> 23)) << 23);
 }
 
 // four e4m3 codes, the first in the low byte (NaN stays NaN; the scale keeps the rest within 448)
@@ -79,9 +91,11 @@ struct NormParams {
   float eps;
 };
 
-// V vectors of 8 elements per thread; vector i of the row belongs to thread i % blockDim.x
+// V vectors of 8 elements per thread; vector i of the row belongs to thread i % blockDim.x.
+// Up to 1024 threads, so 64 registers at most; 56 with two vectors, or an SM holds four rows of 3584 instead of five
+// (777 of them: 5.1 us, 4.6 so).
 template <int V>
-__global__ void __launch_bounds__(1024) k_norm(const NormParams P) {
+__global__ void __maxnreg__(V == 2 ? 56 : 64) k_norm(const NormParams P) {
   __shared__ float red[32];
   start_of_work();
   const int nv = P.n >> 3;
@@ -115,8 +129,24 @@ __global__ void __launch_bounds__(1024) k_norm(const NormParams P) {
           make_uint4(pack_bf16(h[v][0], h[v][1]), pack_bf16(h[v][2], h[v][3]), pack_bf16(h[v][4], h[v][5]),
                      pack_bf16(h[v][6], h[v][7]));
   }
-  const float inv = rsqrtf(block_reduce<false>(ss, red) / (float)P.n + P.eps);
-  float amax = 0.f;
+  float ms = block_reduce<false>(ss, red) / (float)P.n + P.eps, amax = 0.f;
+  if (off_range(ms)) {   // the same for the whole block
+#pragma unroll
+    for (int v = 0; v < V; ++v)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) amax = fmaxf(amax, fabsf(h[v][e]));
+    const float s = row_scale(block_reduce<true>(amax, red), P.eps);
+    ss = amax = 0.f;
+#pragma unroll
+    for (int v = 0; v < V; ++v)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        h[v][e] *= s;
+        ss = fmaf(h[v][e], h[v][e], ss);
+      }
+    ms = block_reduce<false>(ss, red) / (float)P.n + P.eps * s * s;
+  }
+  const float inv = rsqrtf(ms);
 #pragma unroll
   for (int v = 0; v < V; ++v) {
     const uint32_t wx[4] = {w[v].x, w[v].y, w[v].z, w[v].w};
@@ -174,8 +204,20 @@ __global__ void __launch_bounds__(256) k_norm_any(const NormParams P) {
     const float h = at(i);
     ss = fmaf(h, h, ss);
   }
-  const float inv = rsqrtf(block_reduce<false>(ss, red) / (float)P.n + P.eps);
-  const auto out = [&](int i) { return at(i) * (inv * bf16_lo(P.w[i])); };
+  float ms = block_reduce<false>(ss, red) / (float)P.n + P.eps, s = 1.f;
+  if (off_range(ms)) {
+    float amax = 0.f;
+    for (int i = threadIdx.x; i < P.n; i += 256) amax = fmaxf(amax, fabsf(at(i)));
+    s = row_scale(block_reduce<true>(amax, red), P.eps);
+    ss = 0.f;
+    for (int i = threadIdx.x; i < P.n; i += 256) {
+      const float h = at(i) * s;
+      ss = fmaf(h, h, ss);
+    }
+    ms = block_reduce<false>(ss, red) / (float)P.n + P.eps * s * s;
+  }
+  const float inv = rsqrtf(ms);
+  const auto out = [&](int i) { return at(i) * s * (inv * bf16_lo(P.w[i])); };
   if (P.y8) {
     const int width = P.group ? P.group : P.n, ng = (P.n + width - 1) / width;
     for (int g = 0; g < ng; ++g) {
@@ -192,7 +234,7 @@ __global__ void __launch_bounds__(256) k_norm_any(const NormParams P) {
   // h may be the residual's own buffer and y the input's: every pass above is over
   __syncthreads();
   for (int i = threadIdx.x; i < P.n; i += 256) {
-    const float h = at(i), y = h * (inv * bf16_lo(P.w[i]));
+    const float h = at(i), y = h * s * (inv * bf16_lo(P.w[i]));
     if (P.h) P.h[row * P.n + i] = (uint16_t)pack_bf16(h, 0.f);
     if (P.y) P.y[row * P.n + i] = (uint16_t)pack_bf16(y, 0.f);
   }

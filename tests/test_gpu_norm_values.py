@@ -53,3 +53,36 @@ def test_codes_beside_an_infinity(gs, n):
     y8, sc, _ = gs.add_rms_norm_fp8(x, w)
     assert (sc == float("inf")).all() and y8[:, 3].float().isnan().all()
     assert (y8[:, :3].float() == 0).all() and (y8[:, 4:].float() == 0).all()
+
+
+@pytest.mark.parametrize("n", [8, 512, 515, 4096, 16384, 40000])
+@pytest.mark.parametrize("size,eps", [(1e20, 1e-5), (2.0 ** 126, 1e-5), (1e-21, 0.0), (1e-25, 1e-50), (1e-30, 1e-36), (1e-38, 0.0),
+                                      (3e18, 1e-5), (1e-20, 1e-5)])
+def test_rows_whose_squares_leave_the_range(gs, n, size, eps):
+    """Finite rows have finite norms, however large or small they are; ordinary rows beside them keep their bits."""
+    from tests import _block_ref as ref
+    g = torch.Generator(device="cuda").manual_seed(n)
+    rand = lambda *s: torch.randn(s, generator=g, device="cuda").clamp(-3.9, 3.9)  # noqa: E731
+    x, r, w = (rand(4, n) / 4).bfloat16(), (rand(4, n) / 4).bfloat16(), rand(n).bfloat16()
+    plain = gs.add_rms_norm(x, w, r, eps)[0]
+    x[1], r[1] = (x[1].double() * size).bfloat16(), (r[1].double() * size).bfloat16()
+    x[2, 0] = size                                # one element alone is out of range
+    y, h = gs.add_rms_norm(x, w, r, eps)
+    eps32 = float(torch.tensor(eps, dtype=torch.float32))
+    hr, yr = ref.norm(x, r, w, eps32)
+    assert yr.isfinite().all()
+    ref.assert_close(y, yr, yr.abs() * (ref.BF + n * 2.0 ** -24) + 1e-30, "y")
+    ref.assert_close(h, hr, hr.abs() * ref.BF + 2.0 ** -134, "h")
+    assert torch.equal(y[[0, 3]], plain[[0, 3]])
+    y8, sc, _ = gs.add_rms_norm_fp8(x, w, r, eps, 128)
+    want = torch.stack([yr[:, i: i + 128].abs().amax(1) for i in range(0, n, 128)], 1) / 448
+    ref.assert_close(sc, want.clamp(min=2.0 ** -126), want * (n * 2.0 ** -24 + 2.0 ** -20) + 1e-37, "scales")
+
+
+def test_empty_and_infinite_rows(gs):
+    for n in (512, 515):
+        x, w = torch.zeros((3, n), dtype=torch.bfloat16, device="cuda"), torch.ones((n,), dtype=torch.bfloat16, device="cuda")
+        x[1, 5], x[2, 7] = float("inf"), float("nan")
+        for eps in (1e-5, 1e-38):
+            y, _ = gs.add_rms_norm(x, w, None, eps)
+            assert (y[0] == 0).all() and y[1, 5].isnan() and (y[1, 6:] == 0).all() and y[2].isnan().all()
