@@ -527,9 +527,9 @@ gs_status gs_cache_append(const gs_paged_cache* cache, const gs_seq_batch* batch
  * After GS_ERR_DEVICE_TIMEOUT the counters have to be zeroed again, those of captured
  * graphs too (or a graph zeroes them itself, before its first call).
  * Errors: INVALID_ARG, UNSUPPORTED (page_size, head_dim, more than 64 query heads a key
- * head, table_width * page_size above 2^31 - 256, or more work than 32 bits count: with r = tokens * q_heads / kv_heads, r of 10^9
- * and more, or (r / 128 + n + 1) * kv_heads * (table_width * page_size / 64 + 6) of
- * 2 * 10^9 and more), CUDA.
+ * head, table_width * page_size above 2^31 - 256, or more work than 32 bits count: with
+ * r = tokens * q_heads / kv_heads, r of 10^9 and more, or (r / 128 + n + 1) * kv_heads *
+ * (table_width * page_size / 64 + 6) of 2 * 10^9 and more), CUDA.
  */
 gs_status gs_paged_attention_workspace(const gs_paged_cache* cache, const gs_seq_batch* batch, int32_t q_heads, size_t* bytes);
 gs_status gs_paged_attention(const gs_paged_cache* cache, const gs_seq_batch* batch, const void* q_dev, int64_t q_stride,

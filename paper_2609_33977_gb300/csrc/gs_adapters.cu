@@ -17,9 +17,9 @@
 // is the output's.  Loads are unconditional, at clamped addresses: one that depends on
 // a branch waits for the one before it.
 //
-// q, k and v of 16 sequences with an adapter each (4096x4096, rank 16): 7.2 us; 9 MB, so the
-// way of a tile through two products and two cluster barriers, not the bytes.  2048 tokens
-// through 4096x11008, rank 32: 27 us, 3.0 TB/s: the loads of one block of inputs wait for
+// q, k and v of 16 sequences with an adapter each (4096x4096, rank 16): 6.9 us, 10.1 with the
+// operands in HBM; 9 MB, so the way of a tile through two products and two cluster barriers,
+// not the bytes.  2048 tokens through 4096x11008, rank 32: 27 us, 3.0 TB/s: the loads of one block of inputs wait for
 // the products of the one before, and two CTAs an SM do not hide all of it.
 #include "gs_block.cuh"
 
@@ -308,7 +308,7 @@ __global__ void __launch_bounds__(kAdThreads, ad_per_sm(NT, MT)) __cluster_dims_
   cluster.sync();
   const float scale = __ldg(L.scale + id);
   {
-    // CTA c sums an eighth of the elements and gives them to every CTA
+    // CTA c sums its part of the elements and gives them to every CTA
     const int per = n / CL;   // n is a multiple of 128
     for (int i = c * per + (int)threadIdx.x; i < (c + 1) * per; i += kAdThreads) {
       float s = 0.f;
@@ -400,9 +400,9 @@ gs_status launch_adapters(const gs_adapter_layer* layers, int n, const int32_t* 
     rank = rank > L.rank ? rank : L.rank;
   }
   // 32 tokens a tile where the mean request has at least 64 (us at 16 / 32 a tile; 4096x11008 but where said otherwise):
-  //   rank 16 and 32    6 requests of 2048 tokens  30.4 / 21.5 and 35.4 / 27.3,  12 x 64 (4096x4096, rank 16)  9.0 / 8.5
-  //   below, rank 32    16 x 48 tokens  21.7 / 24.9,  8 x 32  9.2 / 10.1,  16 x 1 (q, k, v; rank 16)  7.4 / 8.9
-  //   rank 128          2048 tokens  99 / 74;  rank 64: 43.6 / 46.2, its sums leave no second CTA an SM: always 16
+  //   rank 16 and 32    6 requests of 2048 tokens  29.5 / 21.2 and 34.9 / 26.8,  12 x 64 (4096x4096, rank 16)  11.7 / 10.6
+  //   below, rank 32    16 x 48 tokens  19.7 / 24.1,  8 x 48  13.1 / 15.9,  8 x 32  12.9 / 14.6
+  //   rank 128          2048 tokens  101 / 77;  rank 64: 41.4 / 50.1, its sums leave no second CTA an SM: always 16
   // (64 a tile: 34 at rank 16, 53 at 32, 79 at 64.)
   const bool longer = T >= (int64_t)64 * n_seqs;
   if (rank <= 16) return longer ? ad_cluster<2, 2>(P, n, rank, s) : ad_cluster<2, 1>(P, n, rank, s);

@@ -18,13 +18,14 @@ int attention_ctas() { return std::min(sm_count(), kMaxCtas); }
 size_t parts_bytes(int size) { return (size_t)attention_ctas() * 2 * (size_t)size * 4; }
 
 // The few-row kernel serves sequences of at most attn_rows_most() = 32 rows, the chunk kernel
-// the others.  Us in the few-row / the chunk kernel, 128-wide heads: 32 rows  16 x 32 tokens at
-// 2000 keys (32 heads) 102 / 116,  28 rows  16 x 4 (28/4 heads) 29 / 34;  63 and 64 rows, in a
-// few-row form for them,  16 x 9 41 / 34,  16 x 64 156 / 117.
+// the others.  Us in the few-row / the chunk kernel, 128-wide heads: 7 rows  one token at 129
+// keys (28/4 heads) 6.9 / 10.0,  28 rows  16 x 4 tokens at 2000 keys 28.9 / 29.1,  32 rows
+// 16 x 32 (32 heads) 102.9 / 104.6;  above, in a few-row form for 64 rows and before the chunk
+// kernel's last steps,  16 x 9 41 / 34,  16 x 64 156 / 117.
 // Where all sequences are as long as the longest (known from the sizes alone), one launch does
-// (4096 tokens of 40 heads 162 us, both launches 165); otherwise the host cannot tell, and both
+// (4096 tokens of 40 heads 154 us, both launches 158); otherwise the host cannot tell, and both
 // kernels look for theirs, the second on SMs that the first is through with (a mixed step of
-// 681 tokens 84 us, one launch behind the other 89).
+// 681 tokens 77 us, one launch behind the other 80).
 struct Kernels {
   bool few, chunk;
 };

@@ -8,8 +8,8 @@
 // per row keeps the row in registers (8 elements = one 16-byte vector per thread
 // and step), so x and r are read once; sums are float32.  Rows whose length is no
 // multiple of 8, or above 32768, take k_norm_any, which reads them again per pass
-// (512 x 16384: 36 us against 10.6).  2047 x 5120 takes 10.8 us, 7.8 TB/s (the inputs'
-// part that L2 still holds counts as read); one row of 4096 takes 1.8 us, a launch.
+// (512 x 16384: 36 us against 12.2).  2047 x 5120 takes 13.7 us, 6.1 TB/s, in 8 bits 14.4
+// (5.1 TB/s); one row of 4096 takes 1.4 us, a launch.
 #include "gs_block.cuh"
 
 #include <cfloat>
@@ -257,7 +257,7 @@ gs_status launch_add_rms_norm(const void* x, const void* res, const void* w, int
   P.group = group;
   P.eps = eps;
   const int64_t nv = n / 8;
-  // Vectors a thread, us at 2 / 4: 2048 x 1024  3.1 / 3.5, 777 x 3584 in 8 bits  5.0 / 5.1, 1 x 8192  2.5 / 2.7,
+  // Vectors a thread, us at 2 / 4 (three sets of buffers, partly in L2): 2048 x 1024  3.1 / 3.5, 777 x 3584 in 8 bits  5.0 / 5.1, 1 x 8192  2.5 / 2.7,
   // 16 x 5120  2.2 / 2.5; 2047 x 5120  12.0 / 11.2, 1024 x 8192  11.0 / 9.9, 2048 x 11008  36.6 / 29.6.
   // (One a thread: 12.2, 11.7 and 36.6 for the last three, and 2 % more than two at 1 x 4096 to 777 x 3584.)
   if (n % 8 == 0 && nv <= 4096) {
