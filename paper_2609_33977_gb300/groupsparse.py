@@ -588,6 +588,8 @@ class Batch:
         n = kv_lens.numel()
         if offsets.shape != (n + 1,) or kv_lens.dim() != 1 or table.dim() != 2 or table.shape[0] != n:
             raise ValueError("offsets must be [n + 1], kv_lens [n] and table [n, width]")
+        if not 0 <= max_new < 2 ** 31:   # ctypes would keep its low 32 bits
+            raise ValueError(f"max_new must be in [0, 2^31), got {max_new}")
         self.offsets, self.kv_lens, self.table, self.max_new = offsets, kv_lens, table, int(max_new)
         self._c = _BatchStruct(offsets.data_ptr(), kv_lens.data_ptr(), table.data_ptr(), n, table.shape[1], 0, self.max_new)
         self._ref = ctypes.addressof(self._c)

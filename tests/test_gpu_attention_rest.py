@@ -82,3 +82,9 @@ def test_append_and_adapters_leave_tokens_of_no_sequence(gs):
     assert (y[:2] == 7).all() and (y[7:] == 7).all() and torch.equal(y[5:7], base[5:7])
     want, bound = ref.adapters(x[2:7], base[2:7], ad.A, ad.B, ad.scale, [3, 2], [1, -1])
     ref.assert_close(y[2:7], want, bound)
+
+
+def test_a_batch_refuses_more_new_tokens_than_32_bits(gs):
+    for bad in (2 ** 32 + 1, 2 ** 31, -1):
+        with pytest.raises(ValueError, match="max_new"):
+            gs.Batch(ref.offsets([1]), ref.i32([5]), ref.i32([[0]]), bad)
