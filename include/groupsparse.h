@@ -590,10 +590,13 @@ gs_status gs_cache_read_fp8(const gs_paged_cache_fp8* cache, const gs_seq_batch*
 
 /*
  * gs_paged_attention_fp8 - gs_paged_attention over a cache in 8 bits: the same formula on
- * the values that the codes stand for.  float32 scores, sums and softmax.  A key or value
- * that is NaN reaches the tokens that see it, and no others.  Memory past a sequence's
- * length may hold anything; codes of NaN (0x7f, 0xff) at positions of a sequence, which
- * gs_cache_append_fp8 does not write, may reach any token of it.
+ * the values that the codes stand for.  float32 scores, sums and softmax.  For the second
+ * product the weights are rounded to bf16, or, for sequences of few rows (new tokens x
+ * query heads a key head; 32, or 64 where sequences x key heads are few), weights times
+ * their values' scales s to f16: 11 bits of each, or steps of 2^-30 of the row's largest
+ * weight times scale.  A key or value that is NaN reaches the tokens that see it, and no
+ * others.  Memory past a sequence's length may hold anything; codes of NaN (0x7f, 0xff) at
+ * positions of a sequence, which gs_cache_append_fp8 does not write, may reach any token of it.
  * Arguments, workspace (of its own workspace call), captured graphs and errors as there.
  */
 gs_status gs_paged_attention_fp8_workspace(const gs_paged_cache_fp8* cache, const gs_seq_batch* batch, int32_t q_heads,

@@ -5,15 +5,17 @@
 // arithmetic counts twice as much.  Keys are the long side of both products (m16n8k16 with
 // 16 keys, then 16 channels, as its rows and 8 query rows as its columns), so up to 8 rows
 // cost half the instructions that 16 do:
-//     S^T = K Q^T,   p = exp2(c S - m),   O^T = V^T P^T.
+//     S^T = K Q^T,   l = sum exp2(c S - m),   O^T = V^T P^T,   P = exp2(c S + e - M + 6).
 // Codes become f16 on their way into the fragments (exactly), two at a time; a key's power
-// multiplies its scores, a value's power its weights, in float32.  Queries are moved to f16
-// by a power of two a row.  The maximum m in use is raised only when a score passes it by 8
-// (a vote instead of an exchange between the lanes that hold a row's keys), so that weights are
-// up to 2^8, and l at least 1.  Weights enter the second product with 11 bits, times their
-// values' powers, counted from the largest power so far that the row sees (2^-6 of it is one): what
-// they lose is 2^-12 of themselves or 2^-31 of that largest power.  A value of no visible key has weight 0
-// whatever its power, so a NaN stays with the rows that see it.
+// multiplies its scores in float32.  Queries are moved to f16 by a power of two a row.
+// The power 2^e of a value is added to the exponent of its weight, and the numerators have a
+// running maximum M of their own beside the softmax's m: the largest of weight times power
+// is what P in f16 is counted from, not the largest power, whose key may weigh nothing.  P keeps
+// 11 bits: it loses 2^-11 of itself at most, or, below 2^-20 of that largest one, 2^-31 of it.  O's
+// unit 2^M goes with its part as an exponent, and is applied after the division by l, so that
+// no sum leaves float32's range.  The maxima in use are raised only when a weight or a numerator
+// passes 2^8 (a vote instead of an exchange between the lanes that hold a row's keys), so l is at least 1.
+// A value of no visible key has weight 0 whatever its power, so a NaN stays with the rows that see it.
 //
 // A unit is 256 keys of a key head, 64 for each of four pairs of computing warps, and a pair
 // has a fetching warp and a ring of its own (TMA, a box a page and operand; 192 KB in all):
@@ -24,9 +26,8 @@
 //
 // 16 sequences of 90 to 4000 keys, 32 heads: 43.6 us, 4.9 TB/s (nothing computed 40.3, and parts of split items not joined
 // 36.7).  Three of 30001 to 65536 keys, 28/4 heads: 34.0 us, 4.4 TB/s; one of 60000: 23.4; four tokens there 38.4.  One of
-// 129 keys: 6.6 us.  24 of 2 to 16000 keys with 2 to 4 new tokens, 16/2 heads of 64: 20.4 us.  (Largest powers of all
-// rows together, which a value that a row does not see could then take bits from: 42.8, 34.0, 36.6 and 19.6.)  With 16 rows as the products' rows
-// instead, and one ring for all warps, the first three took 59.9, 40.8 and (129 keys) 7.8.
+// 129 keys: 6.6 us.  24 of 2 to 16000 keys with 2 to 4 new tokens, 16/2 heads of 64: 20.4 us.   With 16 rows as the
+// products' rows instead, and one ring for all warps, the first three took 59.9, 40.8 and (129 keys) 7.8.
 #include "gs_attn_rows.cuh"
 
 #include <algorithm>
@@ -95,9 +96,27 @@ __device__ __forceinline__ uint32_t transposed(uint32_t v) {
   asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(v));
   return r;
 }
-// 2^(exponent field - 127); 0 below the field's range
-__device__ __forceinline__ float power_of(int field) { return __uint_as_float((uint32_t)max(field, 0) << 23); }
+// 2^(exponent field - 127)
+__device__ __forceinline__ float power_of(int field) { return __uint_as_float((uint32_t)field << 23); }
 __device__ __forceinline__ float power_or_nan(uint32_t code) { return __uint_as_float(code == 255u ? 0x7FC00000u : code << 23); }
+// log2 of a power of two (-inf of 0)
+__device__ __forceinline__ float lg2(float x) {
+  float y;
+  asm("lg2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+// the larger of each half, numbers before NaN
+__device__ __forceinline__ uint32_t max_f16x2(uint32_t a, uint32_t b) {
+  uint32_t r;
+  asm("max.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+  return r;
+}
+// What O's sums are multiplied by, one after the other: 1 / l and half of the unit's exponent, then the other half.  (At once
+// 2^(M - m) may leave float32's range where the result does not.)  M is -inf where no value has a power: O is 0, or NaN.
+__device__ __forceinline__ float2 back_from(float m, float l, float M, bool seen) {
+  const float f = M == -INFINITY ? 0.f : ex2(0.5f * (M - m) - 3.f);
+  return seen ? make_float2(f / l, f) : make_float2(0.f, 0.f);
+}
 __device__ __forceinline__ void arrive_by(uint64_t* bar, uint32_t count) {
   asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0], %1;" ::"r"(smem_u32(bar)), "r"(count) : "memory");
 }
@@ -160,7 +179,7 @@ __device__ __forceinline__ void join_late(const AttnParams& P, const Segment* la
     // A row is one of 8, 16 or all lanes', so that a warp's rows take their steps together; parts come in chunks that fit.
     const int width = rows > 2 * WARPS ? 8 : rows > WARPS ? 16 : 32, l = lane & (width - 1), mine = lane / width;
     const int chunk = kChunk * (width / 8);
-    float4* mls = reinterpret_cast<float4*>(room) + mine * kFlatFp8;   // maximum and sum of every part
+    float4* mls = reinterpret_cast<float4*>(room) + mine * kFlatFp8;   // m, l and M of every part
     float4* os = reinterpret_cast<float4*>(room + kMlBytes) + mine * chunk * kPieces;
 #pragma unroll 1
     for (int at = warp + WARPS * mine; at - WARPS * mine < rows; at += WARPS * (32 / width)) {
@@ -170,7 +189,7 @@ __device__ __forceinline__ void join_late(const AttnParams& P, const Segment* la
       const int n_parts = at < rows && j.n > 1 ? j.n : 0;
       const auto part_at = [&](int i) { return part_slot(P, g.first_cta, j.first + i * j.stride, kPart); };
       for (int i = l; i < n_parts; i += width) copy16_l2(mls + i, part_at(i) + ROWS * D + kPartPad * row);
-      float mm = -INFINITY, ll = 0.f;
+      float mm = -INFINITY, ll = 0.f, top = -INFINITY;
       float4 a[D / 32];
 #pragma unroll
       for (int c = 0; c < D / 32; ++c) a[c] = make_float4(0.f, 0.f, 0.f, 0.f);
@@ -185,15 +204,19 @@ __device__ __forceinline__ void join_late(const AttnParams& P, const Segment* la
             if (l + width * c < kPieces) copy16_l2(os + i * kPieces + l + width * c, src + l + width * c);
         }
         asm volatile("cp.async.wait_all;" ::: "memory");
-        if (c0 == 0) {   // a lane a part: its factor, and its sum times that, in its maximum's and sum's place
+        if (c0 == 0) {   // a lane a part: the factor of its O, and its l times the other one, in its maximum's and sum's place
 #pragma unroll 1
-          for (int i = l; i < n_parts; i += width) mm = fmaxf(mm, mls[i].x);
+          for (int i = l; i < n_parts; i += width) mm = fmaxf(mm, mls[i].x), top = fmaxf(top, mls[i].z);
 #pragma unroll 1
-          for (int d = width / 2; d > 0; d >>= 1) mm = fmaxf(mm, __shfl_xor_sync(0xffffffffu, mm, d));
+          for (int d = width / 2; d > 0; d >>= 1) {
+            mm = fmaxf(mm, __shfl_xor_sync(0xffffffffu, mm, d));
+            top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
+          }
 #pragma unroll 1
           for (int i = l; i < n_parts; i += width) {
-            const float f = ex2(mls[i].x - (mm == -INFINITY ? 0.f : mm));
-            *reinterpret_cast<float2*>(mls + i) = make_float2(f, mls[i].y * f);
+            const float4 x = mls[i];
+            *reinterpret_cast<float2*>(mls + i) =
+                make_float2(ex2(x.z - (top == -INFINITY ? 0.f : top)), x.y * ex2(x.x - (mm == -INFINITY ? 0.f : mm)));
           }
         }
         __syncwarp();
@@ -213,7 +236,7 @@ __device__ __forceinline__ void join_late(const AttnParams& P, const Segment* la
       }
       if (n_parts == 0) continue;
       const int tok = row_token(P, row0<kTwo>(g) + row), hd = row0<kTwo>(g) + row - tok * P.group;
-      const float inv = g.s.seen(tok) > 0 ? 1.f / ll : 0.f;
+      const float2 back = back_from(mm, ll, top, g.s.seen(tok) > 0);
       float* slot = part_at(0);
 #pragma unroll
       for (int c = 0; c < D / 32; ++c) {
@@ -223,9 +246,9 @@ __device__ __forceinline__ void join_late(const AttnParams& P, const Segment* la
           reinterpret_cast<float4*>(slot + row * D)[piece] = a[c];
         else
           reinterpret_cast<uint2*>(P.out + ((int64_t)(g.s.tok0 + tok) * P.q_heads + g.h * P.group + hd) * D)[piece] =
-              make_uint2(pack_bf16(a[c].x * inv, a[c].y * inv), pack_bf16(a[c].z * inv, a[c].w * inv));
+              make_uint2(pack_bf16(a[c].x * back.x * back.y, a[c].y * back.x * back.y), pack_bf16(a[c].z * back.x * back.y, a[c].w * back.x * back.y));
       }
-      if (!j.last && l == 0) *reinterpret_cast<float4*>(slot + ROWS * D + kPartPad * row) = make_float4(mm, ll, 0.f, 0.f);
+      if (!j.last && l == 0) *reinterpret_cast<float4*>(slot + ROWS * D + kPartPad * row) = make_float4(mm, ll, top, 0.f);
     }
     on[0] = on[0] && !j0.last;
     on[1] = on[1] && !j1.last;
@@ -264,6 +287,7 @@ __global__ void __launch_bounds__(RowsCfg<D>::kThreads, 1) k_attn_rows_fp8(const
   __shared__ Segment segs[kPairs][S];    // of the slot, where it is its segment's first; r < 0: the end
   __shared__ WorkShared work;
   __shared__ float2 join_ml[2][W * 16];  // [warp][its rows]: maximum and sum
+  __shared__ float join_top[2][W * 16];  // the numerators' maximum
   __shared__ Segment late[2];            // split items' segments of this CTA, joined at its end
   __shared__ int abort_s, last_s[2];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(af_smem_raw) + 1023) & ~uintptr_t(1023));
@@ -455,19 +479,19 @@ __global__ void __launch_bounds__(RowsCfg<D>::kThreads, 1) k_attn_rows_fp8(const
       }
       const int all_see = g.s.seen(0);                 // keys below this are visible to every row
       float o[D / 16][NT][4];                          // channels 16 j + 2 gq (and + 1: the last two), rows 8 n + 2 qd, + 1
-      float m[NT][2], l[NT][2];
+      float m[NT][2], l[NT][2], M[NT][2];
+      float r[NT][2] = {}, more[NT][2];                // 2^(6 - (M - m)); a step's part of l
+      float limit = 0.f;                               // the largest power that a weight times r may meet
+      bool unset = true;                               // some row that sees keys has no M yet
 #pragma unroll
       for (int n = 0; n < NT; ++n) {
 #pragma unroll
-        for (int e = 0; e < 2; ++e) m[n][e] = -INFINITY, l[n][e] = 0.f;
+        for (int e = 0; e < 2; ++e) m[n][e] = M[n][e] = -INFINITY, l[n][e] = 0.f;
 #pragma unroll
         for (int j = 0; j < D / 16; ++j)
 #pragma unroll
           for (int e = 0; e < 4; ++e) o[j][n][e] = 0.f;
       }
-      // The largest power among the values so far that the row sees (its field): one for all rows until keys come that not all of
-      // them see, then a row's own, v_top + own.  o counts in 2^-6 of it.
-      int v_top = 0, own[NT][2] = {};
       for (int t = g.ta; t < g.tb; ++t) {
         if (t > g.ta) {
           // the slot before goes back; the segment's last one is kept for the join
@@ -487,7 +511,6 @@ __global__ void __launch_bounds__(RowsCfg<D>::kThreads, 1) k_attn_rows_fp8(const
           if (key0 >= len) break;                                        // uniform over the warp
           const bool masked = key0 + kSub > all_see;
           const uint8_t* pw = powers_at(pair, st) + at;
-          const uint32_t mine = pw[kSlotKeys + (lane & (kSub - 1))];     // a lane a value's power
           uint32_t kp[MT][2], vp[MT][2];                                 // powers of keys and values 16 i + gq, + 8
 #pragma unroll
           for (int i = 0; i < MT; ++i)
@@ -513,42 +536,20 @@ __global__ void __launch_bounds__(RowsCfg<D>::kThreads, 1) k_attn_rows_fp8(const
                 for (int n = 0; n < NT; ++n) mma16816(s[i][n], a, qf[2 * c + b][n][0], qf[2 * c + b][n][1]);
               }
             }
-          float shift = 1.f;
-          if (!masked) {
-            const int v_new = max(v_top, (int)__reduce_max_sync(0xffffffffu, mine != 255u ? mine : 0u));
-            shift = power_of(127 + v_top - v_new);
-            v_top = v_new;
-          } else {
+          float vw[MT][2];   // powers of values
+          float most = -INFINITY;
 #pragma unroll
-            for (int n = 0; n < NT; ++n)
+          for (int i = 0; i < MT; ++i)
 #pragma unroll
-              for (int e = 0; e < 2; ++e) {
-                int more = own[n][e];
+            for (int b = 0; b < 2; ++b) {
+              const float power = power_or_nan(kp[i][b]);
+              vw[i][b] = power_or_nan(vp[i][b]);
+              most = fmaxf(most, vw[i][b]);
 #pragma unroll
-                for (int i = 0; i < MT; ++i)
+              for (int n = 0; n < NT; ++n)
 #pragma unroll
-                  for (int b = 0; b < 2; ++b)
-                    if (key0 + 16 * i + 8 * b + gq < seen[n][e] && vp[i][b] != 255u) more = max(more, (int)vp[i][b] - v_top);
-#pragma unroll
-                for (int d = 4; d < 32; d <<= 1) more = max(more, __shfl_xor_sync(0xffffffffu, more, d));
-                if (more > own[n][e]) {
-                  const float f = power_of(127 + own[n][e] - more);
-#pragma unroll
-                  for (int j = 0; j < D / 16; ++j) o[j][n][e] *= f, o[j][n][2 + e] *= f;
-                  own[n][e] = more;
-                }
-              }
-          }
-          bool rise = false;
-          float top[NT][2];
-#pragma unroll
-          for (int n = 0; n < NT; ++n)
-#pragma unroll
-            for (int e = 0; e < 2; ++e)
-#pragma unroll
-              for (int i = 0; i < MT; ++i)
-#pragma unroll
-                for (int b = 0; b < 2; ++b) s[i][n][2 * b + e] *= power_or_nan(kp[i][b]) * unit[n][e];
+                for (int e = 0; e < 2; ++e) s[i][n][2 * b + e] *= power * unit[n][e];
+            }
           if (masked) {
 #pragma unroll
             for (int n = 0; n < NT; ++n)
@@ -560,76 +561,88 @@ __global__ void __launch_bounds__(RowsCfg<D>::kThreads, 1) k_attn_rows_fp8(const
                   for (int b = 0; b < 2; ++b)
                     if (key0 + 16 * i + 8 * b + gq >= seen[n][e]) s[i][n][2 * b + e] = -INFINITY;
           }
+          // Numerators: a weight times r times its value's power, where every row sees every key, none has passed a maximum in use by
+          // more than 2^8 (they count in 2^-6), and weights below float32's range are nothing beside the largest numerator
+          // whatever the power.  Otherwise (redo) the maxima are raised, and numerators are formed from exponents.  (Always so,
+          // in one loop: 16 x 32 tokens 107 us, 104 thus; by the scores' maxima instead of the results: 111.)
+          uint32_t p16[MT][NT][2];   // of two rows, keys 16 i + 8 b + gq
+          bool redo = unset || masked;
+          if (!redo) {
+            bool above = most > limit;
 #pragma unroll
-          for (int n = 0; n < NT; ++n)
-#pragma unroll
-            for (int e = 0; e < 2; ++e) {
-              top[n][e] = -INFINITY;
-#pragma unroll
-              for (int i = 0; i < MT; ++i)
-#pragma unroll
-                for (int b = 0; b < 2; ++b) top[n][e] = fmaxf(top[n][e], s[i][n][2 * b + e]);
-              rise |= seen[n][e] > 0 && top[n][e] > m[n][e] + 8.f;   // rows that are none have no say: theirs are any numbers
-            }
-          if (__any_sync(0xffffffffu, rise) || shift != 1.f) {
-#pragma unroll
-            for (int n = 0; n < NT; ++n)
-#pragma unroll
-              for (int e = 0; e < 2; ++e) {
-                const float mn = fmaxf(m[n][e], keys_max(top[n][e]));
-                const float fm = mn == m[n][e] ? 1.f : ex2(m[n][e] - mn);   // m = -inf: 0
-                m[n][e] = mn;
-                l[n][e] *= fm;
-#pragma unroll
-                for (int j = 0; j < D / 16; ++j) o[j][n][e] *= fm * shift, o[j][n][2 + e] *= fm * shift;
-              }
-          }
-#pragma unroll
-          for (int n = 0; n < NT; ++n)
-#pragma unroll
-            for (int e = 0; e < 2; ++e) {
-              const float base = m[n][e] == -INFINITY ? 0.f : m[n][e];
-              float sum = 0.f;
+            for (int n = 0; n < NT; ++n) {
+              float sum[2] = {0.f, 0.f};
+              uint32_t top = 0;
 #pragma unroll
               for (int i = 0; i < MT; ++i)
 #pragma unroll
                 for (int b = 0; b < 2; ++b) {
-                  const float w = ex2(s[i][n][2 * b + e] - base);
-                  sum += w;
-                  s[i][n][2 * b + e] = w;
+                  const float w0 = ex2(s[i][n][2 * b] - m[n][0]), w1 = ex2(s[i][n][2 * b + 1] - m[n][1]);
+                  sum[0] += w0, sum[1] += w1;
+                  p16[i][n][b] = pack_f16(w0 * r[n][0] * vw[i][b], w1 * r[n][1] * vw[i][b]);
+                  top = max_f16x2(top, p16[i][n][b]);
                 }
-              l[n][e] += sum;
+              // rows that are none have no say: theirs are any numbers
+              above |= seen[n][0] > 0 && (sum[0] > 256.f || (top & 0xFFFFu) > 0x7400u);
+              above |= seen[n][1] > 0 && (sum[1] > 256.f || (top >> 16) > 0x7400u);
+              more[n][0] = sum[0], more[n][1] = sum[1];
             }
-          // times the value's power, from the largest one; the sums are of weights alone
-          if (!masked) {
+            redo = __any_sync(0xffffffffu, above);
+          }
+          if (redo) {
+            unset = false;
+            limit = INFINITY;
 #pragma unroll
-            for (int i = 0; i < MT; ++i)
+            for (int n = 0; n < NT; ++n) {
+              float base[2], base_o[2], so[MT][2][2];
 #pragma unroll
-              for (int b = 0; b < 2; ++b) {
-                const float x = vp[i][b] == 255u ? __uint_as_float(0x7FC00000u) : power_of((int)vp[i][b] - v_top + 133);
-#pragma unroll
-                for (int n = 0; n < NT; ++n) s[i][n][2 * b] *= x, s[i][n][2 * b + 1] *= x;
-              }
-          } else {   // a value that the row does not see has no weight, whatever its power
-#pragma unroll
-            for (int n = 0; n < NT; ++n)
-#pragma unroll
-              for (int e = 0; e < 2; ++e)
+              for (int e = 0; e < 2; ++e) {
+                float top = -INFINITY, top_o = -INFINITY;
 #pragma unroll
                 for (int i = 0; i < MT; ++i)
 #pragma unroll
                   for (int b = 0; b < 2; ++b) {
-                    const float x = vp[i][b] == 255u ? __uint_as_float(0x7FC00000u) : power_of((int)vp[i][b] - v_top - own[n][e] + 133);
-                    s[i][n][2 * b + e] = key0 + 16 * i + 8 * b + gq >= seen[n][e] ? 0.f : s[i][n][2 * b + e] * x;
+                    // a value that the row does not see has no weight, whatever its power
+                    const bool none = masked && key0 + 16 * i + 8 * b + gq >= seen[n][e];
+                    so[i][b][e] = none ? -INFINITY : s[i][n][2 * b + e] + lg2(vw[i][b]);
+                    top = fmaxf(top, s[i][n][2 * b + e]), top_o = fmaxf(top_o, so[i][b][e]);
                   }
+                const float mn = fmaxf(m[n][e], keys_max(top)), Mn = fmaxf(M[n][e], keys_max(top_o));
+                l[n][e] *= mn == m[n][e] ? 1.f : ex2(m[n][e] - mn);   // m = -inf: 0
+                const float f = Mn == M[n][e] ? 1.f : ex2(M[n][e] - Mn);
+                m[n][e] = mn;
+                M[n][e] = Mn;
+                base[e] = mn == -INFINITY ? 0.f : mn, base_o[e] = Mn == -INFINITY ? 0.f : Mn - 6.f;
+                if (seen[n][e] > key0) {   // there is something to see from here on
+                  const float d = Mn - mn;
+                  r[n][e] = ex2(6.f - d);
+                  unset |= Mn == -INFINITY;   // no value with a power yet, or none that is a number
+                  limit = fminf(limit, d < -100.f ? -1.f : ex2(fminf(d + 90.f, 120.f)));
+                }
+#pragma unroll
+                for (int j = 0; j < D / 16; ++j) o[j][n][e] *= f, o[j][n][2 + e] *= f;
+              }
+              more[n][0] = more[n][1] = 0.f;
+#pragma unroll
+              for (int i = 0; i < MT; ++i)
+#pragma unroll
+                for (int b = 0; b < 2; ++b) {
+#pragma unroll
+                  for (int e = 0; e < 2; ++e) more[n][e] += ex2(s[i][n][2 * b + e] - base[e]);
+                  p16[i][n][b] = pack_f16(ex2(so[i][b][0] - base_o[0]), ex2(so[i][b][1] - base_o[1]));
+                }
+            }
+            unset = __any_sync(0xffffffffu, unset);
           }
+#pragma unroll
+          for (int n = 0; n < NT; ++n) l[n][0] += more[n][0], l[n][1] += more[n][1];
 #pragma unroll
           for (int i = 0; i < MT; ++i) {
             uint32_t pf[NT][2];   // keys 2 qd, + 1 (then + 8) of row gq
 #pragma unroll
             for (int n = 0; n < NT; ++n) {
-              pf[n][0] = transposed(pack_f16(s[i][n][0], s[i][n][1]));
-              pf[n][1] = transposed(pack_f16(s[i][n][2], s[i][n][3]));
+              pf[n][0] = transposed(p16[i][n][0]);
+              pf[n][1] = transposed(p16[i][n][1]);
             }
             uint32_t keep[2] = {~0u, ~0u};   // codes past the sequence's end may be those of NaN
             if (masked) {
@@ -665,20 +678,20 @@ __global__ void __launch_bounds__(RowsCfg<D>::kThreads, 1) k_attn_rows_fp8(const
       ++turn;
       if (kSplit && !meet()) return false;   // both warps of a pair have read all of its keys
       float* slot = g.parts > 1 ? part_slot(P, g.first_cta, g.part, C::kPart) : nullptr;
-      const float u0 = 0.015625f;   // 2^-6
       float2* ml_of = join_ml[turn & 1];
+      float* top_of = join_top[turn & 1];
 #pragma unroll
       for (int n = 0; n < NT; ++n)
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
           const int row = 8 * n + 2 * qd + e;
-          const float sum = keys_sum(l[n][e]), u1 = power_of(v_top + own[n][e]);   // the largest power
+          const float sum = keys_sum(l[n][e]);
           if (row_first + row < g.s.rows) {
             float* dst = part_row(warp, row) + 2 * gq;
 #pragma unroll
             for (int j = 0; j < D / 16; ++j)
-              *reinterpret_cast<float2*>(dst + 16 * j) = make_float2(o[j][n][e] * u0 * u1, o[j][n][2 + e] * u0 * u1);
-            if (gq == 0) ml_of[warp * 16 + row] = make_float2(m[n][e], sum);
+              *reinterpret_cast<float2*>(dst + 16 * j) = make_float2(o[j][n][e], o[j][n][2 + e]);
+            if (gq == 0) ml_of[warp * 16 + row] = make_float2(m[n][e], sum), top_of[warp * 16 + row] = M[n][e];
           }
         }
       // warps without a row too: the slots that they hand back have to be the ones that all are at
@@ -690,14 +703,17 @@ __global__ void __launch_bounds__(RowsCfg<D>::kThreads, 1) k_attn_rows_fp8(const
         const int hi = kSplit ? row >> 4 : 0, r16 = row & 15;
         const auto warp_of = [&](int i) { return kSplit ? 2 * i + hi : i; };
         float2 ml[kParts];
-        float mm = -INFINITY, ll = 0.f;
+        float fo[kParts], mm = -INFINITY, ll = 0.f, top = -INFINITY;
 #pragma unroll
-        for (int i = 0; i < kParts; ++i) ml[i] = ml_of[warp_of(i) * 16 + r16], mm = fmaxf(mm, ml[i].x);
-        const float base = mm == -INFINITY ? 0.f : mm;
+        for (int i = 0; i < kParts; ++i) {
+          ml[i] = ml_of[warp_of(i) * 16 + r16], fo[i] = top_of[warp_of(i) * 16 + r16];
+          mm = fmaxf(mm, ml[i].x), top = fmaxf(top, fo[i]);
+        }
+        const float base = mm == -INFINITY ? 0.f : mm, base_o = top == -INFINITY ? 0.f : top;
 #pragma unroll
-        for (int i = 0; i < kParts; ++i) ml[i].x = ex2(ml[i].x - base), ll = fmaf(ml[i].y, ml[i].x, ll);
+        for (int i = 0; i < kParts; ++i) ll = fmaf(ml[i].y, ex2(ml[i].x - base), ll), fo[i] = ex2(fo[i] - base_o);
         const int tok = row_token(P, row0<kTwo>(g) + row), hd = row0<kTwo>(g) + row - tok * P.group;
-        const float inv = g.s.seen(tok) > 0 ? 1.f / ll : 0.f;
+        const float2 back = back_from(mm, ll, top, g.s.seen(tok) > 0);
 #pragma unroll
         for (int c = 0; c < (D / 4 + kWidth - 1) / kWidth; ++c) {
           const int piece = at + kWidth * c;
@@ -706,17 +722,17 @@ __global__ void __launch_bounds__(RowsCfg<D>::kThreads, 1) k_attn_rows_fp8(const
 #pragma unroll
           for (int i = 0; i < kParts; ++i) {
             const float4 x = reinterpret_cast<const float4*>(part_row(warp_of(i), r16))[piece];
-            const float f = ml[i].x;
+            const float f = fo[i];
             a.x = fmaf(x.x, f, a.x), a.y = fmaf(x.y, f, a.y), a.z = fmaf(x.z, f, a.z), a.w = fmaf(x.w, f, a.w);
           }
           if (slot)
             reinterpret_cast<float4*>(slot + row * D)[piece] = a;
           else
             reinterpret_cast<uint2*>(P.out + ((int64_t)(g.s.tok0 + tok) * P.q_heads + g.h * P.group + hd) * D)[piece] =
-                make_uint2(pack_bf16(a.x * inv, a.y * inv), pack_bf16(a.z * inv, a.w * inv));
+                make_uint2(pack_bf16(a.x * back.x * back.y, a.y * back.x * back.y), pack_bf16(a.z * back.x * back.y, a.w * back.x * back.y));
         }
         if (slot && at < 2)   // a whole sector
-          reinterpret_cast<float4*>(slot + C::kRows * D + kPartPad * row)[at] = make_float4(at == 0 ? mm : 0.f, at == 0 ? ll : 0.f, 0.f, 0.f);
+          reinterpret_cast<float4*>(slot + C::kRows * D + kPartPad * row)[at] = at == 0 ? make_float4(mm, ll, top, 0.f) : make_float4(0.f, 0.f, 0.f, 0.f);
       }
       asm volatile("fence.proxy.async.shared::cta;" ::: "memory");   // the slots were written here; copies overwrite them
       __syncwarp();
