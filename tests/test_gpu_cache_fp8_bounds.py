@@ -40,8 +40,8 @@ def _rand(shape, seed, scale=1.0):
     return (torch.randn(shape, generator=g, device="cuda") * scale).to(torch.bfloat16)
 
 
-def reference(q, cache, table, new, kv, scale, few):
-    """(out, bound) in 64 bits."""
+def reference(q, cache, table, new, kv, scale, few, weight=None):
+    """(out, bound) in 64 bits.  weight: what to round the weights (largest: 1) to, to see what a bound tells apart."""
     T, hq, d = q.shape
     hkv, g = cache.kv_heads, hq // cache.kv_heads
     codes_of, s_of = cache.v_pages.float().double(), f8.scale_values(cache.v_scales)
@@ -59,6 +59,8 @@ def reference(q, cache, table, new, kv, scale, few):
         seen = (torch.arange(m, device=q.device)[None] <= (m - n + torch.arange(n, device=q.device)).repeat(g)[:, None])
         w = (sc - sc.masked_fill(~seen, -math.inf).amax(-1, keepdim=True)).exp() * seen
         total = w.sum(-1, keepdim=True)
+        if weight is not None:
+            w = w.to(weight).double()
         p = w / total
         V = C * S.transpose(1, 2)
         o, a = p @ V, p @ V.abs()
@@ -80,6 +82,13 @@ def _check(gs, cache, table, q, few, new, kv, scale, what):
     ref.assert_close(got, want, bound, what)
     assert torch.equal(got, gs.paged_attention(q, cache, b, scale)) and gs.device_status() == gs.GS_OK
     return got
+
+
+@pytest.mark.parametrize("few,hq,hkv,d,new,kv", FORMS)
+@pytest.mark.parametrize("vscale", [1.0, 2.0 ** -60, 2.0 ** -90, 2.0 ** 40])
+def test_each_form_within_its_own_bound(gs, few, hq, hkv, d, new, kv, vscale):
+    cache, table = f8.make_cache(gs, kv, hkv, d, 32, 200, vscale=vscale)
+    _check(gs, cache, table, _rand((sum(new), hq, d), 201, 1.0), few, new, kv, d ** -0.5, f"values of {vscale}")
 
 
 @pytest.mark.parametrize("few,hq,hkv,d,new,kv", FORMS)
@@ -110,3 +119,23 @@ def test_values_of_all_sizes_under_weights_of_all_sizes(gs, few, hq, hkv, d, new
     g = torch.Generator(device="cuda").manual_seed(221)
     vs += torch.where(vs == 255, 0, torch.randint(-60, 61, vs.shape, generator=g, device="cuda")).to(torch.uint8)
     _check(gs, cache, table, _rand((sum(new), hq, d), 222), few, new, kv, scale * d ** -0.5, "powers at random")
+
+
+@pytest.mark.parametrize("d", [64, 128])
+def test_weights_of_few_rows_keep_eleven_bits(gs, d):
+    """A few keys whose values are one vector and its opposite: what is left of them is the weights' differences.  Weights
+    rounded to bf16 are outside the bound, rounded to f16 inside."""
+    n, hkv = 96, 4
+    kv = [2 + i % 5 for i in range(n)]
+    cache, table = f8.make_cache(gs, kv, hkv, d, 16, 240)
+    ks = cache.k_scales.view(torch.uint8)
+    ks -= 4 * (ks != 255)
+    u = f8.bytes_of(f8.quantise(_rand((hkv, 1, d), 241).double())[0]) & 127
+    cache.v_pages.view(torch.uint8).copy_((u + 128 * (torch.arange(16, device="cuda") % 2)[:, None].to(torch.uint8)).expand(cache.v_pages.shape))
+    cache.v_scales.view(torch.uint8).fill_(127)
+    q = _rand((n, hkv, d), 242)
+    _check(gs, cache, table, q, True, [1] * n, kv, d ** -0.5, "opposite values")
+    want, bound = reference(q, cache, table, [1] * n, kv, d ** -0.5, True)
+    for weight, inside in ((torch.bfloat16, False), (torch.float16, True)):
+        other, _ = reference(q, cache, table, [1] * n, kv, d ** -0.5, True, weight)
+        assert bool(((other - want).abs() <= bound).all()) == inside
