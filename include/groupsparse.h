@@ -594,7 +594,8 @@ gs_status gs_cache_read_fp8(const gs_paged_cache_fp8* cache, const gs_seq_batch*
  * product the weights are rounded to bf16, or, for sequences of few rows (new tokens x
  * query heads a key head; 32, or 64 where sequences x key heads are few), weights times
  * their values' scales s to f16: 11 bits of each, or steps of 2^-30 of the row's largest
- * weight times scale.  A key or value that is NaN reaches the tokens that see it, and no
+ * weight times scale.  No sum of values leaves float32's range where scales are 2^119 at
+ * most (many rows: for 2^16 visible keys at least).  A key or value that is NaN reaches the tokens that see it, and no
  * others.  Memory past a sequence's length may hold anything; codes of NaN (0x7f, 0xff) at
  * positions of a sequence, which gs_cache_append_fp8 does not write, may reach any token of it.
  * Arguments, workspace (of its own workspace call), captured graphs and errors as there.

@@ -216,7 +216,9 @@ __device__ __forceinline__ uint32_t times(uint32_t x, uint32_t m) {
 // Two e4m3 codes of a word as bf16, times m.  A code's four exponent and three fraction bits are moved to where bf16 has the
 // ends of its own, which makes them 2^-120 of their value (zeros and subnormals too); the product is exact.  kPick: the codes into
 // the upper bytes.  m = 2^(120 + e) is a bf16 up to e = 7, the power kHighPower.
-constexpr uint32_t kHighPower = 134u;
+// Values become 2^-kDown of what they are, which the division by the sum of weights gives back: sums of up to 2^16 of the largest
+// (448 * 2^119, weights of up to 2^8) stay in float32's range so, and the smallest codes (2^-109) are still bf16's least number.
+constexpr uint32_t kHighPower = 134u, kDown = 24u;
 template <uint32_t kPick>
 __device__ __forceinline__ uint32_t bf16_of(uint32_t codes, uint32_t m) {
   const uint32_t t = __byte_perm(codes, 0u, kPick);
@@ -554,6 +556,7 @@ __global__ void __launch_bounds__(ChunkCfg<D, k8>::kThreads, 1) k_attn_chunk(con
       const int row = lane / kLanes, col = lane % kLanes;
       const bool odd = (col >> 2) & 1;   // these lanes store their second half first, into other banks than the rest
       const uint32_t src0 = smem_u32(v ? raw_v : raw_k) + (uint32_t)((16 * mine + row) * D + 16 * col);
+      const uint32_t up = v ? 120u - kDown : 120u;
       const uint32_t dst0 = smem_u32(v ? ring_v : ring_k) + (uint32_t)((16 * mine + row) * 128 + (col >> 2) * (kCT * 128));
       uint32_t raw = 0, rph = 0u, slot = 0, ph = 1u;
       bool ok = true;
@@ -580,7 +583,7 @@ __global__ void __launch_bounds__(ChunkCfg<D, k8>::kThreads, 1) k_attn_chunk(con
             const int k = i * kStep + row;   // of this warp's 16
             const uint4 c = codes[i];
             const uint32_t code = power[i];
-            const uint32_t m = (code == 0u ? 0u : min(code, kHighPower) + 120u << 7) * 0x10001u;
+            const uint32_t m = (code == 0u ? 0u : min(code, kHighPower) + up << 7) * 0x10001u;
             const uint32_t x0 = odd ? c.z : c.x, x1 = odd ? c.w : c.y, x2 = odd ? c.x : c.z, x3 = odd ? c.y : c.w;
             const uint32_t q = (2 * (col & 3) + odd) ^ ((16 * mine + k) & 7);
             store16(dst + i * (kStep * 128) + (q << 4), bf16_of<0x1404>(x0, m), bf16_of<0x3424>(x0, m), bf16_of<0x1404>(x1, m), bf16_of<0x3424>(x1, m));
@@ -933,7 +936,7 @@ __global__ void __launch_bounds__(ChunkCfg<D, k8>::kThreads, 1) k_attn_chunk(con
           }
           // A lane has a whole row: 64 bytes of it, in two sectors.
           if (row.on) {
-            const float inv = row.vis > 0 ? reciprocal(sum) : 0.f;
+            const float inv = row.vis > 0 ? reciprocal(sum) * (k8 ? (float)(1u << kDown) : 1.f) : 0.f;
             uint32_t w[16];
 #pragma unroll
             for (int e = 0; e < 16; ++e) w[e] = pack_bf16(o[2 * e] * inv, o[2 * e + 1] * inv);

@@ -121,6 +121,21 @@ def test_values_of_all_sizes_under_weights_of_all_sizes(gs, few, hq, hkv, d, new
     _check(gs, cache, table, _rand((sum(new), hq, d), 222), few, new, kv, scale * d ** -0.5, "powers at random")
 
 
+@pytest.mark.parametrize("few,hq,hkv,d,new,kv", FORMS)
+def test_sums_of_the_largest_values_are_finite(gs, few, hq, hkv, d, new, kv):
+    """Many keys of the same weight, all with the largest value that append writes: their mean is that value."""
+    cache, table = f8.make_cache(gs, kv, hkv, d, 32, 230)
+    cache.k_pages.view(torch.uint8).zero_()
+    cache.k_scales.view(torch.uint8).fill_(127)
+    sign = torch.where(torch.arange(d, device="cuda") % 3 == 0, 0xFE, 0x7E).to(torch.uint8)
+    cache.v_pages.view(torch.uint8).copy_(sign.expand(cache.v_pages.shape))
+    cache.v_scales.view(torch.uint8).fill_(246)
+    b = gs.Batch(ref.offsets(new), ref.i32(kv), table, max(new))
+    got = gs.paged_attention(_rand((sum(new), hq, d), 231), cache, b)
+    want = (sign.view(torch.float8_e4m3fn).double() * 2.0 ** 119).to(torch.bfloat16)
+    assert torch.equal(got, want.expand(got.shape))
+
+
 @pytest.mark.parametrize("d", [64, 128])
 def test_weights_of_few_rows_keep_eleven_bits(gs, d):
     """A few keys whose values are one vector and its opposite: what is left of them is the weights' differences.  Weights
