@@ -93,20 +93,51 @@ __global__ void __launch_bounds__(kAppThreads) k_cache_append(const AppendParams
       if (t >= first) pos = (int64_t)__ldg(P.kv_lens + seq) - (end - first) + (t - first);
     }
   }
+  if (!k8 && H == 1 && !on[0]) return;   // in 8 bits a warp's threads meet below
   const bool turn = pos >= 0 && pos < P.n_pos;
   int64_t page = -1;
   // one head a thread: loads that its kind needs; two: all of them, without a branch before the next one's
   if (turn && (H > 1 || kind[0] != 0) && (pos >> P.page_shift) < P.width)
     page = __ldg(P.table + (int64_t)seq * P.width + (pos >> P.page_shift));
-  const int64_t slot = pos & ((1 << P.page_shift) - 1);
   float c[8], n[8];
-  if (turn && (H > 1 || kind[0] != 2)) {
+  const auto load_angles = [&]() {
     const float4* cp = reinterpret_cast<const float4*>(P.cos_t + pos * (D / 2) + 8 * i);
     const float4* sp = reinterpret_cast<const float4*>(P.sin_t + pos * (D / 2) + 8 * i);
     const float4 c0 = __ldg(cp), c1 = __ldg(cp + 1), s0 = __ldg(sp), s1 = __ldg(sp + 1);
     c[0] = c0.x, c[1] = c0.y, c[2] = c0.z, c[3] = c0.w, c[4] = c1.x, c[5] = c1.y, c[6] = c1.z, c[7] = c1.w;
     n[0] = s0.x, n[1] = s0.y, n[2] = s0.z, n[3] = s0.w, n[4] = s1.x, n[5] = s1.y, n[6] = s1.z, n[7] = s1.w;
+  };
+  if constexpr (!k8) {
+    // One head a thread: the angles are loaded where they are used.  (In one path with 8 bits, which
+    // converts what it does not turn too: 44 registers instead of 40; 3000 tokens of 28 + 2 x 4 heads, out of L2, 9.1 us, not 8.4.)
+    if (H > 1 && turn) load_angles();
+#pragma unroll
+    for (int h = 0; h < H; ++h) {
+      uint32_t aw[4] = {a[h].x, a[h].y, a[h].z, a[h].w}, bw[4] = {b[h].x, b[h].y, b[h].z, b[h].w};
+      if (turn && kind[h] != 2) {
+        if (H == 1) load_angles();
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const float al = bf16_lo(aw[e]), ah = bf16_hi(aw[e]), bl = bf16_lo(bw[e]), bh = bf16_hi(bw[e]);
+          aw[e] = pack_bf16(al * c[2 * e] - bl * n[2 * e], ah * c[2 * e + 1] - bh * n[2 * e + 1]);
+          bw[e] = pack_bf16(bl * c[2 * e] + al * n[2 * e], bh * c[2 * e + 1] + ah * n[2 * e + 1]);
+        }
+      }
+      if (!on[h]) continue;
+      uint16_t* dst;
+      if (kind[h] == 0) {
+        dst = P.q_out + (t * P.q_heads + head[h]) * D;
+      } else {
+        if (page < 0 || page >= P.pages) continue;   // no place for this token
+        const int64_t slot = pos & ((1 << P.page_shift) - 1);
+        dst = (kind[h] == 1 ? P.k_pages : P.v_pages) + (((page * P.kv_heads + head[h]) << P.page_shift) + slot) * D;
+      }
+      reinterpret_cast<uint4*>(dst)[i] = make_uint4(aw[0], aw[1], aw[2], aw[3]);
+      reinterpret_cast<uint4*>(dst + D / 2)[i] = make_uint4(bw[0], bw[1], bw[2], bw[3]);
+    }
+    return;
   }
+  if (turn && (H > 1 || kind[0] != 2)) load_angles();
 #pragma unroll
   for (int h = 0; h < H; ++h) {
     uint32_t aw[4] = {a[h].x, a[h].y, a[h].z, a[h].w}, bw[4] = {b[h].x, b[h].y, b[h].z, b[h].w};
@@ -123,29 +154,27 @@ __global__ void __launch_bounds__(kAppThreads) k_cache_append(const AppendParams
       }
     }
     const bool placed = page >= 0 && page < P.pages;
+    const int64_t slot = pos & ((1 << P.page_shift) - 1);
     const int64_t row = placed ? ((page * P.kv_heads + head[h]) << P.page_shift) + slot : 0;
-    if constexpr (k8) {
-      uint32_t top = 0;   // bits of magnitudes: ordered like them, NaN above all
-      if (H > 1 || kind[h] != 0) {
+    uint32_t top = 0;   // bits of magnitudes: ordered like them, NaN above all
+    if (H > 1 || kind[h] != 0) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) top = max(top, max(__float_as_uint(ak[e]) & 0x7FFFFFFFu, __float_as_uint(bk[e]) & 0x7FFFFFFFu));
-      }
-      for (int d = per / 2; d > 0; d >>= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, d));   // a head's threads need each other
-      if (on[h] && kind[h] != 0 && placed) {
-        const bool finite = top < 0x7F800000u;
-        const int code = finite ? min(max((int)(top >> 23) - 8 + ((top & 0x7FFFFFu) > 0x600000u ? 1 : 0), 27), 246) : 255;
-        const float inv = finite ? __uint_as_float((uint32_t)(254 - code) << 23) : 0.f;
-        uint8_t* dst = reinterpret_cast<uint8_t*>(kind[h] == 1 ? P.k_pages : P.v_pages) + row * D + 8 * i;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) ak[e] = finite ? ak[e] * inv : 0.f, bk[e] = finite ? bk[e] * inv : 0.f;
-        *reinterpret_cast<uint2*>(dst) = make_uint2(pack_e4m3(ak[0], ak[1], ak[2], ak[3]), pack_e4m3(ak[4], ak[5], ak[6], ak[7]));
-        *reinterpret_cast<uint2*>(dst + D / 2) = make_uint2(pack_e4m3(bk[0], bk[1], bk[2], bk[3]), pack_e4m3(bk[4], bk[5], bk[6], bk[7]));
-        if (i == 0) (kind[h] == 1 ? P.k_scales : P.v_scales)[row] = (uint8_t)code;
-      }
-      if (kind[h] != 0) continue;
+      for (int e = 0; e < 8; ++e) top = max(top, max(__float_as_uint(ak[e]) & 0x7FFFFFFFu, __float_as_uint(bk[e]) & 0x7FFFFFFFu));
     }
-    if (!on[h] || (kind[h] != 0 && !placed)) continue;   // no place for this token
-    uint16_t* dst = kind[h] == 0 ? P.q_out + (t * P.q_heads + head[h]) * D : (kind[h] == 1 ? P.k_pages : P.v_pages) + row * D;
+    for (int d = per / 2; d > 0; d >>= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, d));   // a head's threads need each other
+    if (on[h] && kind[h] != 0 && placed) {
+      const bool finite = top < 0x7F800000u;
+      const int code = finite ? min(max((int)(top >> 23) - 8 + ((top & 0x7FFFFFu) > 0x600000u ? 1 : 0), 27), 246) : 255;
+      const float inv = finite ? __uint_as_float((uint32_t)(254 - code) << 23) : 0.f;
+      uint8_t* dst = reinterpret_cast<uint8_t*>(kind[h] == 1 ? P.k_pages : P.v_pages) + row * D + 8 * i;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) ak[e] = finite ? ak[e] * inv : 0.f, bk[e] = finite ? bk[e] * inv : 0.f;
+      *reinterpret_cast<uint2*>(dst) = make_uint2(pack_e4m3(ak[0], ak[1], ak[2], ak[3]), pack_e4m3(ak[4], ak[5], ak[6], ak[7]));
+      *reinterpret_cast<uint2*>(dst + D / 2) = make_uint2(pack_e4m3(bk[0], bk[1], bk[2], bk[3]), pack_e4m3(bk[4], bk[5], bk[6], bk[7]));
+      if (i == 0) (kind[h] == 1 ? P.k_scales : P.v_scales)[row] = (uint8_t)code;
+    }
+    if (!on[h] || kind[h] != 0) continue;
+    uint16_t* dst = P.q_out + (t * P.q_heads + head[h]) * D;
     reinterpret_cast<uint4*>(dst)[i] = make_uint4(aw[0], aw[1], aw[2], aw[3]);
     reinterpret_cast<uint4*>(dst + D / 2)[i] = make_uint4(bw[0], bw[1], bw[2], bw[3]);
   }
