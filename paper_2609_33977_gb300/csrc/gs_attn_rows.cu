@@ -26,7 +26,6 @@ namespace {
 using namespace sm100;
 
 constexpr int kTile = 128;
-
 constexpr int kJoin = 8;   // rows of parts that a warp has under way when it joins them
 // Parts joined in one level: the three long sequences above take 53 us, 55 with at most 8, 4 tokens of 28/4 heads at 60000
 // keys 42 (always one level: 46).  More go in groups of at most sqrt(256).
@@ -82,69 +81,27 @@ struct RowsCfg {
   static_assert(kSmem <= 227 * 1024 - 4096, "shared memory budget");
 };
 
-// The last of a split item's CTAs joins its parts, in order: by all computing warps, whose barrier meet() is.  false: some
-// role gave up.
-template <int D, int ROWS, int WARPS, class Meet>
-__device__ __forceinline__ bool join_parts(const AttnParams& P, const Segment& g, int warp, int lane, int* last_s, Meet meet) {
-  using L = Lane<D>;
-  constexpr int kC = D / 32, kPart = ROWS * (D + kPartPad);
-#pragma unroll 1
-  for (int level = 0; level < 2; ++level) {
-    const JoinStep j = join_step(g, level, kFlat);
-    if (j.n > 1) {
-      __threadfence();
-      if (!meet()) return false;
-      if (threadIdx.x == 0) {
-        int32_t* cnt = P.cnt + level * (int)gridDim.x + g.first_cta + j.first;
-        *last_s = atomicAdd(cnt, 1) == j.n - 1;
-        if (*last_s) *cnt = 0;
-        __threadfence();
-      }
-      if (!meet()) return false;
-      if (!*last_s) break;
-      for (int row = warp; row < g.s.rows; row += WARPS) {   // a warp a row, a lane a part's maximum and sum
-        const auto part_at = [&](int i) { return part_slot(P, g.first_cta, j.first + i * j.stride, kPart); };
-        float2 ml = __ldcg(reinterpret_cast<const float2*>(part_at(min(lane, j.n - 1)) + ROWS * D + kPartPad * row));
-        if (lane >= j.n) ml = make_float2(-INFINITY, 0.f);
-        float mm = ml.x;
-#pragma unroll
-        for (int d = 16; d > 0; d >>= 1) mm = fmaxf(mm, __shfl_xor_sync(0xffffffffu, mm, d));
-        const float fp = ex2(ml.x - (mm == -INFINITY ? 0.f : mm));
-        float ll = ml.y * fp, a[kC];
-#pragma unroll
-        for (int d = 16; d > 0; d >>= 1) ll += __shfl_xor_sync(0xffffffffu, ll, d);
-#pragma unroll
-        for (int c = 0; c < kC; ++c) a[c] = 0.f;
-#pragma unroll 1
-        for (int p0 = 0; p0 < j.n; p0 += kJoin) {
-          typename L::V v[kJoin];
-#pragma unroll
-          for (int i = 0; i < kJoin; ++i)
-            v[i] = __ldcg(reinterpret_cast<const typename L::V*>(part_at(min(p0 + i, j.n - 1)) + row * D) + lane);
-#pragma unroll
-          for (int i = 0; i < kJoin; ++i) {
-            const float f = __shfl_sync(0xffffffffu, fp, (p0 + i) & 31);
-            float x[kC];
-            L::unpack(v[i], x);
-            if (p0 + i < j.n) {
-#pragma unroll
-              for (int c = 0; c < kC; ++c) a[c] = fmaf(x[c], f, a[c]);
-            }
-          }
-        }
-        if (!j.last) {   // in the place of the group's first part
-          store_part<D, ROWS>(part_at(0), row, lane, a, mm, ll);
-        } else {
-          const int tok = row_token(P, row), hd = row - tok * P.group;
-          L::store_bf16(P.out + ((int64_t)(g.s.tok0 + tok) * P.q_heads + g.h * P.group + hd) * D + kC * lane, a,
-                        g.s.seen(tok) > 0 ? 1.f / ll : 0.f);
-        }
-      }
-    }
-    if (j.last) break;
+// a row's D / 32 channels per lane
+template <int D>
+struct Lane;
+template <>
+struct Lane<128> {
+  using V = float4;
+  static __device__ __forceinline__ void unpack(const V& v, float (&a)[4]) { a[0] = v.x, a[1] = v.y, a[2] = v.z, a[3] = v.w; }
+  static __device__ __forceinline__ V pack(const float (&a)[4]) { return make_float4(a[0], a[1], a[2], a[3]); }
+  static __device__ __forceinline__ void store_bf16(uint16_t* dst, const float (&a)[4], float f) {
+    *reinterpret_cast<uint2*>(dst) = make_uint2(pack_bf16(a[0] * f, a[1] * f), pack_bf16(a[2] * f, a[3] * f));
   }
-  return true;
-}
+};
+template <>
+struct Lane<64> {
+  using V = float2;
+  static __device__ __forceinline__ void unpack(const V& v, float (&a)[2]) { a[0] = v.x, a[1] = v.y; }
+  static __device__ __forceinline__ V pack(const float (&a)[2]) { return make_float2(a[0], a[1]); }
+  static __device__ __forceinline__ void store_bf16(uint16_t* dst, const float (&a)[2], float f) {
+    *reinterpret_cast<uint32_t*>(dst) = pack_bf16(a[0] * f, a[1] * f);
+  }
+};
 
 template <int D, int WR>
 __global__ void __launch_bounds__(RowsCfg<D, WR>::kThreads, 1) k_attn_rows(const __grid_constant__ AttnParams P) {
@@ -266,6 +223,12 @@ __global__ void __launch_bounds__(RowsCfg<D, WR>::kThreads, 1) k_attn_rows(const
       const bool met = wait_warp(&meet_bar, mph);
       mph ^= 1u;
       return met;
+    };
+    // A part: [rows][D], then [rows][8] with maximum and sum, the rest zeros: a 32-byte sector that is written in part
+    // costs whoever reads it a fill from HBM.
+    const auto store_part = [&](float* slot, int row, const float (&a)[kC], float mm, float ll) {
+      reinterpret_cast<typename L::V*>(slot + row * D)[lane] = L::pack(a);
+      if (lane < 2) reinterpret_cast<float4*>(slot + C::kRows * D + kPartPad * row)[lane] = lane == 0 ? make_float4(mm, ll, 0.f, 0.f) : make_float4(0.f, 0.f, 0.f, 0.f);
     };
     uint32_t st = 0, ph = 0u, turn = 0, qs = 0;
     bool ok = true;
@@ -510,7 +473,7 @@ __global__ void __launch_bounds__(RowsCfg<D, WR>::kThreads, 1) k_attn_rows(const
           }
         }
         if (slot) {
-          store_part<D, C::kRows>(slot, row, lane, a, mm, ll);
+          store_part(slot, row, a, mm, ll);
         } else {
           L::store_bf16(P.out + ((int64_t)(g.s.tok0 + tok) * P.q_heads + g.h * P.group + hd) * D + kC * lane, a,
                         vis > 0 ? 1.f / ll : 0.f);
@@ -524,7 +487,62 @@ __global__ void __launch_bounds__(RowsCfg<D, WR>::kThreads, 1) k_attn_rows(const
         ph ^= 1u;
       }
       if (slot) {
-        ok = join_parts<D, C::kRows, C::kWarps>(P, g, warp, lane, &last_s, meet);
+        // ---- the last of the item's CTAs joins its parts, in order
+#pragma unroll 1
+        for (int level = 0; level < 2; ++level) {
+          const JoinStep j = join_step(g, level, kFlat);
+          if (j.n > 1) {
+            __threadfence();
+            if (!(ok = meet())) break;
+            if (threadIdx.x == 0) {
+              int32_t* cnt = P.cnt + level * (int)gridDim.x + g.first_cta + j.first;
+              last_s = atomicAdd(cnt, 1) == j.n - 1;
+              if (last_s) *cnt = 0;
+              __threadfence();
+            }
+            if (!(ok = meet())) break;
+            if (!last_s) break;
+            for (int row = warp; row < g.s.rows; row += C::kWarps) {   // a warp a row, a lane a part's maximum and sum
+              const auto part_at = [&](int i) { return part_slot(P, g.first_cta, j.first + i * j.stride, C::kPart); };
+              float2 ml = __ldcg(reinterpret_cast<const float2*>(part_at(min(lane, j.n - 1)) + C::kRows * D + kPartPad * row));
+              if (lane >= j.n) ml = make_float2(-INFINITY, 0.f);
+              float mm = ml.x;
+#pragma unroll
+              for (int d = 16; d > 0; d >>= 1) mm = fmaxf(mm, __shfl_xor_sync(0xffffffffu, mm, d));
+              const float fp = ex2(ml.x - (mm == -INFINITY ? 0.f : mm));
+              float ll = ml.y * fp, a[kC];
+#pragma unroll
+              for (int d = 16; d > 0; d >>= 1) ll += __shfl_xor_sync(0xffffffffu, ll, d);
+#pragma unroll
+              for (int c = 0; c < kC; ++c) a[c] = 0.f;
+#pragma unroll 1
+              for (int p0 = 0; p0 < j.n; p0 += kJoin) {
+                typename L::V v[kJoin];
+#pragma unroll
+                for (int i = 0; i < kJoin; ++i)
+                  v[i] = __ldcg(reinterpret_cast<const typename L::V*>(part_at(min(p0 + i, j.n - 1)) + row * D) + lane);
+#pragma unroll
+                for (int i = 0; i < kJoin; ++i) {
+                  const float f = __shfl_sync(0xffffffffu, fp, (p0 + i) & 31);
+                  float x[kC];
+                  L::unpack(v[i], x);
+                  if (p0 + i < j.n) {
+#pragma unroll
+                    for (int c = 0; c < kC; ++c) a[c] = fmaf(x[c], f, a[c]);
+                  }
+                }
+              }
+              if (!j.last) {   // in the place of the group's first part
+                store_part(part_at(0), row, a, mm, ll);
+              } else {
+                const int tok = row_token(P, row), hd = row - tok * P.group;
+                L::store_bf16(P.out + ((int64_t)(g.s.tok0 + tok) * P.q_heads + g.h * P.group + hd) * D + kC * lane, a,
+                              g.s.seen(tok) > 0 ? 1.f / ll : 0.f);
+              }
+            }
+          }
+          if (j.last) break;
+        }
         if (!ok) break;
       }
     }

@@ -1,4 +1,6 @@
-// What the kernels for few rows share: fragments, and how a split item's parts lie in the workspace.
+// What the two kernels for few rows share: their most rows, the room of a row of a part, and loads of fragments.
+// A part is [rows][D], then [rows][kPartPad] with maximum and sum (over 8 bits the numerators' maximum too), the rest zeros:
+// a 32-byte sector that is written in part costs whoever reads it a fill from HBM.
 #pragma once
 
 #include "gs_attn.cuh"
@@ -7,6 +9,7 @@ namespace gs {
 
 constexpr int kMost = 32;      // rows
 constexpr int kPartPad = 8;    // floats of a row of a part beside the output's
+
 __device__ __forceinline__ void ldsm4(uint32_t (&v)[4], uint32_t addr) {
   asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];"
                : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3])
@@ -19,34 +22,4 @@ __device__ __forceinline__ void ldsm4t(uint32_t (&v)[4], uint32_t addr) {
                : "r"(addr)
                : "memory");
 }
-// a row's D / 32 channels per lane
-template <int D>
-struct Lane;
-template <>
-struct Lane<128> {
-  using V = float4;
-  static __device__ __forceinline__ void unpack(const V& v, float (&a)[4]) { a[0] = v.x, a[1] = v.y, a[2] = v.z, a[3] = v.w; }
-  static __device__ __forceinline__ V pack(const float (&a)[4]) { return make_float4(a[0], a[1], a[2], a[3]); }
-  static __device__ __forceinline__ void store_bf16(uint16_t* dst, const float (&a)[4], float f) {
-    *reinterpret_cast<uint2*>(dst) = make_uint2(pack_bf16(a[0] * f, a[1] * f), pack_bf16(a[2] * f, a[3] * f));
-  }
-};
-template <>
-struct Lane<64> {
-  using V = float2;
-  static __device__ __forceinline__ void unpack(const V& v, float (&a)[2]) { a[0] = v.x, a[1] = v.y; }
-  static __device__ __forceinline__ V pack(const float (&a)[2]) { return make_float2(a[0], a[1]); }
-  static __device__ __forceinline__ void store_bf16(uint16_t* dst, const float (&a)[2], float f) {
-    *reinterpret_cast<uint32_t*>(dst) = pack_bf16(a[0] * f, a[1] * f);
-  }
-};
-
-// A part: [rows][D], then [rows][8] with maximum and sum, the rest zeros: a 32-byte sector that is written in part
-// costs whoever reads it a fill from HBM.
-template <int D, int ROWS>
-__device__ __forceinline__ void store_part(float* slot, int row, int lane, const float (&a)[D / 32], float mm, float ll) {
-  reinterpret_cast<typename Lane<D>::V*>(slot + row * D)[lane] = Lane<D>::pack(a);
-  if (lane < 2) reinterpret_cast<float4*>(slot + ROWS * D + kPartPad * row)[lane] = lane == 0 ? make_float4(mm, ll, 0.f, 0.f) : make_float4(0.f, 0.f, 0.f, 0.f);
-}
-
 }  // namespace gs
