@@ -542,7 +542,7 @@ gs_status gs_paged_attention(const gs_paged_cache* cache, const gs_seq_batch* ba
  * reads.  A head's channels x of a token are held as e4m3 codes q with one power of two
  * s: q = x / s rounded to nearest even, where s = 2^e is the least power of two with
  * max|x| <= 448 s, but at least 2^-100 and at most 2^119 (beyond 448 * 2^119 codes are
- * +-448).  They stand for s q, which bf16 holds exactly.  Being a power of two, s costs
+ * +-448).  They stand for s q, which bf16 holds exactly for these s.  Being a power of two, s costs
  * no accuracy: an e4m3 code has the same four significant bits wherever it lies.
  * ------------------------------------------------------------------------ */
 
@@ -574,7 +574,8 @@ gs_status gs_cache_append_fp8(const gs_paged_cache_fp8* cache, const gs_seq_batc
  * at[i] + p of the outputs gets position p of sequence i, for all rows from at[i] to
  * at[i + 1] - 1.  Rows at or past the sequence's length, or whose page number is outside
  * [0, pages), get zeros; rows of no sequence are not written.  Out of 8 bits the values
- * are s q exactly (NaN where the scale is).
+ * are s q, exactly for scales from 2^-100 to 2^119, otherwise rounded to bf16 (below its least
+ * number to zero, above its largest to an infinity); NaN where the scale is.
  *
  * batch    its n, kv_lens_dev, table_dev and table_width are used.
  * at_dev   int32 [n + 1], non-decreasing, from 0 to at most `rows` (values outside are
@@ -598,6 +599,7 @@ gs_status gs_cache_read_fp8(const gs_paged_cache_fp8* cache, const gs_seq_batch*
  * most (many rows: for 2^16 visible keys at least).  A key or value that is NaN reaches the tokens that see it, and no
  * others.  Memory past a sequence's length may hold anything; codes of NaN (0x7f, 0xff) at
  * positions of a sequence, which gs_cache_append_fp8 does not write, may reach any token of it.
+ * Values under scales below 2^-100, which it does not write either, may be rounded to steps of 2^-109.
  * Arguments, workspace (of its own workspace call), captured graphs and errors as there.
  */
 gs_status gs_paged_attention_fp8_workspace(const gs_paged_cache_fp8* cache, const gs_seq_batch* batch, int32_t q_heads,
