@@ -22,9 +22,10 @@ from tests import _fp8_ref as f8
 
 pytestmark = pytest.mark.gpu
 
-# (query heads, key heads, width, new tokens, lengths).  At most 32 rows a key head, or 64 where sequences x key heads are few.
+# (query heads, key heads, width, new tokens, lengths).  At most 32 rows a key head, or 64 where sequences x key heads are few.  40000
+# keys of one key head lie in so many parts that they are joined in two levels.
 FEW = [(4, 4, 128, [1], [90]), (4, 4, 64, [1, 1], [700, 33]), (7, 1, 128, [1], [9000]), (28, 4, 128, [4], [300]), (28, 4, 128, [2, 1], [70, 2000]),
-       (16, 2, 64, [4, 2, 3], [500, 130, 1500]), (28, 4, 128, [9], [2000]), (8, 1, 64, [8, 5], [400, 90])]
+       (16, 2, 64, [4, 2, 3], [500, 130, 1500]), (7, 1, 128, [1], [40000]), (28, 4, 128, [9], [2000]), (8, 1, 64, [8, 5], [400, 90])]
 CHUNK = [(4, 4, 128, [150], [444]), (28, 4, 128, [100], [3000]), (16, 2, 64, [77, 200], [900, 200])]
 FORMS = [pytest.param(True, *f, id="few-" + "-".join(map(str, f))) for f in FEW] + [pytest.param(False, *f, id="chunk-" + "-".join(map(str, f))) for f in CHUNK]
 
