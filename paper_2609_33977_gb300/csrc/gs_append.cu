@@ -17,7 +17,7 @@
 //
 // Into 8 bits (k8): a head's threads agree on the largest magnitude, as float bits, whose
 // exponent (one more past 1.75, the fraction of 448) gives the power of two; it takes the place
-// of the bf16 rounding, so that keys are rounded once.  The same tokens 11.8 and 1.9 us, and 4096 of 40 + 2 x 40 heads 45.2 (4.7
+// of the bf16 rounding, so that keys are rounded once.  The same tokens 11.5 and 2.0 us, and 4096 of 40 + 2 x 40 heads 44.8 (4.7
 // TB/s; with one head a thread 49.9, but the 3000 of 28 + 2 x 4 would take 13.7 with two, a quarter of the threads idle).
 #include "gs_block.cuh"
 

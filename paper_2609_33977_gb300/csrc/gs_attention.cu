@@ -22,7 +22,7 @@ size_t parts_bytes(int size) { return (size_t)attention_ctas() * 2 * (size_t)siz
 // keys (28/4 heads) 6.9 / 10.0,  28 rows  16 x 4 tokens at 2000 keys 28.9 / 29.1,  32 rows
 // 16 x 32 (32 heads) 102.9 / 104.6;  above, in a few-row form for 64 rows and before the chunk
 // kernel's last steps,  16 x 9 41 / 34,  16 x 64 156 / 117.
-// Over 8 bits: 32 rows  16 x 32 (32 heads, 2000 keys) 103 / 137,  28 rows  4 tokens at 60000 keys 38.4 / 75.
+// Over 8 bits: 32 rows  16 x 32 (32 heads, 2000 keys) 103 / 137,  28 rows  4 tokens at 60000 keys 38.2 / 75.
 // Where all sequences are as long as the longest (known from the sizes alone), one launch does
 // (4096 tokens of 40 heads 154 us, both launches 158); otherwise the host cannot tell, and both
 // kernels look for theirs, the second on SMs that the first is through with (a mixed step of

@@ -37,8 +37,8 @@
 // Over a cache in 8 bits (k8) eight more warps turn the codes of a unit, as they arrive, into the bf16 tiles that the products
 // read: a code's bits moved to where bf16 has its own, times 2^(120 + e), exactly.  Every item converts the keys that it sees, so
 // half as many warps, or short items, wait for the conversion; otherwise it costs issue slots and shared memory's time, and the softmax
-// its registers (144 a thread instead of 200).  Prompts as above 266 us, 810 TFLOP/s (235 if nothing is converted; four converting
-// warps and 168 registers 323); 4096 tokens 203; 512 at 8192 keys 82.5; 64 at 8192, whose items have one half, 49.  Queries of one
+// its registers (144 a thread instead of 200).  Prompts as above 267 us, 807 TFLOP/s (235 if nothing is converted; four converting
+// warps and 168 registers 323); 4096 tokens 202; 512 at 8192 keys 83.4; 64 at 8192, whose items have one half, 49.5.  Queries of one
 // half in TMEM, for one buffer of P a half instead of two: 341.
 #include "gs_attn.cuh"
 

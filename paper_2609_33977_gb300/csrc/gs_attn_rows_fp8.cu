@@ -24,9 +24,10 @@
 // were.  Up to 16 rows, the two warps of a pair share its keys (tiles of 8 rows: one or two, by
 // the segment's own rows); above, its rows.
 //
-// 16 sequences of 90 to 4000 keys, 32 heads: 43.6 us, 4.9 TB/s (nothing computed 40.3, and parts of split items not joined
-// 36.7).  Three of 30001 to 65536 keys, 28/4 heads: 34.0 us, 4.4 TB/s; one of 60000: 23.4; four tokens there 38.4.  One of
-// 129 keys: 6.6 us.  24 of 2 to 16000 keys with 2 to 4 new tokens, 16/2 heads of 64: 20.4 us.   With 16 rows as the
+// 16 sequences of 90 to 4000 keys, 32 heads: 43.7 us, 4.9 TB/s (in an earlier form nothing computed 40.3, and parts of split
+// items not joined 36.7).  Three of 30001 to 65536 keys, 28/4 heads: 34.6 us, 4.3 TB/s; one of 60000: 24.0; four tokens there
+// 38.2.  One of 129 keys: 6.6 us.  24 of 2 to 16000 keys with 2 to 4 new tokens, 16/2 heads of 64: 20.8 us.  Scores that keep
+// passing the maximum cost more (keys' heads of sizes 2^-3 to 2^3 at random: 16 x 32 tokens at 2000 keys 124 us, else 103).   With 16 rows as the
 // products' rows instead, and one ring for all warps, the first three took 59.9, 40.8 and (129 keys) 7.8.
 #include "gs_attn_rows.cuh"
 
@@ -778,8 +779,9 @@ gs_status rows_launch(const AttnParams& P, int ctas, cudaStream_t s) {
 }  // namespace
 
 // Two row tiles read a sequence's keys twice, but are through sooner than an item of the chunk kernel's with its joins, unless
-// there are many items (28/4 heads, us here / in the chunk kernel): 9 tokens at 30000 keys 34.6 / 63.9, 5 at 8000 22.1 / 41.2, nine
-// sequences of 1 to 9 at 100 to 9000 29.5 / 50.5, 19 x 9 (76 items) at 2000 29.7 / 39.8, at 8000 88.9 / 79.9, 38 x 9 at 2000 54.5 / 42.4.
+// there are many items (28/4 heads, us here / in the chunk kernel): 9 tokens at 30000 keys 35.0 / 63.9, 5 at 8000 22.3 / 41.2, nine
+// sequences of 1 to 9 at 100 to 9000 29.5 / 50.5, 19 x 9 (76 items) at 2000 30.1 / 39.8, 38 x 9 at 2000 54.5 / 42.3.  The rule asks
+// for the items alone, although where they are half of the CTAs the length decides too: 19 x 9 at 8000 keys 89.6 / 79.9.
 int attn_rows_fp8_most(int64_t items, int ctas) { return 2 * items <= ctas ? 2 * kMost : kMost; }
 int attn_rows_fp8_box(int page_size) { return std::min(page_size, kSlotKeys); }
 
