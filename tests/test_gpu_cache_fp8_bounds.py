@@ -123,6 +123,40 @@ def test_values_of_all_sizes_under_weights_of_all_sizes(gs, few, hq, hkv, d, new
 
 
 @pytest.mark.parametrize("few,hq,hkv,d,new,kv", FORMS)
+@pytest.mark.parametrize("which", ["first", "all", "some", "keys"])
+def test_scales_of_zero_read_as_zero(gs, few, hq, hkv, d, new, kv, which):
+    """Heads whose scale byte is 0, whatever their codes: values of the first keys, of all keys, of some; or keys (a score of 0)."""
+    cache, table = f8.make_cache(gs, kv, hkv, d, 32, 250)
+    sc = (cache.k_scales if which == "keys" else cache.v_scales).view(torch.uint8)
+    some = torch.rand(sc.shape, generator=torch.Generator(device="cuda").manual_seed(251), device="cuda") < 0.7
+    if which == "all":
+        some.fill_(True)
+    if which == "first":
+        some.fill_(False)
+        for i, m in enumerate(kv):
+            pages = table[i, : -(-m // 32)].long()
+            for at, page in enumerate(pages.tolist()):
+                some[page, :, : max(0, min(32, m * 2 // 3 - 32 * at))] = True
+    sc.masked_fill_(some & (sc != 255), 0)
+    got = _check(gs, cache, table, _rand((sum(new), hq, d), 252), few, new, kv, d ** -0.5, which)
+    assert (got == 0).all() == (which == "all")
+
+
+@pytest.mark.parametrize("few,hq,hkv,d,new,kv", FORMS)
+@pytest.mark.parametrize("operand", [0, 1])
+def test_nan_at_the_first_key_stays_with_its_head(gs, few, hq, hkv, d, new, kv, operand):
+    cache, table = f8.make_cache(gs, kv, hkv, d, 32, 260)
+    q = _rand((sum(new), hq, d), 261)
+    b = gs.Batch(ref.offsets(new), ref.i32(kv), table, max(new))
+    clean = gs.paged_attention(q, cache, b)
+    (cache.k_scales, cache.v_scales)[operand].view(torch.uint8)[int(table[0, 0]), hkv - 1, 0] = 255
+    got = gs.paged_attention(q, cache, b)
+    own = torch.zeros(got.shape, dtype=torch.bool, device="cuda")
+    own[: new[0], hq - hq // hkv:] = True
+    assert got[own].isnan().all() and torch.equal(got[~own], clean[~own])
+
+
+@pytest.mark.parametrize("few,hq,hkv,d,new,kv", FORMS)
 def test_sums_of_the_largest_values_are_finite(gs, few, hq, hkv, d, new, kv):
     """Many keys of the same weight, all with the largest value that append writes: their mean is that value."""
     cache, table = f8.make_cache(gs, kv, hkv, d, 32, 230)
